@@ -66,7 +66,8 @@ enum {
 /* Sticky device flags (nuq_last_error_flags). */
 enum {
     NUQ_FLAG_CAPACITY = 1,  /* encoded words did not fit words_cap; words is incomplete */
-    NUQ_FLAG_NONFINITE = 2, /* a bucket norm was Inf/NaN; that bucket was encoded empty */
+    NUQ_FLAG_NONFINITE = 2, /* a bucket norm was Inf/NaN; that bucket was encoded empty. A gradient norm or
+                               new state of AdamW was: the step left that part as it was */
     NUQ_FLAG_MALFORMED = 4  /* a decoded stream broke the format, or nuq_encode refused a bucket; output is
                                incomplete */
 };
@@ -398,6 +399,94 @@ int nuq_moments_accumulate(const float *g, double *sum, double *sumsq, uint64_t 
 #define NUQ_VARIANCE_WORKSPACE_BYTES 16384u
 int nuq_normalized_variance(const double *sum, const double *sumsq, uint64_t d, uint64_t M, void *workspace,
                             uint64_t workspace_bytes, double *out2, nuq_stream_t stream);
+
+/* ---- training of transformers: AdamW, the gradients' norm, layer norm ------------------------------ */
+
+/* Element types. */
+#define NUQ_F32 0u
+#define NUQ_BF16 1u
+#define NUQ_F16 2u
+
+/* The norm of T tensors taken as one vector, and the factor that clips them.  g: HOST array of T device
+ * pointers, element-aligned (NULL where n is 0); n: HOST array of T counts; type: NUQ_F32, NUQ_BF16 or
+ * NUQ_F16.  out (DEVICE, 2 floats): out[0] = sqrt(sum of all g_i^2), out[1] = min(1, max_norm / out[0]).
+ * Summed in fp64 in an order that depends on the sizes alone: equal inputs give equal bits, and no square
+ * overflows.  Where the norm is not finite (or above the largest float) out[1] is NaN, which the steps
+ * below take as "leave everything as it is", and NUQ_FLAG_NONFINITE is raised.  max_norm: positive,
+ * infinite for the norm alone (NUQ_EINVAL otherwise).  workspace: DEVICE memory of at least
+ * NUQ_GRADIENT_NORM_WORKSPACE_BYTES bytes, 8-byte aligned, overwritten. */
+#define NUQ_GRADIENT_NORM_WORKSPACE_BYTES 65536u
+int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint32_t type, float max_norm,
+                      void *workspace, uint64_t workspace_bytes, float *out, nuq_stream_t stream);
+
+/* One AdamW step on T tensors at once; step t = 1, 2, ... of the tensors' states.  Per element, with
+ * lambda = decay[i] of its tensor and c = *coefficient (1 without):
+ *   g = c * gradient;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   w <- w (1 - alpha lambda) - alpha / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * w, g, m, v: HOST arrays of T device pointers to n[i] elements each (element-aligned; NULL where n[i]
+ * is 0), w, m, v fp32, g of type g_type; the arrays of a call must not overlap.  copy: NULL, or a HOST
+ * array of T device pointers to n[i] elements of copy_type (NUQ_BF16 or NUQ_F16): the new w, rounded
+ * to nearest, for a model that computes in 16 bits.  decay: HOST array of T, NULL for none.
+ * coefficient: DEVICE float, or NULL: nuq_gradient_norm's out + 1, or a scale that gradients were
+ * multiplied with, inverted.
+ * Evaluated in fp32, one rounding per product and sum in m and v; w within a few units of the last
+ * place of the subtracted term.  An element whose new m or v would not be finite keeps w, m and v
+ * (its copy is still written) and raises NUQ_FLAG_NONFINITE.
+ * NUQ_EINVAL: t = 0; alpha, beta or decay not finite; beta outside [0, 1); eps below 2^-126. */
+int nuq_adamw_step(uint32_t T, float *const *w, const void *const *g, float *const *m, float *const *v,
+                   void *const *copy, const uint64_t *n, const float *decay, uint32_t g_type,
+                   uint32_t copy_type, double alpha, double beta1, double beta2, double eps, uint64_t t,
+                   const float *coefficient, nuq_stream_t stream);
+
+/* The same with m and v held in 8 bits.  A tensor's elements are cut into blocks of NUQ_STATE_BLOCK (the
+ * last one short); scales[i] holds 2 * nuq_state_blocks(n[i]) floats, for block b  a = scales[2b] = its
+ * largest |m| and  e = scales[2b+1] = its largest v, both 0 where below 2^-126.  Code k of
+ *   m (n[i] bytes, OCP float8 e4m3): stands for  e4m3(k) * (a * 2^-8); stored is the code nearest to
+ *     m * (1/a) * 256;
+ *   v (n[i] bytes, unsigned float, 5 bits of exponent, 3 of fraction): stands for
+ *     float(bits k << 20) * 2^96 * e; stored is the code k whose float(bits k << 20), which may be
+ *     subnormal, is nearest to v * (1/e) * 2^-96, at least 1 where v > 0;
+ * nearest with ties to even, each product and quotient rounded to fp32.  The largest element of a block
+ * is held exactly.  All zeros (codes and scales) is the state before step 1.  The step uses the new m and
+ * v before they are rounded to codes.  A block with a new m or v that is not finite keeps w, codes and
+ * scales (its copy is still written) and raises NUQ_FLAG_NONFINITE.  Other arguments and errors as above. */
+#define NUQ_STATE_BLOCK 256u
+uint64_t nuq_state_blocks(uint64_t n);
+int nuq_adamw_step_coded(uint32_t T, float *const *w, const void *const *g, uint8_t *const *m,
+                         uint8_t *const *v, float *const *scales, void *const *copy, const uint64_t *n,
+                         const float *decay, uint32_t g_type, uint32_t copy_type, double alpha,
+                         double beta1, double beta2, double eps, uint64_t t, const float *coefficient,
+                         nuq_stream_t stream);
+
+/* m[n], v[n] (DEVICE floats) <- the values that the codes of one tensor stand for. */
+int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const float *scales, uint64_t n,
+                           float *m, float *v, nuq_stream_t stream);
+
+/* Layer norm of `rows` rows of `hidden` elements.  With s = x, or s = x + residual rounded to x's type
+ * and stored in total:  mean, var of the row (divided by hidden);  rstd = 1 / sqrt(var + eps);
+ * y = (s - mean) * rstd * weight + bias.
+ * x, residual, total, y: DEVICE, of `type`, element-aligned, row r at r * ld elements (ldx, ldr: any;
+ * ldt, ldy: at least hidden).  residual and total: both or neither.  weight, bias: hidden elements of
+ * weight_type (`type` or NUQ_F32), each may be NULL.  mean, rstd: `rows` floats each, may be NULL.
+ * y may be x.  Statistics in fp32, the variance from centred values.  eps: finite, not negative. */
+int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, uint64_t ldr,
+                           const void *weight, const void *bias, uint64_t rows, uint32_t hidden, float eps,
+                           uint32_t type, uint32_t weight_type, void *total, uint64_t ldt, void *y,
+                           uint64_t ldy, float *mean, float *rstd, nuq_stream_t stream);
+
+/* Its gradients, from dy, the forward's s (x, or total) and its mean and rstd.  With n = (s - mean) * rstd
+ * and d = dy * weight:  dx = rstd * (d - mean(d) - n * mean(d n)) (+ add), the gradient of x and of
+ * residual alike; add: the gradient that arrives through total, may be NULL.  dweight = sum over rows of
+ * dy * n, dbias = sum of dy (hidden elements of weight_type, each may be NULL): summed in fp32 in a fixed
+ * order, rounded once.  dx may be dy.  Row strides as above (ldg of dy, ldx, lda of add: any; ldd of dx
+ * at least hidden).  workspace: DEVICE memory, nuq_layer_norm_workspace_bytes(rows, hidden) bytes,
+ * 16-byte aligned, overwritten; may be NULL where neither dweight nor dbias is asked for. */
+uint64_t nuq_layer_norm_workspace_bytes(uint64_t rows, uint32_t hidden);
+int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_t ldx, const void *weight,
+                            const float *mean, const float *rstd, const void *add, uint64_t lda,
+                            uint64_t rows, uint32_t hidden, uint32_t type, uint32_t weight_type, void *dx,
+                            uint64_t ldd, void *dweight, void *dbias, void *workspace,
+                            uint64_t workspace_bytes, nuq_stream_t stream);
 
 /* ---- errors ---------------------------------------------------------------------- */
 

@@ -17,6 +17,9 @@ from .binding import (  # noqa: F401
     nuq_fixed_words, nuq_pack_fixed, nuq_quantize_pack_fixed_batch, nuq_unpack_accumulate_fixed,
     nuq_quantize_pack_fixed_table_batch, nuq_unpack_accumulate_fixed_table,
     nuq_momentum_step, nuq_decode_momentum_step, nuq_moments_accumulate, nuq_normalized_variance, VARIANCE_WORKSPACE_BYTES,
+    nuq_gradient_norm, GRADIENT_NORM_WORKSPACE_BYTES, nuq_adamw_step, nuq_adamw_step_coded, nuq_adamw_state_values,
+    nuq_state_blocks, STATE_BLOCK,
+    nuq_layer_norm_forward, nuq_layer_norm_backward, nuq_layer_norm_workspace_bytes,
     nuq_last_error_flags, library_path, exported_symbols,
     nuq_encode_shape, nuq_decode_tile, nuq_timing_begin, nuq_timing_collect, T_NORMS, T_QUANTIZE, T_ENCODE, T_QUANTIZE_ENCODE, T_DECODE,
 )

@@ -36,6 +36,7 @@ SYNC_BLOCK = 2048
 MAX_BUCKET, MAX_S, MAX_WORKERS = 32768, 14, 32
 
 _u64, _u32, _i32, _vp, _f32 = ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int, ctypes.c_void_p, ctypes.c_float
+_f64 = ctypes.c_double
 
 _SIGNATURES = {
     "nuq_num_buckets": (_u64, [_u64, _u32]),
@@ -80,6 +81,17 @@ _SIGNATURES = {
                                         _vp, _vp]),
     "nuq_moments_accumulate": (_i32, [_vp, _vp, _vp, _u64, _vp]),
     "nuq_normalized_variance": (_i32, [_vp, _vp, _u64, _u64, _vp, _u64, _vp, _vp]),
+    "nuq_gradient_norm": (_i32, [_u32, _vp, _vp, _u32, _f32, _vp, _u64, _vp, _vp]),
+    "nuq_adamw_step": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _f64, _f64, _f64, _f64, _u64, _vp, _vp]),
+    "nuq_state_blocks": (_u64, [_u64]),
+    "nuq_adamw_step_coded": (_i32, [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _f64, _f64, _f64, _f64, _u64, _vp,
+                                    _vp]),
+    "nuq_adamw_state_values": (_i32, [_vp, _vp, _vp, _u64, _vp, _vp, _vp]),
+    "nuq_layer_norm_forward": (_i32, [_vp, _u64, _vp, _u64, _vp, _vp, _u64, _u32, _f32, _u32, _u32, _vp, _u64, _vp, _u64, _vp,
+                                      _vp, _vp]),
+    "nuq_layer_norm_workspace_bytes": (_u64, [_u64, _u32]),
+    "nuq_layer_norm_backward": (_i32, [_vp, _u64, _vp, _u64, _vp, _vp, _vp, _vp, _u64, _u64, _u32, _u32, _u32, _vp, _u64, _vp,
+                                       _vp, _vp, _u64, _vp]),
     "nuq_last_error_flags": (_i32, [_vp, _vp]),
     "nuq_encode_shape": (_i32, [_u32, _u32, _u64, _u32, _u32, _u32, _vp, _u32, _vp]),
     "nuq_decode_tile": (_u32, [_u32, _u64, _u32, _u32, _u32, _i32, _u32]),
@@ -595,6 +607,174 @@ def nuq_normalized_variance(total: torch.Tensor, total_sq: torch.Tensor, M: int,
            _lib.nuq_normalized_variance(_ptr(total, torch.float64), _ptr(total_sq, torch.float64), d, M,
                                         _ptr(workspace), workspace.numel() * workspace.element_size(),
                                         _ptr(out2, torch.float64), _stream()))
+
+
+# ------------------------------------------ AdamW, the gradients' norm, layer norm
+
+GRADIENT_NORM_WORKSPACE_BYTES = 65536
+STATE_BLOCK = 256
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise ValueError("%s: expected float32, bfloat16 or float16, got %s" % (what, t.dtype)) from None
+
+
+def _tensors(ts, what: str, like: list[int] | None = None, dtype: torch.dtype | None = None):
+    """(pointer array, element counts) of device tensors of one type, each as long as `like` says."""
+    ts = list(ts)
+    if like is not None and len(ts) != len(like):
+        raise ValueError("%s: %d tensors, %d are needed" % (what, len(ts), len(like)))
+    counts = [t.numel() for t in ts]
+    dtype = dtype or (ts[0].dtype if ts else None)
+    for i, t in enumerate(ts):
+        if like is not None and counts[i] != like[i]:
+            raise ValueError("%s[%d] holds %d elements, %d are needed" % (what, i, counts[i], like[i]))
+    return (ctypes.c_void_p * len(ts))(*[_ptr(t, dtype, 0, what) for t in ts]), counts
+
+
+def nuq_gradient_norm(grads, max_norm: float, workspace: torch.Tensor, out: torch.Tensor) -> None:
+    """out[0] <- the norm of all `grads` taken as one vector, out[1] <- min(1, max_norm / norm), both on the device."""
+    pointers, counts = _tensors(grads, "grads")
+    _check("nuq_gradient_norm",
+           _lib.nuq_gradient_norm(len(counts), pointers, (_u64 * len(counts))(*counts), _type(grads[0], "grads") if counts else 0,
+                                  float(max_norm), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                  _ptr(out, torch.float32, 2, "out"), _stream()))
+
+
+def _step_arguments(ws, grads, decays, coefficient, copies):
+    w, counts = _tensors(ws, "ws", dtype=torch.float32)
+    g, _ = _tensors(grads, "grads", counts)
+    T = len(counts)
+    if decays is not None and len(decays) != T:
+        raise ValueError("one weight decay per tensor")
+    copy, copy_type = None, 0
+    if copies is not None:
+        copy, _ = _tensors(copies, "copies", counts)
+        copy_type = _type(copies[0], "copies") if T else 1
+    return (w, g, counts, copy, (_u64 * T)(*counts), None if decays is None else (_f32 * T)(*[float(x) for x in decays]),
+            _type(grads[0], "grads") if T else 0, copy_type,
+            None if coefficient is None else _ptr(coefficient, torch.float32, 1, "coefficient"))
+
+
+def nuq_adamw_step(ws, grads, ms, vs, decays, alpha: float, beta1: float, beta2: float, eps: float, t: int,
+                   coefficient: torch.Tensor | None = None, copies=None) -> None:
+    """Step t (1, 2, ...) of AdamW on lists of tensors: weights and both moments fp32, in place; copies: the weights in 16 bits."""
+    w, g, counts, copy, n, decay, g_type, copy_type, c = _step_arguments(ws, grads, decays, coefficient, copies)
+    m, _ = _tensors(ms, "ms", counts, torch.float32)
+    v, _ = _tensors(vs, "vs", counts, torch.float32)
+    _check("nuq_adamw_step",
+           _lib.nuq_adamw_step(len(counts), w, g, m, v, copy, n, decay, g_type, copy_type, float(alpha), float(beta1),
+                               float(beta2), float(eps), t, c, _stream()))
+
+
+def nuq_state_blocks(n: int) -> int:
+    return _lib.nuq_state_blocks(n)
+
+
+def nuq_adamw_step_coded(ws, grads, ms, vs, scales, decays, alpha: float, beta1: float, beta2: float, eps: float, t: int,
+                         coefficient: torch.Tensor | None = None, copies=None) -> None:
+    """nuq_adamw_step with moments in 8 bits: ms float8_e4m3fn, vs uint8, scales fp32, two per block of STATE_BLOCK elements."""
+    w, g, counts, copy, n, decay, g_type, copy_type, c = _step_arguments(ws, grads, decays, coefficient, copies)
+    m, _ = _tensors(ms, "ms", counts, torch.float8_e4m3fn)
+    v, _ = _tensors(vs, "vs", counts, torch.uint8)
+    s, _ = _tensors(scales, "scales", [2 * nuq_state_blocks(x) for x in counts], torch.float32)
+    _check("nuq_adamw_step_coded",
+           _lib.nuq_adamw_step_coded(len(counts), w, g, m, v, s, copy, n, decay, g_type, copy_type, float(alpha), float(beta1),
+                                     float(beta2), float(eps), t, c, _stream()))
+
+
+def nuq_adamw_state_values(m_codes: torch.Tensor, v_codes: torch.Tensor, scales: torch.Tensor, m: torch.Tensor,
+                           v: torch.Tensor) -> None:
+    n = m_codes.numel()
+    if v_codes.numel() != n or m.numel() != n or v.numel() != n:
+        raise ValueError("codes and values of one length are needed")
+    _check("nuq_adamw_state_values",
+           _lib.nuq_adamw_state_values(_ptr(m_codes, torch.float8_e4m3fn), _ptr(v_codes, torch.uint8),
+                                       _ptr(scales, torch.float32, 2 * nuq_state_blocks(n), "scales"), n,
+                                       _ptr(m, torch.float32), _ptr(v, torch.float32), _stream()))
+
+
+def _rows(t: torch.Tensor, dtype: torch.dtype, rows: int, hidden: int, what: str) -> tuple[int, int]:
+    """(address, row stride) of a tensor [..., hidden] as `rows` rows whose elements stand one after the other."""
+    if t.dtype is not dtype:
+        raise ValueError("%s: expected dtype %s, got %s" % (what, dtype, t.dtype))
+    if t.dim() < 1 or t.shape[-1] != hidden or t.numel() != rows * hidden:
+        raise ValueError("%s: expected %d rows of %d, got %s" % (what, rows, hidden, tuple(t.shape)))
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, hidden)
+        except RuntimeError:
+            raise ValueError("%s: its rows do not stand at one stride" % what) from None
+    if not _on_device(t) or (hidden > 1 and t.stride(1) != 1):
+        raise ValueError("%s: expected a device tensor with contiguous rows" % what)
+    return t.data_ptr(), t.stride(0)
+
+
+def _vector(t: torch.Tensor | None, dtype: torch.dtype, hidden: int, what: str) -> int:
+    if t is not None and t.numel() != hidden:
+        raise ValueError("%s holds %d elements, %d are needed" % (what, t.numel(), hidden))
+    return _ptr(t, dtype, 0, what)
+
+
+def _weight_dtype(x: torch.Tensor, *vectors) -> torch.dtype:
+    for t in vectors:
+        if t is not None:
+            if t.dtype not in (torch.float32, x.dtype):
+                raise ValueError("weight and bias: expected float32 or %s, got %s" % (x.dtype, t.dtype))
+            return t.dtype
+    return torch.float32
+
+
+def nuq_layer_norm_forward(x: torch.Tensor, residual: torch.Tensor | None, weight: torch.Tensor | None,
+                           bias: torch.Tensor | None, eps: float, total: torch.Tensor | None, y: torch.Tensor,
+                           mean: torch.Tensor | None, rstd: torch.Tensor | None) -> None:
+    """y <- layer norm of the rows of x [..., hidden], or of total <- x + residual; mean, rstd: a value per row, for backward."""
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x: expected rows of one element or more")
+    hidden, dtype, kind = x.shape[-1], x.dtype, _weight_dtype(x, weight, bias)
+    rows = x.numel() // hidden
+    if (residual is None) != (total is None):
+        raise ValueError("residual and total: both or neither")
+    none = (0, 0)
+    px, ldx = _rows(x, dtype, rows, hidden, "x")
+    pr, ldr = _rows(residual, dtype, rows, hidden, "residual") if residual is not None else none
+    pt, ldt = _rows(total, dtype, rows, hidden, "total") if total is not None else none
+    py, ldy = _rows(y, dtype, rows, hidden, "y")
+    _check("nuq_layer_norm_forward",
+           _lib.nuq_layer_norm_forward(px, ldx, pr, ldr, _vector(weight, kind, hidden, "weight"), _vector(bias, kind, hidden, "bias"),
+                                       rows, hidden, float(eps), _type(x, "x"), _TYPES[kind], pt, ldt, py, ldy,
+                                       _vector(mean, torch.float32, rows, "mean"), _vector(rstd, torch.float32, rows, "rstd"),
+                                       _stream()))
+
+
+def nuq_layer_norm_workspace_bytes(rows: int, hidden: int) -> int:
+    return _lib.nuq_layer_norm_workspace_bytes(rows, hidden)
+
+
+def nuq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor,
+                            rstd: torch.Tensor, add: torch.Tensor | None, dx: torch.Tensor, dweight: torch.Tensor | None,
+                            dbias: torch.Tensor | None, workspace: torch.Tensor | None) -> None:
+    """dx <- the gradient of the rows x (the forward's total where it had one), plus add; dweight, dbias <- theirs."""
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x: expected rows of one element or more")
+    hidden, dtype, kind = x.shape[-1], x.dtype, _weight_dtype(x, weight, dweight, dbias)
+    rows = x.numel() // hidden
+    pg, ldg = _rows(dy, dtype, rows, hidden, "dy")
+    px, ldx = _rows(x, dtype, rows, hidden, "x")
+    pa, lda = _rows(add, dtype, rows, hidden, "add") if add is not None else (0, 0)
+    pd, ldd = _rows(dx, dtype, rows, hidden, "dx")
+    _check("nuq_layer_norm_backward",
+           _lib.nuq_layer_norm_backward(pg, ldg, px, ldx, _vector(weight, kind, hidden, "weight"),
+                                        _vector(mean, torch.float32, rows, "mean"), _vector(rstd, torch.float32, rows, "rstd"),
+                                        pa, lda, rows, hidden, _type(x, "x"), _TYPES[kind], pd, ldd,
+                                        _vector(dweight, kind, hidden, "dweight"), _vector(dbias, kind, hidden, "dbias"),
+                                        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                        _stream()))
 
 
 def nuq_last_error_flags() -> int:

@@ -8,7 +8,7 @@ import subprocess
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "nuq.hip")
+SRCS = [os.path.join(HERE, "csrc", x) for x in ("nuq.hip", "nuq_train.hip")]
 LIB = os.path.join(HERE, "libnuq.so")
 CALLS_SRC = os.path.join(HERE, "csrc", "nuq_calls.cpp")
 CALLS = os.path.join(HERE, "_nuq_calls" + sysconfig.get_config_var("EXT_SUFFIX"))       # it serves one Python only, and one torch
@@ -17,7 +17,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "nuq.h")
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-shared", "-fPIC",
+    "-fPIC",
 ]
 
 
@@ -40,7 +40,9 @@ def _calls_command(out: str) -> list[str]:
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     tmp, calls_tmp = ("%s.tmp.%d" % (x, os.getpid()) for x in (LIB, CALLS))
-    commands = (("hipcc", [hipcc, *HIPCC_FLAGS, _header_key(), "-o", tmp, SRC]), ("g++", _calls_command(calls_tmp)))
+    objects = ["%s.%d.o" % (tmp, i) for i in range(len(SRCS))]
+    commands = [("hipcc", [hipcc, *HIPCC_FLAGS, _header_key(), "-c", "-o", o, src]) for o, src in zip(objects, SRCS)]
+    commands.append(("g++", _calls_command(calls_tmp)))
     for what, cmd in commands:                         # before either runs
         if not shutil.which(cmd[0]):
             raise RuntimeError("no %s: %s does not exist" % (what, cmd[0]))
@@ -57,6 +59,14 @@ def build(verbose: bool = False) -> str:
             failed.append("%s failed:\n%s" % (what, out))
         elif verbose and out:
             print(out)
+    if not failed:
+        p = subprocess.run([hipcc, HIPCC_FLAGS[0], "-shared", "-o", tmp, *objects], stdout=subprocess.PIPE,
+                           stderr=subprocess.STDOUT, text=True)
+        if p.returncode != 0:
+            failed.append("hipcc failed:\n%s" % p.stdout)
+    for o in objects:
+        if os.path.exists(o):
+            os.remove(o)
     if failed:
         raise RuntimeError("\n".join(failed))
     os.replace(tmp, LIB)

@@ -16,6 +16,7 @@
 #include "nuq_device.hpp"
 #include "nuq_encode_kernels.hpp"
 #include "nuq_fixed_kernels.hpp"
+#include "nuq_host.hpp"
 #include "nuq_huffman_kernels.hpp"
 #include "nuq_sgd_kernels.hpp"
 #include "nuq_table_kernels.hpp"
@@ -50,8 +51,10 @@ void *static_workspace_ptr()
 // Sticky error flags, one word per device (each device holds its own copy of the symbol).
 __device__ uint32_t g_flags;
 
+}  // namespace
+
 // Their address on the current device, looked up once per device and kept (a symbol does not move).
-uint32_t *flags_ptr()
+uint32_t *nuq::flags_ptr()
 {
     static std::atomic<void *> ptrs[64];
     int dev = 0;
@@ -66,6 +69,8 @@ uint32_t *flags_ptr()
     }
     return static_cast<uint32_t *>(p);
 }
+
+namespace {
 
 // ---- optional per-launch timing (benchmarks only) ----
 struct Timing {
@@ -357,11 +362,6 @@ template <int TEAM>
 uint32_t team_rows(uint32_t bucket)
 {
     return std::max<uint32_t>(TEAM > kWave ? kNormParts<TEAM> : 1, (bucket + 4 * TEAM - 1) / (4 * TEAM));
-}
-
-int check_launch()
-{
-    return hipGetLastError() == hipSuccess ? NUQ_OK : NUQ_EHIP;
 }
 
 // Grid of a per-bucket kernel: x = workgroups over the buckets of one worker, y = worker.

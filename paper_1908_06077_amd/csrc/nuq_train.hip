@@ -1,0 +1,420 @@
+// C ABI of the optimizer and the layer norm (see include/nuq.h): argument checks, the tables of tensors and the launches.  A
+// source file of its own, so that it is built beside the other.
+#include "../../include/nuq.h"
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "nuq_host.hpp"
+
+#include "nuq_adamw_kernels.hpp"
+#include "nuq_layer_norm_kernels.hpp"
+
+namespace {
+
+using namespace nuq;
+
+template <class T>
+struct Type {
+    using type = T;
+};
+
+// f(Type<element>) for one of the three element types.
+template <class F>
+int with_type(uint32_t type, F &&f)
+{
+    return type == NUQ_F32 ? f(Type<float>{}) : type == NUQ_BF16 ? f(Type<__bf16>{}) : f(Type<_Float16>{});
+}
+
+uint32_t width(uint32_t type) { return type == NUQ_F32 ? 4u : 2u; }
+
+bool off_grid(const void *p, uint32_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) != 0; }
+
+bool valid_array(const void *p, uint64_t n, uint32_t bytes) { return n == 0 || (p && !off_grid(p, bytes)); }
+
+// What a step's launches have in common, and what the step's arguments are checked for.
+struct AdamwCall {
+    uint32_t T, g_type, copy_type;
+    const void *const *g;
+    void *const *copy;
+    const uint64_t *n;
+    const float *decay;
+    double alpha, beta1, beta2, eps;
+    uint64_t t;
+    const float *coefficient;
+
+    bool valid(float *const *w) const
+    {
+        if (g_type > NUQ_F16 || (copy && copy_type != NUQ_BF16 && copy_type != NUQ_F16) || t == 0 || !std::isfinite(alpha) ||
+            !std::isfinite(beta1) || !std::isfinite(beta2) || beta1 < 0.0 || !(beta1 < 1.0) || beta2 < 0.0 || !(beta2 < 1.0) ||
+            !(eps >= 0x1p-126) || !std::isfinite((float)eps) || (coefficient && off_grid(coefficient, 4)) ||
+            (T > 0 && (!w || !g || !n)))
+            return false;
+        for (uint32_t i = 0; i < T; ++i)
+            if (!valid_array(w[i], n[i], 4) || !valid_array(g[i], n[i], width(g_type)) ||
+                (copy && !valid_array(copy[i], n[i], 2)) || n[i] > UINT64_MAX / 16u || (decay && !std::isfinite(decay[i])))
+                return false;
+        return true;
+    }
+    AdamwNumbers numbers() const
+    {
+        const double fade1 = -std::expm1((double)t * std::log(beta1)), fade2 = -std::expm1((double)t * std::log(beta2));
+        return {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(alpha / fade1),
+                (float)(1.0 / std::sqrt(fade2)), (float)eps};
+    }
+    float keep(uint32_t i) const { return decay ? (float)(1.0 - alpha * (double)decay[i]) : 1.0f; }
+    const void *g_at(uint32_t i, uint64_t e) const { return static_cast<const char *>(g[i]) + e * width(g_type); }
+
+    // Whether tensor j's elements follow those of tensor i, whose run is `before` elements long, in the arrays all steps have.
+    bool follows(float *const *w, uint32_t i, uint32_t j, uint64_t before) const
+    {
+        return w[j] == w[i] + before && g[j] == g_at(i, before) && keep(i) == keep(j) &&
+               (!copy || copy[j] == static_cast<char *>(copy[i]) + before * 2u);
+    }
+    // f(gradient type, copy type, whether there is a copy)
+    template <class F>
+    int with_types(F &&f) const
+    {
+        return with_type(g_type, [&](auto gt) {
+            return !copy                     ? f(gt, Type<__bf16>{}, std::false_type{})
+                   : copy_type == NUQ_BF16 ? f(gt, Type<__bf16>{}, std::true_type{})
+                                           : f(gt, Type<_Float16>{}, std::true_type{});
+        });
+    }
+};
+
+// Walks the tensors of a call, joined where one follows another, and fills tables of at most kMost of them: put(slot, tensor,
+// elements) for each, launch(tensors, chunks) for each table.  Runs are cut so that a launch has at most 2^30 chunks.
+template <uint32_t kMost, class Follows, class Put, class Launch>
+int for_tables(uint32_t T, const uint64_t *n, uint64_t chunk, Follows &&follows, Put &&put, Launch &&launch)
+{
+    constexpr uint64_t kChunks = 1ull << 30;
+    uint32_t slots = 0;
+    uint64_t chunks = 0;
+    const auto flush = [&]() -> int {
+        const int rc = slots ? launch(slots, (uint32_t)chunks) : (int)NUQ_OK;
+        slots = 0;
+        chunks = 0;
+        return rc;
+    };
+    for (uint32_t i = 0; i < T;) {
+        uint64_t run = n[i];
+        uint32_t j = i + 1;
+        while (run && j < T && (n[j] == 0 || follows(i, j, run)))
+            run += n[j++];
+        for (uint64_t at = 0; at < run;) {
+            if (slots == kMost || chunks == kChunks)
+                if (const int rc = flush(); rc != NUQ_OK)
+                    return rc;
+            const uint64_t take = std::min(run - at, (kChunks - chunks) * chunk);
+            put(slots++, i, at, take, (uint32_t)chunks);
+            chunks += (take + chunk - 1) / chunk;
+            at += take;
+        }
+        i = j;
+    }
+    return flush();
+}
+
+}  // namespace
+
+extern "C" {
+
+int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint32_t type, float max_norm, void *workspace,
+                      uint64_t workspace_bytes, float *out, nuq_stream_t stream)
+{
+    if (type > NUQ_F16 || !(max_norm > 0.0f) || !workspace || off_grid(workspace, 8) ||
+        workspace_bytes < NUQ_GRADIENT_NORM_WORKSPACE_BYTES || !out || off_grid(out, 4) || (T > 0 && (!g || !n)))
+        return NUQ_EINVAL;
+    for (uint32_t i = 0; i < T; ++i)
+        if (!valid_array(g[i], n[i], width(type)) || n[i] > UINT64_MAX / 16u)
+            return NUQ_EINVAL;
+    uint32_t *const flags = flags_ptr();
+    if (!flags)
+        return NUQ_EHIP;
+    const uint32_t w = width(type);
+    const auto follows = [&](uint32_t i, uint32_t j, uint64_t before) {
+        return g[j] == static_cast<const char *>(g[i]) + before * w;
+    };
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    NormTable P;
+    double *const partial = static_cast<double *>(workspace);
+    // the launches share the partials
+    uint32_t launches = 0;
+    (void)for_tables<kNormTensors>(T, n, kNormChunk, follows, [](auto...) {}, [&](uint32_t, uint32_t) {
+        ++launches;
+        return (int)NUQ_OK;
+    });
+    if (launches > kNormPartials)
+        return NUQ_EINVAL;
+    const uint32_t most = launches ? std::min(2048u, kNormPartials / launches) : 0u;
+    uint32_t used = 0;
+    const int rc = for_tables<kNormTensors>(
+        T, n, kNormChunk, follows,
+        [&](uint32_t slot, uint32_t i, uint64_t at, uint64_t take, uint32_t start) {
+            P.g[slot] = static_cast<const char *>(g[i]) + at * w;
+            P.n[slot] = take;
+            P.start[slot] = start;
+        },
+        [&](uint32_t slots, uint32_t chunks) {
+            P.start[slots] = chunks;
+            P.count = slots;
+            P.partial = partial + used;
+            const uint32_t grid = std::min(chunks, most);
+            used += grid;
+            return with_type(type, [&](auto t) {
+                hipLaunchKernelGGL(k_gradient_norm<typename decltype(t)::type>, dim3(grid), dim3(256), 0, st, P);
+                return check_launch();
+            });
+        });
+    if (rc != NUQ_OK)
+        return rc;
+    hipLaunchKernelGGL(k_gradient_norm_finish, dim3(1), dim3(1024), 0, st, partial, used, max_norm, out, flags);
+    return check_launch();
+}
+
+int nuq_adamw_step(uint32_t T, float *const *w, const void *const *g, float *const *m, float *const *v, void *const *copy,
+                   const uint64_t *n, const float *decay, uint32_t g_type, uint32_t copy_type, double alpha, double beta1,
+                   double beta2, double eps, uint64_t t, const float *coefficient, nuq_stream_t stream)
+{
+    const AdamwCall C{T, g_type, copy_type, g, copy, n, decay, alpha, beta1, beta2, eps, t, coefficient};
+    if (!C.valid(w) || (T > 0 && (!m || !v)))
+        return NUQ_EINVAL;
+    for (uint32_t i = 0; i < T; ++i)
+        if (!valid_array(m[i], n[i], 4) || !valid_array(v[i], n[i], 4))
+            return NUQ_EINVAL;
+    AdamwTable P;
+    P.num = C.numbers();
+    P.coefficient = coefficient;
+    P.flags = flags_ptr();
+    if (!P.flags)
+        return NUQ_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return for_tables<kTableTensors>(
+        T, n, kAdamwChunk,
+        [&](uint32_t i, uint32_t j, uint64_t before) {
+            return C.follows(w, i, j, before) && m[j] == m[i] + before && v[j] == v[i] + before;
+        },
+        [&](uint32_t slot, uint32_t i, uint64_t at, uint64_t take, uint32_t start) {
+            P.w[slot] = w[i] + at;
+            P.m[slot] = m[i] + at;
+            P.v[slot] = v[i] + at;
+            P.g[slot] = C.g_at(i, at);
+            P.copy[slot] = copy ? static_cast<char *>(copy[i]) + at * 2u : nullptr;
+            P.n[slot] = take;
+            P.keep[slot] = C.keep(i);
+            P.start[slot] = start;
+        },
+        [&](uint32_t slots, uint32_t chunks) {
+            P.count = slots;
+            return C.with_types([&](auto gt, auto ct, auto has) {
+                hipLaunchKernelGGL((k_adamw<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value>),
+                                   dim3(chunks), dim3(256), 0, st, P);
+                return check_launch();
+            });
+        });
+}
+
+uint64_t nuq_state_blocks(uint64_t n) { return n / NUQ_STATE_BLOCK + (n % NUQ_STATE_BLOCK != 0); }
+
+int nuq_adamw_step_coded(uint32_t T, float *const *w, const void *const *g, uint8_t *const *m, uint8_t *const *v,
+                         float *const *scales, void *const *copy, const uint64_t *n, const float *decay, uint32_t g_type,
+                         uint32_t copy_type, double alpha, double beta1, double beta2, double eps, uint64_t t,
+                         const float *coefficient, nuq_stream_t stream)
+{
+    const AdamwCall C{T, g_type, copy_type, g, copy, n, decay, alpha, beta1, beta2, eps, t, coefficient};
+    if (!C.valid(w) || (T > 0 && (!m || !v || !scales)))
+        return NUQ_EINVAL;
+    for (uint32_t i = 0; i < T; ++i)
+        if (!valid_array(m[i], n[i], 1) || !valid_array(v[i], n[i], 1) || !valid_array(scales[i], n[i], 4))
+            return NUQ_EINVAL;
+    AdamwCodedTable P;
+    P.num = C.numbers();
+    P.coefficient = coefficient;
+    P.flags = flags_ptr();
+    if (!P.flags)
+        return NUQ_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return for_tables<kCodedTensors>(
+        T, n, kCodedChunk,
+        [&](uint32_t i, uint32_t j, uint64_t before) {
+            return before % NUQ_STATE_BLOCK == 0 && C.follows(w, i, j, before) && m[j] == m[i] + before &&
+                   v[j] == v[i] + before && scales[j] == scales[i] + 2u * (before / NUQ_STATE_BLOCK);
+        },
+        [&](uint32_t slot, uint32_t i, uint64_t at, uint64_t take, uint32_t start) {     // (`at`: whole chunks)
+            P.w[slot] = w[i] + at;
+            P.m[slot] = m[i] + at;
+            P.v[slot] = v[i] + at;
+            P.scales[slot] = scales[i] + 2u * (at / NUQ_STATE_BLOCK);
+            P.g[slot] = C.g_at(i, at);
+            P.copy[slot] = copy ? static_cast<char *>(copy[i]) + at * 2u : nullptr;
+            P.n[slot] = take;
+            P.keep[slot] = C.keep(i);
+            P.start[slot] = start;
+        },
+        [&](uint32_t slots, uint32_t chunks) {
+            P.count = slots;
+            return C.with_types([&](auto gt, auto ct, auto has) {
+                hipLaunchKernelGGL((k_adamw_coded<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value>),
+                                   dim3(chunks), dim3(256), 0, st, P);
+                return check_launch();
+            });
+        });
+}
+
+int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const float *scales, uint64_t n, float *m, float *v,
+                           nuq_stream_t stream)
+{
+    if (n == 0)
+        return NUQ_OK;
+    const uint64_t groups = (n + 1023u) / 1024u;
+    if (!m_codes || !v_codes || !valid_array(scales, n, 4) || !valid_array(m, n, 4) || !valid_array(v, n, 4) ||
+        groups > 0x7fffffffull)
+        return NUQ_EINVAL;
+    hipLaunchKernelGGL(k_adamw_values, dim3((uint32_t)groups), dim3(256), 0, static_cast<hipStream_t>(stream), m_codes, v_codes,
+                       scales, m, v, n);
+    return check_launch();
+}
+
+}  // extern "C"
+
+namespace {
+
+// The team of threads and the 16-byte vectors per thread that hold a row of `vecs` such vectors: f(team, vectors), or f(0, 0)
+// where nothing does.
+template <class F>
+int with_row_shape(uint32_t vecs, F &&f)
+{
+    using std::integral_constant;
+#define NUQ_SHAPE(team, count)                                                                                        \
+    if (vecs <= team * count)                                                                                         \
+        return f(integral_constant<int, team>{}, integral_constant<int, count>{});
+    NUQ_SHAPE(4, 1)
+    NUQ_SHAPE(16, 1)
+    NUQ_SHAPE(16, 2)
+    NUQ_SHAPE(64, 1)
+    NUQ_SHAPE(64, 2)
+    NUQ_SHAPE(256, 1)
+    NUQ_SHAPE(256, 2)
+    NUQ_SHAPE(256, 4)
+    NUQ_SHAPE(512, 4)
+    NUQ_SHAPE(1024, 4)
+#undef NUQ_SHAPE
+    return f(integral_constant<int, 0>{}, integral_constant<int, 0>{});
+}
+
+// f(Type<element>, Type<weight>)
+template <class F>
+int with_types(uint32_t type, uint32_t weight_type, F &&f)
+{
+    return with_type(type, [&](auto t) { return weight_type == type ? f(t, t) : f(t, Type<float>{}); });
+}
+
+bool valid_rows(uint64_t rows, uint32_t hidden, uint32_t type, uint32_t weight_type, const void *weight)
+{
+    return hidden >= 1 && hidden <= 1u << 30 && rows <= 1ull << 31 && type <= NUQ_F16 &&
+           (weight_type == type || weight_type == NUQ_F32) && (!weight || !off_grid(weight, width(weight_type)));
+}
+
+// Partial sums of the weights' gradients: rows of workgroups.
+constexpr uint32_t kParts = 512, kLongParts = 64;
+static_assert(kParts <= 1024, "nuq_layer_norm_workspace_bytes");
+
+}  // namespace
+
+extern "C" {
+
+int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, const void *weight,
+                           const void *bias, uint64_t rows, uint32_t hidden, float eps, uint32_t type, uint32_t weight_type,
+                           void *total, uint64_t ldt, void *y, uint64_t ldy, float *mean, float *rstd, nuq_stream_t stream)
+{
+    if (!valid_rows(rows, hidden, type, weight_type, weight) || (bias && off_grid(bias, width(weight_type))) ||
+        !std::isfinite(eps) || eps < 0.0f || !residual != !total || (mean && off_grid(mean, 4)) || (rstd && off_grid(rstd, 4)))
+        return NUQ_EINVAL;
+    if (rows == 0)
+        return NUQ_OK;
+    const uint32_t w = width(type);
+    if (!valid_array(x, 1, w) || !valid_array(y, 1, w) || (residual && (off_grid(residual, w) || off_grid(total, w))) ||
+        (rows > 1 && (ldy < hidden || (total && ldt < hidden))))
+        return NUQ_EINVAL;
+    const LayerNormForward P{x, residual, weight, bias, total, y, mean, rstd, rows, ldx, ldr, ldt, ldy, hidden, eps};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return with_types(type, weight_type, [&](auto tt, auto wt) {
+        using T = typename decltype(tt)::type;
+        using W = typename decltype(wt)::type;
+        return with_row_shape((hidden + kVecOf<T> - 1) / kVecOf<T>, [&](auto team, auto count) {
+            constexpr int TEAM = decltype(team)::value, NV = decltype(count)::value;
+            if constexpr (TEAM == 0) {
+                if (residual)
+                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, true>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+                else
+                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, false>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+            } else {
+                constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
+                const dim3 grid((uint32_t)((rows + TEAMS - 1) / TEAMS));
+                if (residual)
+                    hipLaunchKernelGGL((k_layer_norm_forward<T, W, TEAM, NV, true>), grid, dim3(WG), 0, st, P);
+                else
+                    hipLaunchKernelGGL((k_layer_norm_forward<T, W, TEAM, NV, false>), grid, dim3(WG), 0, st, P);
+            }
+            return check_launch();
+        });
+    });
+}
+
+uint64_t nuq_layer_norm_workspace_bytes(uint64_t rows, uint32_t hidden)
+{
+    return 8ull * hidden * std::min<uint64_t>(rows, 1024u);
+}
+
+int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_t ldx, const void *weight, const float *mean,
+                            const float *rstd, const void *add, uint64_t lda, uint64_t rows, uint32_t hidden, uint32_t type,
+                            uint32_t weight_type, void *dx, uint64_t ldd, void *dweight, void *dbias, void *workspace,
+                            uint64_t workspace_bytes, nuq_stream_t stream)
+{
+    const bool sums = dweight || dbias;
+    if (!valid_rows(rows, hidden, type, weight_type, weight) || (dweight && off_grid(dweight, width(weight_type))) ||
+        (dbias && off_grid(dbias, width(weight_type))))
+        return NUQ_EINVAL;
+    const uint32_t w = width(type);
+    if (rows > 0 && (!valid_array(dy, 1, w) || !valid_array(x, 1, w) || !valid_array(dx, 1, w) || !valid_array(mean, 1, 4) ||
+                     !valid_array(rstd, 1, 4) || (add && off_grid(add, w)) || (rows > 1 && ldd < hidden) ||
+                     (sums && (!workspace || off_grid(workspace, 16)))))
+        return NUQ_EINVAL;
+    if (rows > 0 && sums && workspace_bytes < nuq_layer_norm_workspace_bytes(rows, hidden))
+        return NUQ_ECAPACITY;
+    const LayerNormBackward P{dy, x, weight, add, mean, rstd, dx, static_cast<float *>(workspace), rows, ldg, ldx, lda, ldd, hidden};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return with_types(type, weight_type, [&](auto tt, auto wt) {
+        using T = typename decltype(tt)::type;
+        using W = typename decltype(wt)::type;
+        uint32_t parts = 0;
+        const int rc = rows == 0 ? (int)NUQ_OK : with_row_shape((hidden + kVecOf<T> - 1) / kVecOf<T>, [&](auto team, auto count) {
+            constexpr int TEAM = decltype(team)::value, NV = decltype(count)::value;
+            if constexpr (TEAM == 0) {
+                parts = (uint32_t)std::min<uint64_t>(rows, kLongParts);
+                if (sums)
+                    hipLaunchKernelGGL((k_layer_norm_columns<T>), dim3((hidden + 255u) / 256u, parts), dim3(256), 0, st, P);
+                hipLaunchKernelGGL((k_layer_norm_backward_long<T, W>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+            } else {
+                constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
+                const uint64_t groups = (rows + TEAMS - 1) / TEAMS;
+                parts = (uint32_t)std::min<uint64_t>(groups, kParts);
+                if (sums)
+                    hipLaunchKernelGGL((k_layer_norm_backward<T, W, TEAM, NV, true>), dim3(parts), dim3(WG), 0, st, P);
+                else
+                    hipLaunchKernelGGL((k_layer_norm_backward<T, W, TEAM, NV, false>), dim3((uint32_t)std::min<uint64_t>(groups, 8192u)),
+                                       dim3(WG), 0, st, P);
+            }
+            return check_launch();
+        });
+        if (rc != NUQ_OK || !sums)
+            return rc;
+        hipLaunchKernelGGL((k_layer_norm_finish<W>), dim3((hidden + 63u) / 64u, 2), dim3(1024), 0, st, P.partial, parts, hidden,
+                           static_cast<W *>(dweight), static_cast<W *>(dbias));
+        return check_launch();
+    });
+}
+
+}  // extern "C"

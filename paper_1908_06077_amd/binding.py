@@ -639,6 +639,9 @@ def _tensors(ts, what: str, like: list[int] | None = None, dtype: torch.dtype | 
 
 def nuq_gradient_norm(grads, max_norm: float, workspace: torch.Tensor, out: torch.Tensor) -> None:
     """out[0] <- the norm of all `grads` taken as one vector, out[1] <- min(1, max_norm / norm), both on the device."""
+    code = _calls.gradient_norm(grads, max_norm, workspace, out)
+    if code is not None:
+        return _check("nuq_gradient_norm", code)
     pointers, counts = _tensors(grads, "grads")
     _check("nuq_gradient_norm",
            _lib.nuq_gradient_norm(len(counts), pointers, (_u64 * len(counts))(*counts), _type(grads[0], "grads") if counts else 0,
@@ -664,6 +667,9 @@ def _step_arguments(ws, grads, decays, coefficient, copies):
 def nuq_adamw_step(ws, grads, ms, vs, decays, alpha: float, beta1: float, beta2: float, eps: float, t: int,
                    coefficient: torch.Tensor | None = None, copies=None) -> None:
     """Step t (1, 2, ...) of AdamW on lists of tensors: weights and both moments fp32, in place; copies: the weights in 16 bits."""
+    code = _calls.adamw_step(ws, grads, ms, vs, decays, alpha, beta1, beta2, eps, t, coefficient, copies)
+    if code is not None:
+        return _check("nuq_adamw_step", code)
     w, g, counts, copy, n, decay, g_type, copy_type, c = _step_arguments(ws, grads, decays, coefficient, copies)
     m, _ = _tensors(ms, "ms", counts, torch.float32)
     v, _ = _tensors(vs, "vs", counts, torch.float32)
@@ -679,6 +685,9 @@ def nuq_state_blocks(n: int) -> int:
 def nuq_adamw_step_coded(ws, grads, ms, vs, scales, decays, alpha: float, beta1: float, beta2: float, eps: float, t: int,
                          coefficient: torch.Tensor | None = None, copies=None) -> None:
     """nuq_adamw_step with moments in 8 bits: ms float8_e4m3fn, vs uint8, scales fp32, two per block of STATE_BLOCK elements."""
+    code = _calls.adamw_step_coded(ws, grads, ms, vs, scales, decays, alpha, beta1, beta2, eps, t, coefficient, copies)
+    if code is not None:
+        return _check("nuq_adamw_step_coded", code)
     w, g, counts, copy, n, decay, g_type, copy_type, c = _step_arguments(ws, grads, decays, coefficient, copies)
     m, _ = _tensors(ms, "ms", counts, torch.float8_e4m3fn)
     v, _ = _tensors(vs, "vs", counts, torch.uint8)
@@ -734,6 +743,9 @@ def nuq_layer_norm_forward(x: torch.Tensor, residual: torch.Tensor | None, weigh
                            bias: torch.Tensor | None, eps: float, total: torch.Tensor | None, y: torch.Tensor,
                            mean: torch.Tensor | None, rstd: torch.Tensor | None) -> None:
     """y <- layer norm of the rows of x [..., hidden], or of total <- x + residual; mean, rstd: a value per row, for backward."""
+    code = _calls.layer_norm_forward(x, residual, weight, bias, eps, total, y, mean, rstd)
+    if code is not None:
+        return _check("nuq_layer_norm_forward", code)
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x: expected rows of one element or more")
     hidden, dtype, kind = x.shape[-1], x.dtype, _weight_dtype(x, weight, bias)
@@ -760,6 +772,9 @@ def nuq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Ten
                             rstd: torch.Tensor, add: torch.Tensor | None, dx: torch.Tensor, dweight: torch.Tensor | None,
                             dbias: torch.Tensor | None, workspace: torch.Tensor | None) -> None:
     """dx <- the gradient of the rows x (the forward's total where it had one), plus add; dweight, dbias <- theirs."""
+    code = _calls.layer_norm_backward(dy, x, weight, mean, rstd, add, dx, dweight, dbias, workspace)
+    if code is not None:
+        return _check("nuq_layer_norm_backward", code)
     if x.dim() < 1 or x.shape[-1] < 1:
         raise ValueError("x: expected rows of one element or more")
     hidden, dtype, kind = x.shape[-1], x.dtype, _weight_dtype(x, weight, dweight, dbias)

@@ -14,6 +14,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
+#include <vector>
 
 #include "../../include/nuq.h"
 
@@ -30,7 +31,9 @@ PyObject *g_norms, *g_bit_off, *g_words, *g_sync;                   // attribute
     X(nuq_decode_accumulate) X(nuq_decode_momentum_step) X(nuq_quantize_encode_table_batch)                          \
     X(nuq_decode_accumulate_table) X(nuq_quantize_pack_fixed_batch) X(nuq_unpack_accumulate_fixed)                   \
     X(nuq_quantize_pack_fixed_table_batch) X(nuq_unpack_accumulate_fixed_table)                                      \
-    X(nuq_quantize_encode_huffman_batch) X(nuq_decode_accumulate_huffman) X(nuq_moments_accumulate)
+    X(nuq_quantize_encode_huffman_batch) X(nuq_decode_accumulate_huffman) X(nuq_moments_accumulate)                  \
+    X(nuq_gradient_norm) X(nuq_adamw_step) X(nuq_adamw_step_coded) X(nuq_state_blocks) X(nuq_layer_norm_forward)     \
+    X(nuq_layer_norm_backward)
 #define NUQ_POINTER(name) decltype(&::name) p_##name = nullptr;
 NUQ_CALLS(NUQ_POINTER)
 
@@ -393,6 +396,198 @@ PyObject *moments_accumulate(PyObject *const *a)         // g, total, total_sq
     return launch(p_nuq_moments_accumulate, g, total, total_sq, d);
 }
 
+// ---- the optimizer and the layer norm ----
+
+uint32_t type_of(at::ScalarType t)
+{
+    need(t == at::kFloat || t == at::kBFloat16 || t == at::kHalf);
+    return t == at::kFloat ? NUQ_F32 : t == at::kBFloat16 ? NUQ_BF16 : NUQ_F16;
+}
+
+// Device tensors of one type, each as long as `like` says (where it says anything).
+struct Many {
+    std::vector<void *> p;
+    std::vector<uint64_t> n;
+    at::ScalarType type = at::kFloat;
+    explicit Many(PyObject *o, const std::vector<uint64_t> *like = nullptr)
+    {
+        const Items items(o, like ? like->size() : 0, like ? like->size() : UINT32_MAX);
+        p.resize(items.n);
+        n.resize(items.n);
+        for (uint64_t i = 0; i < items.n; ++i) {
+            const at::Tensor &t = device_tensor(items[i]);
+            p[i] = t.data_ptr();
+            n[i] = (uint64_t)t.numel();
+            need(i == 0 || t.scalar_type() == type);
+            type = t.scalar_type();
+            need(!like || n[i] == (*like)[i]);
+        }
+    }
+    Many(PyObject *o, const std::vector<uint64_t> *like, at::ScalarType wanted) : Many(o, like) { need(n.empty() || type == wanted); }
+    template <class T>
+    T *const *as() const
+    {
+        return reinterpret_cast<T *const *>(p.data());
+    }
+};
+
+PyObject *gradient_norm(PyObject *const *a)              // grads, max_norm, workspace, out
+{
+    const Many g(a[0]);
+    const Bytes ws(a[2]);
+    return launch(p_nuq_gradient_norm, (uint32_t)g.n.size(), g.as<const void>(), g.n.data(), type_of(g.type), (float)real(a[1]), ws.p,
+                  ws.n, address<float>(a[3], at::kFloat, 2));
+}
+
+// The arguments that both steps share: ws, grads; decays, alpha, beta1, beta2, eps, t, coefficient, copies from `at` on.
+struct StepArguments {
+    Many w, g;
+    std::vector<float> decay;
+    std::vector<void *> copy;
+    uint32_t g_type, copy_type = NUQ_BF16;
+    double alpha, beta1, beta2, eps;
+    uint64_t t;
+    const float *c = nullptr;
+    StepArguments(PyObject *const *a, int at) : w(a[0], nullptr, at::kFloat), g(a[1], &w.n), g_type(type_of(g.type))
+    {
+        if (a[at] != Py_None) {
+            const Items items(a[at], w.n.size(), w.n.size());
+            decay.resize(items.n);
+            for (uint64_t i = 0; i < items.n; ++i)
+                decay[i] = (float)real(items[i]);
+        }
+        alpha = real(a[at + 1]);
+        beta1 = real(a[at + 2]);
+        beta2 = real(a[at + 3]);
+        eps = real(a[at + 4]);
+        t = whole(a[at + 5], UINT64_MAX);
+        if (a[at + 6] != Py_None)
+            c = address<const float>(a[at + 6], at::kFloat, 1);
+        if (a[at + 7] != Py_None && !w.n.empty()) {
+            Many m(a[at + 7], &w.n);
+            copy_type = type_of(m.type);
+            copy.swap(m.p);
+        }
+    }
+    const float *decays() const { return decay.empty() ? nullptr : decay.data(); }
+    void *const *copies() const { return copy.empty() ? nullptr : copy.data(); }
+};
+
+PyObject *adamw_step(PyObject *const *a)                 // ws, grads, ms, vs, decays, alpha, beta1, beta2, eps, t, coefficient, copies
+{
+    const StepArguments S(a, 4);
+    const Many m(a[2], &S.w.n, at::kFloat), v(a[3], &S.w.n, at::kFloat);
+    return launch(p_nuq_adamw_step, (uint32_t)S.w.n.size(), S.w.as<float>(), S.g.as<const void>(), m.as<float>(), v.as<float>(),
+                  S.copies(), S.w.n.data(), S.decays(), S.g_type, S.copy_type, S.alpha, S.beta1, S.beta2, S.eps, S.t, S.c);
+}
+
+PyObject *adamw_step_coded(PyObject *const *a)           // ws, grads, ms, vs, scales, decays, ... as above
+{
+    const StepArguments S(a, 5);
+    const Many m(a[2], &S.w.n, at::kFloat8_e4m3fn), v(a[3], &S.w.n, at::kByte);
+    std::vector<uint64_t> two(S.w.n.size());
+    for (size_t i = 0; i < two.size(); ++i)
+        two[i] = 2u * p_nuq_state_blocks(S.w.n[i]);
+    const Many scales(a[4], &two, at::kFloat);
+    return launch(p_nuq_adamw_step_coded, (uint32_t)S.w.n.size(), S.w.as<float>(), S.g.as<const void>(), m.as<uint8_t>(),
+                  v.as<uint8_t>(), scales.as<float>(), S.copies(), S.w.n.data(), S.decays(), S.g_type, S.copy_type, S.alpha, S.beta1,
+                  S.beta2, S.eps, S.t, S.c);
+}
+
+// `rows` rows of `hidden` elements of one type, or none (0 rows asked: as many as there are).
+struct Rows {
+    void *p = nullptr;
+    uint64_t ld = 0, rows = 0;
+    uint32_t hidden = 0;
+    at::ScalarType type = at::kFloat;
+    Rows(PyObject *o, const Rows *like)
+    {
+        if (o == Py_None)
+            return;
+        need(THPVariable_CheckExact(o));
+        const at::Tensor &t = THPVariable_Unpack(o);
+        need(t.is_cuda() && t.layout() == at::kStrided && t.has_storage() && !at::isTensorSubclassLike(t) && t.dim() >= 1);
+        const int64_t last = t.size(-1);
+        need(last >= 1 && last <= INT32_MAX);
+        hidden = (uint32_t)last;
+        rows = (uint64_t)t.numel() / hidden;
+        type = t.scalar_type();
+        if (t.dim() == 2) {
+            need(hidden == 1 || t.stride(1) == 1);
+            ld = (uint64_t)t.stride(0);
+        } else {
+            need(t.is_contiguous());
+            ld = hidden;
+        }
+        p = t.data_ptr();
+        need(!like || (like->rows == rows && like->hidden == hidden && like->type == type));
+    }
+};
+
+// A contiguous vector of n elements, or none.
+struct Vector {
+    void *p = nullptr;
+    at::ScalarType type = at::kFloat;
+    bool there = false;
+    Vector(PyObject *o, uint64_t n)
+    {
+        if (o == Py_None)
+            return;
+        const at::Tensor &t = device_tensor(o);
+        need((uint64_t)t.numel() == n);
+        p = t.data_ptr();
+        type = t.scalar_type();
+        there = true;
+    }
+    float *floats() const
+    {
+        need(type == at::kFloat);
+        return static_cast<float *>(p);
+    }
+};
+
+uint32_t weight_type(at::ScalarType rows, std::initializer_list<const Vector *> vectors)
+{
+    at::ScalarType type = at::kFloat;
+    bool any = false;
+    for (const Vector *v : vectors)
+        if (v->there) {
+            need(!any || v->type == type);
+            type = v->type;
+            any = true;
+        }
+    need(type == at::kFloat || type == rows);
+    return type_of(type);
+}
+
+PyObject *layer_norm_forward(PyObject *const *a)         // x, residual, weight, bias, eps, total, y, mean, rstd
+{
+    const Rows x(a[0], nullptr), residual(a[1], &x), total(a[5], &x), y(a[6], &x);
+    need(x.hidden > 0 && y.hidden > 0 && (residual.hidden > 0) == (total.hidden > 0));
+    const Vector weight(a[2], x.hidden), bias(a[3], x.hidden), mean(a[7], x.rows), rstd(a[8], x.rows);
+    return launch(p_nuq_layer_norm_forward, x.p, x.ld, residual.p, residual.ld, weight.p, bias.p, x.rows, x.hidden,
+                  (float)real(a[4]), type_of(x.type), weight_type(x.type, {&weight, &bias}), total.p, total.ld, y.p, y.ld,
+                  mean.floats(), rstd.floats());
+}
+
+PyObject *layer_norm_backward(PyObject *const *a)        // dy, x, weight, mean, rstd, add, dx, dweight, dbias, workspace
+{
+    const Rows x(a[1], nullptr), dy(a[0], &x), add(a[5], &x), dx(a[6], &x);
+    need(x.hidden > 0 && dy.hidden > 0 && dx.hidden > 0);
+    const Vector weight(a[2], x.hidden), mean(a[3], x.rows), rstd(a[4], x.rows), dweight(a[7], x.hidden), dbias(a[8], x.hidden);
+    need(mean.there && rstd.there);
+    void *ws = nullptr;
+    uint64_t bytes = 0;
+    if (a[9] != Py_None) {
+        const Bytes b(a[9]);
+        ws = b.p;
+        bytes = b.n;
+    }
+    return launch(p_nuq_layer_norm_backward, dy.p, dy.ld, x.p, x.ld, weight.p, mean.floats(), rstd.floats(), add.p, add.ld, x.rows,
+                  x.hidden, type_of(x.type), weight_type(x.type, {&weight, &dweight, &dbias}), dx.p, dx.ld, dweight.p, dbias.p, ws,
+                  bytes);
+}
+
 // bind(addresses of the entry points in NUQ_CALLS' order, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -441,6 +636,11 @@ PyMethodDef g_methods[] = {
     NUQ_METHOD(quantize_encode_huffman_batch, 8),
     NUQ_METHOD(decode_accumulate_huffman, 9),
     NUQ_METHOD(moments_accumulate, 3),
+    NUQ_METHOD(gradient_norm, 4),
+    NUQ_METHOD(adamw_step, 12),
+    NUQ_METHOD(adamw_step_coded, 13),
+    NUQ_METHOD(layer_norm_forward, 9),
+    NUQ_METHOD(layer_norm_backward, 10),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nuq_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -32,8 +32,7 @@ __device__ __forceinline__ float adamw_weight(float w, float m, float v, float k
     return __builtin_fmaf(-N.step, u, w * keep);
 }
 
-constexpr uint32_t kAdamwRows = 2;                              // vectors of four that a thread takes
-constexpr uint32_t kAdamwChunk = 256u * 4u * kAdamwRows;        // elements per workgroup
+constexpr uint32_t kAdamwChunk = 256u * 4u;     // elements per workgroup: four per thread
 
 struct AdamwTable {
     float *w[kTableTensors], *m[kTableTensors], *v[kTableTensors];
@@ -50,47 +49,61 @@ struct AdamwTable {
 static_assert(sizeof(AdamwTable) <= 4096, "a launch's arguments");
 
 // One pass: 28 bytes per element with 32-bit gradients.  An element whose new moments are not finite is left as it is.
-template <class G, class C, bool kCopy>
-__global__ __launch_bounds__(256) void k_adamw(const AdamwTable P)
+// kOnce: the call's arrays are larger than the last-level cache.  kWhole: the workgroup's elements are all there.
+template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
+__device__ __forceinline__ void adamw_chunk(const AdamwTable &P, uint32_t t, uint64_t base)
 {
-    const uint32_t t = (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start, P.count, blockIdx.x));
-    const uint64_t base = (uint64_t)(blockIdx.x - P.start[t]) * kAdamwChunk, n = P.n[t];
+    const uint64_t i = base + threadIdx.x * 4u;
+    const int64_t have = (int64_t)P.n[t] - (int64_t)i;
+    float w[4], m[4], v[4], g[4];
+    load_some<4, kWhole, kOnce>(g, static_cast<const G *>(P.g[t]) + i, have);
+    load_some<4, kWhole, kOnce>(m, P.m[t] + i, have);
+    load_some<4, kWhole, kOnce>(v, P.v[t] + i, have);
+    load_some<4, kWhole, kOnce>(w, P.w[t] + i, have);
     const float keep = P.keep[t], c = P.coefficient ? *P.coefficient : 1.0f;
-    float *const pw = P.w[t], *const pm = P.m[t], *const pv = P.v[t];
-    const G *const pg = static_cast<const G *>(P.g[t]);
-    float w[kAdamwRows][4], m[kAdamwRows][4], v[kAdamwRows][4], g[kAdamwRows][4];
+    float m1[4], v1[4];
+    uint32_t top = 0;
 #pragma unroll
-    for (uint32_t r = 0; r < kAdamwRows; ++r) {
-        const uint64_t i = base + (r * 256u + threadIdx.x) * 4u;
-        const int64_t have = (int64_t)n - (int64_t)i;
-        load_some<4>(g[r], pg + i, have);
-        load_some<4>(m[r], pm + i, have);
-        load_some<4>(v[r], pv + i, have);
-        load_some<4>(w[r], pw + i, have);
+    for (int e = 0; e < 4; ++e) {
+        m1[e] = m[e];
+        v1[e] = v[e];
+        adamw_moments(m1[e], v1[e], g[e] * c, P.num);
+        top = max(top, max(__builtin_bit_cast(uint32_t, m1[e]) & 0x7FFFFFFFu, __builtin_bit_cast(uint32_t, v1[e])));
     }
-    bool lost = false;
+    if (__any(top >= 0x7F800000u)) {                         // (infinities and NaN; what has no element here is zeros)
 #pragma unroll
-    for (uint32_t r = 0; r < kAdamwRows; ++r) {
-        const uint64_t i = base + (r * 256u + threadIdx.x) * 4u;
-        const int64_t have = (int64_t)n - (int64_t)i;
+        for (int e = 0; e < 4; ++e)
+            if (max(__builtin_bit_cast(uint32_t, m1[e]) & 0x7FFFFFFFu, __builtin_bit_cast(uint32_t, v1[e])) < 0x7F800000u) {
+                m[e] = m1[e];
+                v[e] = v1[e];
+                w[e] = adamw_weight(w[e], m1[e], v1[e], keep, P.num);
+            }
+        if (threadIdx.x % 64u == 0)
+            atomicOr(P.flags, NUQ_FLAG_NONFINITE);
+    } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float m1 = m[r][e], v1 = v[r][e];
-            adamw_moments(m1, v1, g[r][e] * c, P.num);
-            const bool fine = __builtin_fabsf(m1) < __builtin_inff() && v1 < __builtin_inff();
-            lost |= !fine;
-            m[r][e] = fine ? m1 : m[r][e];
-            v[r][e] = fine ? v1 : v[r][e];
-            w[r][e] = fine ? adamw_weight(w[r][e], m1, v1, keep, P.num) : w[r][e];
+            m[e] = m1[e];
+            v[e] = v1[e];
+            w[e] = adamw_weight(w[e], m1[e], v1[e], keep, P.num);
         }
-        store_some<4>(pm + i, m[r], have);
-        store_some<4>(pv + i, v[r], have);
-        store_some<4>(pw + i, w[r], have);
-        if constexpr (kCopy)
-            store_some<4>(static_cast<C *>(P.copy[t]) + i, w[r], have);
     }
-    if (__any(lost) && threadIdx.x % 64u == 0)
-        atomicOr(P.flags, NUQ_FLAG_NONFINITE);
+    store_some<4, kWhole, kOnce>(P.m[t] + i, m, have);
+    store_some<4, kWhole, kOnce>(P.v[t] + i, v, have);
+    store_some<4, kWhole, kOnce>(P.w[t] + i, w, have);
+    if constexpr (kCopy)
+        store_some<4, kWhole, kOnce>(static_cast<C *>(P.copy[t]) + i, w, have);
+}
+
+template <class G, class C, bool kCopy, bool kOnce>
+__global__ __launch_bounds__(256) void k_adamw(const AdamwTable P)
+{
+    const uint32_t t = P.count == 1u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start, P.count, blockIdx.x));
+    const uint64_t base = (uint64_t)(blockIdx.x - P.start[t]) * kAdamwChunk;
+    if (base + kAdamwChunk <= P.n[t])
+        adamw_chunk<G, C, kCopy, kOnce, true>(P, t, base);
+    else
+        adamw_chunk<G, C, kCopy, kOnce, false>(P, t, base);
 }
 
 // ---- states in 8 bits ----
@@ -103,8 +116,7 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamwTable P)
 
 constexpr uint32_t kStateBlock = NUQ_STATE_BLOCK;
 static_assert(kStateBlock == 256, "a wave holds four elements of a block per lane");
-constexpr uint32_t kCodedRows = 4;                              // blocks that a wave takes
-constexpr uint32_t kCodedChunk = 4u * kCodedRows * kStateBlock; // elements per workgroup
+constexpr uint32_t kCodedChunk = 4u * kStateBlock;              // elements per workgroup: a block per wave
 constexpr uint32_t kCodedTensors = 60;
 
 struct AdamwCodedTable {
@@ -124,20 +136,29 @@ static_assert(sizeof(AdamwCodedTable) <= 4096, "a launch's arguments");
 
 typedef uint32_t CodeWord __attribute__((aligned(1), may_alias));
 
+template <bool kWhole, bool kOnce>
 __device__ __forceinline__ uint32_t load_codes(const uint8_t *from, int64_t have)
 {
-    if (have >= 4)
-        return *reinterpret_cast<const CodeWord *>(from);
+    if (kWhole || have >= 4) {
+        if constexpr (kOnce)
+            return __builtin_nontemporal_load(reinterpret_cast<const CodeWord *>(from));
+        else
+            return *reinterpret_cast<const CodeWord *>(from);
+    }
     uint32_t x = 0;
 #pragma unroll
     for (int e = 0; e < 3; ++e)
         x |= e < have ? (uint32_t)from[e] << (8 * e) : 0u;
     return x;
 }
+template <bool kWhole, bool kOnce>
 __device__ __forceinline__ void store_codes(uint8_t *to, uint32_t x, int64_t have)
 {
-    if (have >= 4) {
-        *reinterpret_cast<CodeWord *>(to) = x;
+    if (kWhole || have >= 4) {
+        if constexpr (kOnce)
+            __builtin_nontemporal_store(x, reinterpret_cast<CodeWord *>(to));
+        else
+            *reinterpret_cast<CodeWord *>(to) = x;
     } else {
 #pragma unroll
         for (int e = 0; e < 3; ++e)
@@ -181,74 +202,66 @@ __device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv)
 }
 
 // One pass: 16 bytes per element with 32-bit gradients.  A block whose new moments are not all finite is left as it is.
-template <class G, class C, bool kCopy>
-__global__ __launch_bounds__(256) void k_adamw_coded(const AdamwCodedTable P)
+// kOnce as above; kWhole: the wave's block is all there.
+template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
+__device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, uint32_t t, uint64_t block)
 {
-    const uint32_t t = (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start, P.count, blockIdx.x));
-    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-    const uint64_t n = P.n[t], block0 = (uint64_t)(blockIdx.x - P.start[t]) * (4u * kCodedRows) + wave * kCodedRows;
+    const uint32_t lane = threadIdx.x % 64u;
+    const uint64_t i = block * kStateBlock + lane * 4u;
+    const int64_t have = (int64_t)P.n[t] - (int64_t)i;
+    float *const scales = P.scales[t] + 2u * block;
+    float w[4], g[4], m[4], v[4];
+    const uint32_t codes_m = load_codes<kWhole, kOnce>(P.m[t] + i, have), codes_v = load_codes<kWhole, kOnce>(P.v[t] + i, have);
+    const float old_a = scales[0], old_b = scales[1];
+    load_some<4, kWhole, kOnce>(g, static_cast<const G *>(P.g[t]) + i, have);
+    load_some<4, kWhole, kOnce>(w, P.w[t] + i, have);
     const float keep = P.keep[t], c = P.coefficient ? *P.coefficient : 1.0f;
-    float *const pw = P.w[t], *const scales = P.scales[t];
-    uint8_t *const pm = P.m[t], *const pv = P.v[t];
-    const G *const pg = static_cast<const G *>(P.g[t]);
-    float w[kCodedRows][4], g[kCodedRows][4], am[kCodedRows], av[kCodedRows];
-    uint32_t cm[kCodedRows], cv[kCodedRows];
+    decode_m(m, codes_m, old_a);
+    decode_v(v, codes_v, old_b);
+    uint32_t top_m = 0, top_v = 0;
 #pragma unroll
-    for (uint32_t r = 0; r < kCodedRows; ++r) {
-        const uint64_t i = (block0 + r) * kStateBlock + lane * 4u;
-        const int64_t have = (int64_t)n - (int64_t)i;
-        const bool some = (block0 + r) * kStateBlock < n;
-        am[r] = some ? scales[2u * (block0 + r)] : 0.0f;
-        av[r] = some ? scales[2u * (block0 + r) + 1u] : 0.0f;
-        cm[r] = load_codes(pm + i, have);
-        cv[r] = load_codes(pv + i, have);
-        load_some<4>(g[r], pg + i, have);
-        load_some<4>(w[r], pw + i, have);
+    for (int e = 0; e < 4; ++e) {
+        adamw_moments(m[e], v[e], g[e] * c, P.num);
+        top_m = max(top_m, kWhole || e < have ? __builtin_bit_cast(uint32_t, m[e]) & 0x7FFFFFFFu : 0u);
+        top_v = max(top_v, kWhole || e < have ? __builtin_bit_cast(uint32_t, v[e]) : 0u);
     }
-    bool lost = false;
-#pragma unroll
-    for (uint32_t r = 0; r < kCodedRows; ++r) {
-        const uint64_t i = (block0 + r) * kStateBlock + lane * 4u;
-        const int64_t have = (int64_t)n - (int64_t)i;
-        float m[4], v[4];
-        decode_m(m, cm[r], am[r]);
-        decode_v(v, cv[r], av[r]);
-        uint32_t top_m = 0, top_v = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            adamw_moments(m[e], v[e], g[r][e] * c, P.num);
-            top_m = max(top_m, e < have ? __builtin_bit_cast(uint32_t, m[e]) & 0x7FFFFFFFu : 0u);
-            top_v = max(top_v, e < have ? __builtin_bit_cast(uint32_t, v[e]) : 0u);
-        }
-        top_m = wave_max(top_m);
-        top_v = wave_max(top_v);
-        if (max(top_m, top_v) >= 0x7F800000u) {
-            lost = true;
-            if constexpr (kCopy)
-                store_some<4>(static_cast<C *>(P.copy[t]) + i, w[r], have);
-            continue;
-        }
+    top_m = wave_max(top_m);
+    top_v = wave_max(top_v);
+    if (max(top_m, top_v) < 0x7F800000u) {
         top_m = top_m < 0x00800000u ? 0u : top_m;
         top_v = top_v < 0x00800000u ? 0u : top_v;
         const float a = __builtin_bit_cast(float, top_m), b = __builtin_bit_cast(float, top_v);
-        store_codes(pm + i, encode_m(m, top_m ? 1.0f / a : 0.0f), have);
-        store_codes(pv + i, encode_v(v, top_v ? 1.0f / b : 0.0f), have);
-        if (lane == 0 && have > 0) {
-            scales[2u * (block0 + r)] = a;
-            scales[2u * (block0 + r) + 1u] = b;
+        store_codes<kWhole, kOnce>(P.m[t] + i, encode_m(m, top_m ? 1.0f / a : 0.0f), have);
+        store_codes<kWhole, kOnce>(P.v[t] + i, encode_v(v, top_v ? 1.0f / b : 0.0f), have);
+        if (lane == 0) {
+            scales[0] = a;
+            scales[1] = b;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            w[r][e] = adamw_weight(w[r][e], m[e], v[e], keep, P.num);
-        store_some<4>(pw + i, w[r], have);
-        if constexpr (kCopy)
-            store_some<4>(static_cast<C *>(P.copy[t]) + i, w[r], have);
-    }
-    if (lost && lane == 0)
+            w[e] = adamw_weight(w[e], m[e], v[e], keep, P.num);
+        store_some<4, kWhole, kOnce>(P.w[t] + i, w, have);
+    } else if (lane == 0) {
         atomicOr(P.flags, NUQ_FLAG_NONFINITE);
+    }
+    if constexpr (kCopy)
+        store_some<4, kWhole, kOnce>(static_cast<C *>(P.copy[t]) + i, w, have);
+}
+
+template <class G, class C, bool kCopy, bool kOnce>
+__global__ __launch_bounds__(256) void k_adamw_coded(const AdamwCodedTable P)
+{
+    const uint32_t t = P.count == 1u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start, P.count, blockIdx.x));
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint64_t block = (uint64_t)(blockIdx.x - P.start[t]) * 4u + wave, n = P.n[t];
+    if ((block + 1u) * kStateBlock <= n)
+        adamw_block<G, C, kCopy, kOnce, true>(P, t, block);
+    else if (block * kStateBlock < n)
+        adamw_block<G, C, kCopy, kOnce, false>(P, t, block);
 }
 
 // The values that the codes of one tensor stand for.
+template <bool kOnce>
 __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *pm, const uint8_t *pv, const float *scales, float *m,
                                                       float *v, uint64_t n)
 {
@@ -256,11 +269,12 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *pm, const u
     const int64_t have = (int64_t)n - (int64_t)i;
     if (have <= 0)
         return;
-    float x[4];
-    decode_m(x, load_codes(pm + i, have), scales[2u * block]);
-    store_some<4>(m + i, x, have);
-    decode_v(x, load_codes(pv + i, have), scales[2u * block + 1u]);
-    store_some<4>(v + i, x, have);
+    const uint32_t codes_m = load_codes<false, kOnce>(pm + i, have), codes_v = load_codes<false, kOnce>(pv + i, have);
+    float x[4], y[4];
+    decode_m(x, codes_m, scales[2u * block]);
+    decode_v(y, codes_v, scales[2u * block + 1u]);
+    store_some<4, false, kOnce>(m + i, x, have);
+    store_some<4, false, kOnce>(v + i, y, have);
 }
 
 // ---- the norm of all gradients ----
@@ -268,7 +282,7 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *pm, const u
 // workgroup adds them in a fixed order.
 
 constexpr uint32_t kNormTensors = 128;
-constexpr uint32_t kNormChunk = 256u * 4u * 4u;
+constexpr uint32_t kNormChunk = 4096u;
 constexpr uint32_t kNormPartials = NUQ_GRADIENT_NORM_WORKSPACE_BYTES / sizeof(double);
 
 struct NormTable {
@@ -279,6 +293,25 @@ struct NormTable {
     double *partial;
 };
 static_assert(sizeof(NormTable) <= 4096, "a launch's arguments");
+
+template <class G, int WG, bool kWhole>
+__device__ __forceinline__ double square_sum(const G *pg, uint64_t base, uint64_t n)
+{
+    constexpr int VEC = 16 / sizeof(G), ROWS = (int)kNormChunk / (WG * VEC);
+    float g[ROWS][VEC];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const uint64_t i = base + (uint64_t)(r * WG + (int)threadIdx.x) * VEC;
+        load_some<VEC, kWhole>(g[r], pg + i, (int64_t)n - (int64_t)i);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            sum = __builtin_fma((double)g[r][e], (double)g[r][e], sum);
+    return sum;
+}
 
 // Workgroup p takes the p-th share of the chunks and writes partial[p].
 template <class G>
@@ -299,42 +332,70 @@ __global__ __launch_bounds__(256) void k_gradient_norm(const NormTable P)
             ++t;
         const G *const pg = static_cast<const G *>(P.g[t]);
         const uint64_t base = (uint64_t)(chunk - P.start[t]) * kNormChunk, n = P.n[t];
-        float g[4][4];
-#pragma unroll
-        for (uint32_t r = 0; r < 4u; ++r) {
-            const uint64_t i = base + (r * 256u + threadIdx.x) * 4u;
-            load_some<4>(g[r], pg + i, (int64_t)n - (int64_t)i);
-        }
-#pragma unroll
-        for (uint32_t r = 0; r < 4u; ++r)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                sum += (double)g[r][e] * (double)g[r][e];
+        sum += base + kNormChunk <= n ? square_sum<G, 256, true>(pg, base, n) : square_sum<G, 256, false>(pg, base, n);
     }
     sum = workgroup_sum<256>(sum, red);
     if (threadIdx.x == 0)
         P.partial[blockIdx.x] = sum;
 }
 
-// out[0] = the norm, out[1] = min(1, max_norm / norm); a norm that is not finite makes both NaN or infinite as it is, and the
-// factor NaN: a step behind it changes nothing.
+// out[0] = the norm, out[1] = min(1, max_norm / norm); NaN where the norm is not finite: a step behind it changes nothing.
+__device__ __forceinline__ void norm_and_factor(double sum, float max_norm, float *out, uint32_t *flags)
+{
+    const double norm = sqrt(sum);
+    const float rounded = (float)norm;
+    const bool fine = rounded < __builtin_inff();
+    out[0] = rounded;
+    out[1] = !fine ? __builtin_nanf("") : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
+    if (!fine)
+        atomicOr(flags, NUQ_FLAG_NONFINITE);
+}
+
 __global__ __launch_bounds__(1024) void k_gradient_norm_finish(const double *partial, uint32_t count, float max_norm, float *out,
                                                                uint32_t *flags)
 {
     __shared__ double red[16];
+    double x[kNormPartials / 1024u];
+#pragma unroll
+    for (uint32_t k = 0; k < kNormPartials / 1024u; ++k)     // all loads at once
+        x[k] = threadIdx.x + k * 1024u < count ? partial[threadIdx.x + k * 1024u] : 0.0;
     double sum = 0.0;
-    for (uint32_t p = threadIdx.x; p < count; p += 1024u)
-        sum += partial[p];
+#pragma unroll
+    for (uint32_t k = 0; k < kNormPartials / 1024u; ++k)
+        sum += x[k];
     sum = workgroup_sum<1024>(sum, red);
-    if (threadIdx.x == 0) {
-        const double norm = sqrt(sum);
-        const float rounded = (float)norm;
-        const bool fine = rounded < __builtin_inff();
-        out[0] = rounded;
-        out[1] = !fine ? __builtin_nanf("") : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
-        if (!fine)
-            atomicOr(flags, NUQ_FLAG_NONFINITE);
+    if (threadIdx.x == 0)
+        norm_and_factor(sum, max_norm, out, flags);
+}
+
+// All of it in one workgroup, eight chunks at a time.
+template <class G>
+__global__ __launch_bounds__(1024) void k_gradient_norm_small(const NormTable P, float max_norm, float *out, uint32_t *flags)
+{
+    constexpr int VEC = (int)kNormChunk / 1024;
+    __shared__ double red[16];
+    const uint32_t chunks = P.start[P.count];
+    uint32_t t = 0;
+    double sum = 0.0;
+    for (uint32_t first = 0; first < chunks; first += 8u) {
+        float g[8][VEC];
+#pragma unroll
+        for (uint32_t k = 0; k < 8u; ++k) {
+            const uint32_t chunk = first + k < chunks ? first + k : chunks - 1u;
+            while (chunk >= P.start[t + 1u])
+                ++t;
+            const uint64_t i = (uint64_t)(chunk - P.start[t]) * kNormChunk + threadIdx.x * VEC;
+            load_some<VEC>(g[k], static_cast<const G *>(P.g[t]) + i, first + k < chunks ? (int64_t)P.n[t] - (int64_t)i : 0);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 8u; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                sum = __builtin_fma((double)g[k][e], (double)g[k][e], sum);
     }
+    sum = workgroup_sum<1024>(sum, red);
+    if (threadIdx.x == 0)
+        norm_and_factor(sum, max_norm, out, flags);
 }
 
 }  // namespace nuq

@@ -12,8 +12,42 @@
 
 namespace nuq {
 
-template <class T>
-constexpr int kVecOf = 16 / sizeof(T);         // elements of a 16-byte access
+// How a team of TEAM threads holds a row: each has E elements, in vectors of VEC neighbouring ones (16 bytes, or single elements
+// for rows shorter than that).  A thread whose vector would end behind the row takes the row's last VEC elements instead: its
+// loads need no branch, it computes what a neighbour computes too for the elements they share, and leaves these out of sums.
+template <class T, int TEAM_, int E, int VEC_>
+struct RowShape {
+    static constexpr int TEAM = TEAM_, VEC = VEC_, NV = E / VEC_;
+    static_assert(E % VEC_ == 0, "whole vectors");
+    uint32_t at[NV];            // first column of each vector
+    uint32_t twice[NV];         // elements of it that a neighbour has too: VEC for a vector that is not there
+    __device__ __forceinline__ explicit RowShape(uint32_t hidden)
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const uint32_t col = (uint32_t)(k * TEAM + (int)(threadIdx.x % TEAM)) * VEC;
+            at[k] = min(col, hidden - VEC);
+            twice[k] = min(col - at[k], (uint32_t)VEC);
+        }
+    }
+    __device__ __forceinline__ bool there(int k) const { return twice[k] < (uint32_t)VEC; }
+    __device__ __forceinline__ bool counts(int k, int e) const { return (uint32_t)e >= twice[k]; }
+    template <class V>
+    __device__ __forceinline__ void load(Vec<V, VEC> (&to)[NV], const V *row) const
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            to[k] = *reinterpret_cast<const Vec<V, VEC> *>(row + at[k]);
+    }
+    template <class V>
+    __device__ __forceinline__ void store(V *row, const float (&from)[NV][VEC]) const
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (there(k))
+                store_from_float<VEC>(row + at[k], from[k]);
+    }
+};
 
 struct LayerNormForward {
     const void *x, *residual, *weight, *bias;  // residual, weight, bias: may be none
@@ -44,82 +78,78 @@ __device__ __forceinline__ float row_sum(float x, float *red)
     }
 }
 
-template <class T, class W, int TEAM, int NV, bool kStream>
+// A team takes rows in turn; the next row is on its way while one is worked on, weight and bias stay in registers.
+template <class T, class W, int TEAM, int E, int VEC, bool kStream>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_forward(const LayerNormForward P)
 {
-    constexpr int VEC = kVecOf<T>, WG = TEAM < 256 ? 256 : TEAM;
+    using Shape = RowShape<T, TEAM, E, VEC>;
+    constexpr int NV = Shape::NV, TEAMS = TEAM < 256 ? 256 / TEAM : 1;
     __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
-    const uint64_t row = (uint64_t)blockIdx.x * (WG / TEAM) + threadIdx.x / TEAM;
+    const uint32_t hidden = P.hidden;
+    const Shape S(hidden);
+    const W *const weight = static_cast<const W *>(P.weight), *const bias = static_cast<const W *>(P.bias);
+    uint64_t row = (uint64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
     if (row >= P.rows)                                       // (a whole team; teams of more than a wave are the workgroup)
         return;
-    const uint32_t lane = threadIdx.x % TEAM;
-    const T *const x = static_cast<const T *>(P.x) + row * P.ldx;
-    float s[NV][VEC], sum = 0.0f;
+    Vec<T, VEC> xs[NV], rs[NV];
+    Vec<W, VEC> ws[NV], bs[NV];
+    const auto load = [&]() {
+        S.load(xs, static_cast<const T *>(P.x) + row * P.ldx);
+        if constexpr (kStream)
+            S.load(rs, static_cast<const T *>(P.residual) + row * P.ldr);
+    };
+    load();
+    if (weight)
+        S.load(ws, weight);
+    if (bias)
+        S.load(bs, bias);
+    for (;;) {
+        const uint64_t now = row;
+        float s[NV][VEC], sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const uint32_t col = (k * TEAM + lane) * VEC;
-        load_some<VEC>(s[k], x + col, (int64_t)P.hidden - col);
-    }
-    if constexpr (kStream) {
-        const T *const res = static_cast<const T *>(P.residual) + row * P.ldr;
-        T *const total = static_cast<T *>(P.total) + row * P.ldt;
-        float r[NV][VEC];
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * TEAM + lane) * VEC;
-            load_some<VEC>(r[k], res + col, (int64_t)P.hidden - col);
+            for (int e = 0; e < VEC; ++e) {
+                s[k][e] = (float)xs[k][e];
+                if constexpr (kStream)
+                    s[k][e] = (float)(T)(s[k][e] + (float)rs[k][e]);
+                sum += S.counts(k, e) ? s[k][e] : 0.0f;
+            }
+        row += (uint64_t)gridDim.x * TEAMS;
+        const bool more = row < P.rows;
+        if (more)
+            load();
+        const float mean = row_sum<TEAM>(sum, red[0]) / (float)hidden;
+        if constexpr (kStream)                               // (behind the barrier: total may be x or residual)
+            S.store(static_cast<T *>(P.total) + now * P.ldt, s);
+        float square = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                s[k][e] -= mean;
+                square = __builtin_fmaf(S.counts(k, e) ? s[k][e] : 0.0f, s[k][e], square);
+            }
+        const float rstd = 1.0f / __builtin_sqrtf(row_sum<TEAM>(square, red[1]) / (float)hidden + P.eps);
+        if (threadIdx.x % TEAM == 0) {
+            if (P.mean)
+                P.mean[now] = mean;
+            if (P.rstd)
+                P.rstd[now] = rstd;
         }
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * TEAM + lane) * VEC;
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                s[k][e] = (float)(T)(s[k][e] + r[k][e]);
-            store_some<VEC>(total + col, s[k], (int64_t)P.hidden - col);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            sum += s[k][e];
-    const float mean = row_sum<TEAM>(sum, red[0]) / (float)P.hidden;
-    float square = 0.0f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const uint32_t col = (k * TEAM + lane) * VEC;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            s[k][e] = col + e < P.hidden ? s[k][e] - mean : 0.0f;
-            square = __builtin_fmaf(s[k][e], s[k][e], square);
-        }
-    }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<TEAM>(square, red[1]) / (float)P.hidden + P.eps);
-    if (lane == 0) {
-        if (P.mean)
-            P.mean[row] = mean;
-        if (P.rstd)
-            P.rstd[row] = rstd;
-    }
-    T *const y = static_cast<T *>(P.y) + row * P.ldy;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const uint32_t col = (k * TEAM + lane) * VEC;
-        const int64_t have = (int64_t)P.hidden - col;
-        float w[VEC], b[VEC];
-        if (P.weight)
-            load_some<VEC>(w, static_cast<const W *>(P.weight) + col, have);
-        if (P.bias)
-            load_some<VEC>(b, static_cast<const W *>(P.bias) + col, have);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            s[k][e] *= rstd;
-            if (P.weight)
-                s[k][e] *= w[e];
-            if (P.bias)
-                s[k][e] += b[e];
-        }
-        store_some<VEC>(y + col, s[k], have);
+            for (int e = 0; e < VEC; ++e) {
+                s[k][e] *= rstd;
+                if (weight)
+                    s[k][e] *= (float)ws[k][e];
+                if (bias)
+                    s[k][e] += (float)bs[k][e];
+            }
+        S.store(static_cast<T *>(P.y) + now * P.ldy, s);
+        if (!more)
+            break;
     }
 }
 
@@ -179,45 +209,65 @@ struct LayerNormBackward {
     uint32_t hidden;
 };
 
-// Workgroup p takes rows p, p + parts, ... of each of its teams' strides and writes partial[p].
-template <class T, class W, int TEAM, int NV, bool kSums>
+// A team takes rows in turn, as in the forward pass, and keeps the sums of its columns in registers.  Workgroup p writes
+// partial[p].
+template <class T, class W, int TEAM, int E, int VEC, bool kSums>
 __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward(const LayerNormBackward P)
 {
-    constexpr int VEC = kVecOf<T>, WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM, WAVES = WG / 64;
+    using Shape = RowShape<T, TEAM, E, VEC>;
+    constexpr int NV = Shape::NV, WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM, WAVES = WG / 64;
+    constexpr bool kAhead = TEAM < 1024;                     // (sixteen waves leave too few registers for a row ahead)
     __shared__ float red[2][2][WAVES];
-    const uint32_t lane = threadIdx.x % TEAM;
+    const uint32_t hidden = P.hidden;
+    const Shape S(hidden);
+    const W *const weight = static_cast<const W *>(P.weight);
+    const float per = 1.0f / (float)hidden;
     float dw[NV][VEC] = {}, db[NV][VEC] = {};
     uint32_t turn = 0;
-    for (uint64_t row = (uint64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM; row < P.rows; row += (uint64_t)gridDim.x * TEAMS) {
-        const T *const x = static_cast<const T *>(P.x) + row * P.ldx;
-        const T *const dy = static_cast<const T *>(P.dy) + row * P.ldg;
-        const float mean = P.mean[row], rstd = P.rstd[row];
+    Vec<T, VEC> xs[NV], gs[NV], as[NV];
+    Vec<W, VEC> ws[NV];
+    float mean = 0.0f, rstd = 0.0f;
+    uint64_t row = (uint64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+    const auto load = [&]() {
+        mean = P.mean[row];
+        rstd = P.rstd[row];
+        S.load(gs, static_cast<const T *>(P.dy) + row * P.ldg);
+        S.load(xs, static_cast<const T *>(P.x) + row * P.ldx);
+        if (P.add)
+            S.load(as, static_cast<const T *>(P.add) + row * P.lda);
+    };
+    if (kAhead && row < P.rows)
+        load();
+    if (weight)
+        S.load(ws, weight);
+    while (row < P.rows) {
+        if (!kAhead)
+            load();
+        const uint64_t now = row;
+        const float scale = rstd;
         float n[NV][VEC], d[NV][VEC], s1 = 0.0f, s2 = 0.0f;
+        Vec<T, VEC> a[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * TEAM + lane) * VEC;
-            load_some<VEC>(n[k], x + col, (int64_t)P.hidden - col);
-            load_some<VEC>(d[k], dy + col, (int64_t)P.hidden - col);
-        }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * TEAM + lane) * VEC;
-            float w[VEC];
-            if (P.weight)
-                load_some<VEC>(w, static_cast<const W *>(P.weight) + col, (int64_t)P.hidden - col);
+            a[k] = as[k];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                n[k][e] = (n[k][e] - mean) * rstd;           // (beyond the row dy is 0, and so is what is made of it)
+                n[k][e] = ((float)xs[k][e] - mean) * rstd;
+                d[k][e] = (float)gs[k][e];
                 if constexpr (kSums) {
                     dw[k][e] = __builtin_fmaf(d[k][e], n[k][e], dw[k][e]);
                     db[k][e] += d[k][e];
                 }
-                if (P.weight)
-                    d[k][e] *= w[e];
-                s1 += d[k][e];
-                s2 = __builtin_fmaf(d[k][e], n[k][e], s2);
+                if (weight)
+                    d[k][e] *= (float)ws[k][e];
+                const float c = S.counts(k, e) ? d[k][e] : 0.0f;
+                s1 += c;
+                s2 = __builtin_fmaf(c, n[k][e], s2);
             }
         }
+        row += (uint64_t)gridDim.x * TEAMS;
+        if (kAhead && row < P.rows)
+            load();
         if constexpr (TEAM <= 64) {
             s1 = team_sum<TEAM>(s1);
             s2 = team_sum<TEAM>(s2);
@@ -238,61 +288,49 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward
             }
             turn ^= 1u;
         }
-        s1 /= (float)P.hidden;
-        s2 /= (float)P.hidden;
-        T *const dx = static_cast<T *>(P.dx) + row * P.ldd;
+        s1 *= per;
+        s2 *= per;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const uint32_t col = (k * TEAM + lane) * VEC;
-            const int64_t have = (int64_t)P.hidden - col;
-            float a[VEC];
-            if (P.add)
-                load_some<VEC>(a, static_cast<const T *>(P.add) + row * P.lda + col, have);
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                d[k][e] = (d[k][e] - s1 - n[k][e] * s2) * rstd;
+                d[k][e] = (d[k][e] - s1 - n[k][e] * s2) * scale;
                 if (P.add)
-                    d[k][e] += a[e];
+                    d[k][e] += (float)a[k][e];
             }
-            store_some<VEC>(dx + col, d[k], have);
-        }
+        S.store(static_cast<T *>(P.dx) + now * P.ldd, d);
     }
     if constexpr (kSums) {
-        float *const out = P.partial + (uint64_t)blockIdx.x * 2u * P.hidden;
+        float *const out = P.partial + (uint64_t)blockIdx.x * 2u * hidden;
         if constexpr (TEAM <= 64) {                          // the workgroup's teams, in a fixed order
-            constexpr int COLS = NV * TEAM * VEC;
-            __shared__ float all[WAVES][2][COLS];
+            __shared__ float all[WAVES][TEAM * E];
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+            for (int which = 0; which < 2; ++which) {
+                if (which)
+                    __syncthreads();
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
+                for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int off = TEAM; off < 64; off <<= 1) {
-                        dw[k][e] += __shfl_xor(dw[k][e], off, 64);
-                        db[k][e] += __shfl_xor(db[k][e], off, 64);
+                    for (int e = 0; e < VEC; ++e) {
+                        float sum = which ? db[k][e] : dw[k][e];
+#pragma unroll
+                        for (int off = TEAM; off < 64; off <<= 1)
+                            sum += __shfl_xor(sum, off, 64);
+                        if (threadIdx.x % 64u < TEAM && S.counts(k, e))
+                            all[threadIdx.x / 64u][S.at[k] + e] = sum;
                     }
-                    if (threadIdx.x % 64u < TEAM) {
-                        all[threadIdx.x / 64u][0][(k * TEAM + lane) * VEC + e] = dw[k][e];
-                        all[threadIdx.x / 64u][1][(k * TEAM + lane) * VEC + e] = db[k][e];
-                    }
-                }
-            __syncthreads();
-            for (uint32_t c = threadIdx.x; c < P.hidden; c += WG)
-#pragma unroll
-                for (int which = 0; which < 2; ++which) {
-                    float sum = all[0][which][c];
+                __syncthreads();
+                for (uint32_t c = threadIdx.x; c < hidden; c += WG) {
+                    float sum = all[0][c];
 #pragma unroll
                     for (int k = 1; k < WAVES; ++k)
-                        sum += all[k][which][c];
-                    out[which * P.hidden + c] = sum;
+                        sum += all[k][c];
+                    out[which * hidden + c] = sum;
                 }
-        } else {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const uint32_t col = (k * TEAM + lane) * VEC;
-                store_some<VEC>(out + col, dw[k], (int64_t)P.hidden - col);
-                store_some<VEC>(out + P.hidden + col, db[k], (int64_t)P.hidden - col);
             }
+        } else {                                             // (a shared column: the same sum from both)
+            S.store(out, dw);
+            S.store(out + hidden, db);
         }
     }
 }
@@ -347,27 +385,41 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackw
     P.partial[(uint64_t)blockIdx.y * 2u * P.hidden + P.hidden + col] = db;
 }
 
-// dweight and dbias (blockIdx.y) from the partial sums, in a fixed order: 64 columns per workgroup, 16 threads to each.
+// dweight and dbias (blockIdx.y) from the partial sums, in a fixed order: 16 columns per workgroup, 64 threads to each.
 template <class W>
 __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, W *dweight,
                                                             W *dbias)
 {
-    __shared__ float red[16][64];
+    __shared__ float red[64][17];
     W *const out = blockIdx.y ? dbias : dweight;
     if (!out)
         return;
-    const uint32_t col = blockIdx.x * 64u + threadIdx.x % 64u, group = threadIdx.x / 64u;
+    const uint32_t c = threadIdx.x % 16u, group = threadIdx.x / 16u, col = blockIdx.x * 16u + c;
     float sum = 0.0f;
-    if (col < hidden)
-        for (uint32_t p = group; p < parts; p += 16u)
-            sum += partial[((uint64_t)p * 2u + blockIdx.y) * hidden + col];
-    red[group][threadIdx.x % 64u] = sum;
-    __syncthreads();
-    if (group == 0 && col < hidden) {
+    if (col < hidden) {
+        const float *const from = partial + (uint64_t)blockIdx.y * hidden + col;
+        uint32_t p = group;
+        for (; p + 192u < parts; p += 256u) {                // four loads at once
+            float x[4];
 #pragma unroll
-        for (int k = 1; k < 16; ++k)
-            sum += red[k][threadIdx.x % 64u];
-        out[col] = (W)sum;
+            for (uint32_t k = 0; k < 4u; ++k)
+                x[k] = from[(uint64_t)(p + 64u * k) * 2u * hidden];
+            sum += (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        for (; p < parts; p += 64u)
+            sum += from[(uint64_t)p * 2u * hidden];
+    }
+    red[group][c] = sum;
+    __syncthreads();
+    if (threadIdx.x < 64u) {                                 // one wave: four lanes to a column
+        const uint32_t cc = threadIdx.x / 4u, part = threadIdx.x % 4u, to = blockIdx.x * 16u + cc;
+        sum = 0.0f;
+#pragma unroll
+        for (uint32_t k = 0; k < 16u; ++k)
+            sum += red[part * 16u + k][cc];
+        sum = team_sum<4>(sum);
+        if (part == 0 && to < hidden)
+            out[to] = (W)sum;
     }
 }
 

@@ -3,6 +3,7 @@
 #include "../../include/nuq.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -28,6 +29,11 @@ int with_type(uint32_t type, F &&f)
 }
 
 uint32_t width(uint32_t type) { return type == NUQ_F32 ? 4u : 2u; }
+
+// Arrays that fit this are read and written plainly: they may still be there, and stay for what comes next.  Larger ones take
+// non-temporal loads and stores: an AdamW step on 25.6 M elements (409 MB) 163 -> 130 us, on 1.56 G 8.10 -> 7.52 ms; on 117 MB
+// of 8-bit states, weights and gradients they cost 2 %.
+constexpr uint64_t kLastLevelCache = 256ull << 20;
 
 bool off_grid(const void *p, uint32_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) != 0; }
 
@@ -72,17 +78,26 @@ struct AdamwCall {
         return w[j] == w[i] + before && g[j] == g_at(i, before) && keep(i) == keep(j) &&
                (!copy || copy[j] == static_cast<char *>(copy[i]) + before * 2u);
     }
-    // f(gradient type, copy type, whether there is a copy)
+    // f(gradient type, copy type, whether there is a copy, whether the arrays, `bytes` per element and gradient and copy, are
+    // larger than the last-level cache)
     template <class F>
-    int with_types(F &&f) const
+    int with_types(uint32_t bytes, F &&f) const
     {
+        uint64_t all = 0;
+        for (uint32_t i = 0; i < T; ++i)
+            all += n[i];
+        const bool once = all > kLastLevelCache / (bytes + width(g_type) + (copy ? 2u : 0u));
         return with_type(g_type, [&](auto gt) {
-            return !copy                     ? f(gt, Type<__bf16>{}, std::false_type{})
-                   : copy_type == NUQ_BF16 ? f(gt, Type<__bf16>{}, std::true_type{})
-                                           : f(gt, Type<_Float16>{}, std::true_type{});
+            const auto with_copy = [&](auto ct, auto has) { return once ? f(gt, ct, has, std::true_type{}) : f(gt, ct, has, std::false_type{}); };
+            return !copy                     ? with_copy(Type<__bf16>{}, std::false_type{})
+                   : copy_type == NUQ_BF16 ? with_copy(Type<__bf16>{}, std::true_type{})
+                                           : with_copy(Type<_Float16>{}, std::true_type{});
         });
     }
 };
+
+// Chunks whose norm one workgroup takes in a launch of its own, where two launches cost more than what they win.
+constexpr uint32_t kSmallChunks = 32;
 
 // Walks the tensors of a call, joined where one follows another, and fills tables of at most kMost of them: put(slot, tensor,
 // elements) for each, launch(tensors, chunks) for each table.  Runs are cut so that a launch has at most 2^30 chunks.
@@ -141,14 +156,16 @@ int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint3
     NormTable P;
     double *const partial = static_cast<double *>(workspace);
     // the launches share the partials
-    uint32_t launches = 0;
-    (void)for_tables<kNormTensors>(T, n, kNormChunk, follows, [](auto...) {}, [&](uint32_t, uint32_t) {
+    uint32_t launches = 0, only = 0;
+    (void)for_tables<kNormTensors>(T, n, kNormChunk, follows, [](auto...) {}, [&](uint32_t, uint32_t chunks) {
         ++launches;
+        only = chunks;
         return (int)NUQ_OK;
     });
+    const bool small = launches == 1 && only <= kSmallChunks;
     if (launches > kNormPartials)
         return NUQ_EINVAL;
-    const uint32_t most = launches ? std::min(2048u, kNormPartials / launches) : 0u;
+    const uint32_t most = launches ? kNormPartials / launches : 0u;
     uint32_t used = 0;
     const int rc = for_tables<kNormTensors>(
         T, n, kNormChunk, follows,
@@ -160,6 +177,12 @@ int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint3
         [&](uint32_t slots, uint32_t chunks) {
             P.start[slots] = chunks;
             P.count = slots;
+            if (small)
+                return with_type(type, [&](auto t) {
+                    hipLaunchKernelGGL(k_gradient_norm_small<typename decltype(t)::type>, dim3(1), dim3(1024), 0, st, P, max_norm,
+                                       out, flags);
+                    return check_launch();
+                });
             P.partial = partial + used;
             const uint32_t grid = std::min(chunks, most);
             used += grid;
@@ -168,7 +191,7 @@ int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint3
                 return check_launch();
             });
         });
-    if (rc != NUQ_OK)
+    if (rc != NUQ_OK || small)
         return rc;
     hipLaunchKernelGGL(k_gradient_norm_finish, dim3(1), dim3(1024), 0, st, partial, used, max_norm, out, flags);
     return check_launch();
@@ -208,9 +231,9 @@ int nuq_adamw_step(uint32_t T, float *const *w, const void *const *g, float *con
         },
         [&](uint32_t slots, uint32_t chunks) {
             P.count = slots;
-            return C.with_types([&](auto gt, auto ct, auto has) {
-                hipLaunchKernelGGL((k_adamw<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value>),
-                                   dim3(chunks), dim3(256), 0, st, P);
+            return C.with_types(12, [&](auto gt, auto ct, auto has, auto once) {
+                hipLaunchKernelGGL((k_adamw<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value,
+                                            decltype(once)::value>), dim3(chunks), dim3(256), 0, st, P);
                 return check_launch();
             });
         });
@@ -255,9 +278,9 @@ int nuq_adamw_step_coded(uint32_t T, float *const *w, const void *const *g, uint
         },
         [&](uint32_t slots, uint32_t chunks) {
             P.count = slots;
-            return C.with_types([&](auto gt, auto ct, auto has) {
-                hipLaunchKernelGGL((k_adamw_coded<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value>),
-                                   dim3(chunks), dim3(256), 0, st, P);
+            return C.with_types(6, [&](auto gt, auto ct, auto has, auto once) {
+                hipLaunchKernelGGL((k_adamw_coded<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value,
+                                                  decltype(once)::value>), dim3(chunks), dim3(256), 0, st, P);
                 return check_launch();
             });
         });
@@ -272,8 +295,11 @@ int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const
     if (!m_codes || !v_codes || !valid_array(scales, n, 4) || !valid_array(m, n, 4) || !valid_array(v, n, 4) ||
         groups > 0x7fffffffull)
         return NUQ_EINVAL;
-    hipLaunchKernelGGL(k_adamw_values, dim3((uint32_t)groups), dim3(256), 0, static_cast<hipStream_t>(stream), m_codes, v_codes,
-                       scales, m, v, n);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (n > kLastLevelCache / 10u)
+        hipLaunchKernelGGL(k_adamw_values<true>, dim3((uint32_t)groups), dim3(256), 0, st, m_codes, v_codes, scales, m, v, n);
+    else
+        hipLaunchKernelGGL(k_adamw_values<false>, dim3((uint32_t)groups), dim3(256), 0, st, m_codes, v_codes, scales, m, v, n);
     return check_launch();
 }
 
@@ -281,27 +307,51 @@ int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const
 
 namespace {
 
-// The team of threads and the 16-byte vectors per thread that hold a row of `vecs` such vectors: f(team, vectors), or f(0, 0)
-// where nothing does.
-template <class F>
-int with_row_shape(uint32_t vecs, F &&f)
+// The team of threads, the elements per thread and the vectors that hold a row of `hidden` elements of type T: f(team, elements,
+// vector), or f(0, 0, 0) where nothing does.
+template <class T, class F>
+int with_row_shape(uint32_t hidden, F &&f)
 {
     using std::integral_constant;
-#define NUQ_SHAPE(team, count)                                                                                        \
-    if (vecs <= team * count)                                                                                         \
-        return f(integral_constant<int, team>{}, integral_constant<int, count>{});
-    NUQ_SHAPE(4, 1)
-    NUQ_SHAPE(16, 1)
-    NUQ_SHAPE(16, 2)
-    NUQ_SHAPE(64, 1)
-    NUQ_SHAPE(64, 2)
-    NUQ_SHAPE(256, 1)
-    NUQ_SHAPE(256, 2)
-    NUQ_SHAPE(256, 4)
-    NUQ_SHAPE(512, 4)
-    NUQ_SHAPE(1024, 4)
+    constexpr int VEC = 16 / (int)sizeof(T);                // a 16-byte access
+    if (hidden < VEC)
+        return f(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
+#define NUQ_SHAPE(team, elements)                                                                                     \
+    if (hidden <= team * elements)                                                                                    \
+        return f(integral_constant<int, team>{}, integral_constant<int, elements>{}, integral_constant<int, VEC>{});
+    NUQ_SHAPE(4, 8)
+    NUQ_SHAPE(16, 8)
+    NUQ_SHAPE(16, 16)
+    NUQ_SHAPE(64, 8)
+    NUQ_SHAPE(64, 16)
+    NUQ_SHAPE(256, 8)
+    NUQ_SHAPE(256, 16)
+    NUQ_SHAPE(512, 16)
+    NUQ_SHAPE(768, 16)
+    NUQ_SHAPE(1024, 16)
 #undef NUQ_SHAPE
-    return f(integral_constant<int, 0>{}, integral_constant<int, 0>{});
+    return f(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 0>{});
+}
+
+// Workgroups of `threads` threads of a kernel that the current device holds at once (0 on error), looked up once per kernel and
+// device.
+template <auto kernel>
+uint32_t resident_workgroups(uint32_t threads)
+{
+    static std::atomic<uint32_t> known[64];
+    int dev = 0, per_cu = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0)
+        return 0;
+    uint32_t have = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0u;
+    if (!have) {
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, reinterpret_cast<const void *>(kernel), (int)threads, 0) != hipSuccess ||
+            hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || per_cu < 1 || cus < 1)
+            return 0;
+        have = (uint32_t)per_cu * (uint32_t)cus;
+        if (dev < 64)
+            known[dev].store(have, std::memory_order_relaxed);
+    }
+    return have;
 }
 
 // f(Type<element>, Type<weight>)
@@ -343,22 +393,23 @@ int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, ui
     return with_types(type, weight_type, [&](auto tt, auto wt) {
         using T = typename decltype(tt)::type;
         using W = typename decltype(wt)::type;
-        return with_row_shape((hidden + kVecOf<T> - 1) / kVecOf<T>, [&](auto team, auto count) {
-            constexpr int TEAM = decltype(team)::value, NV = decltype(count)::value;
-            if constexpr (TEAM == 0) {
-                if (residual)
-                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, true>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
-                else
-                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, false>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
-            } else {
-                constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
-                const dim3 grid((uint32_t)((rows + TEAMS - 1) / TEAMS));
-                if (residual)
-                    hipLaunchKernelGGL((k_layer_norm_forward<T, W, TEAM, NV, true>), grid, dim3(WG), 0, st, P);
-                else
-                    hipLaunchKernelGGL((k_layer_norm_forward<T, W, TEAM, NV, false>), grid, dim3(WG), 0, st, P);
-            }
-            return check_launch();
+        return with_row_shape<T>(hidden, [&](auto team, auto elements, auto vec) {
+            constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
+            const auto run = [&](auto stream_c) {
+                constexpr bool kStream = decltype(stream_c)::value;
+                if constexpr (TEAM == 0) {
+                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, kStream>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+                } else {
+                    constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
+                    const uint32_t most = resident_workgroups<k_layer_norm_forward<T, W, TEAM, E, VEC, kStream>>(WG);
+                    if (!most)
+                        return (int)NUQ_EHIP;
+                    const uint32_t grid = (uint32_t)std::min<uint64_t>((rows + TEAMS - 1) / TEAMS, most);
+                    hipLaunchKernelGGL((k_layer_norm_forward<T, W, TEAM, E, VEC, kStream>), dim3(grid), dim3(WG), 0, st, P);
+                }
+                return check_launch();
+            };
+            return residual ? run(std::true_type{}) : run(std::false_type{});
         });
     });
 }
@@ -390,28 +441,31 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
         using T = typename decltype(tt)::type;
         using W = typename decltype(wt)::type;
         uint32_t parts = 0;
-        const int rc = rows == 0 ? (int)NUQ_OK : with_row_shape((hidden + kVecOf<T> - 1) / kVecOf<T>, [&](auto team, auto count) {
-            constexpr int TEAM = decltype(team)::value, NV = decltype(count)::value;
+        const int rc = rows == 0 ? (int)NUQ_OK : with_row_shape<T>(hidden, [&](auto team, auto elements, auto vec) {
+            constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
             if constexpr (TEAM == 0) {
                 parts = (uint32_t)std::min<uint64_t>(rows, kLongParts);
                 if (sums)
                     hipLaunchKernelGGL((k_layer_norm_columns<T>), dim3((hidden + 255u) / 256u, parts), dim3(256), 0, st, P);
                 hipLaunchKernelGGL((k_layer_norm_backward_long<T, W>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+                return check_launch();
             } else {
                 constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
-                const uint64_t groups = (rows + TEAMS - 1) / TEAMS;
-                parts = (uint32_t)std::min<uint64_t>(groups, kParts);
-                if (sums)
-                    hipLaunchKernelGGL((k_layer_norm_backward<T, W, TEAM, NV, true>), dim3(parts), dim3(WG), 0, st, P);
-                else
-                    hipLaunchKernelGGL((k_layer_norm_backward<T, W, TEAM, NV, false>), dim3((uint32_t)std::min<uint64_t>(groups, 8192u)),
-                                       dim3(WG), 0, st, P);
+                const auto run = [&](auto sums_c) {
+                    constexpr bool kSums = decltype(sums_c)::value;
+                    const uint32_t most = resident_workgroups<k_layer_norm_backward<T, W, TEAM, E, VEC, kSums>>(WG);
+                    if (!most)
+                        return (int)NUQ_EHIP;
+                    parts = (uint32_t)std::min<uint64_t>((rows + TEAMS - 1) / TEAMS, kSums ? std::min(most, kParts) : most);
+                    hipLaunchKernelGGL((k_layer_norm_backward<T, W, TEAM, E, VEC, kSums>), dim3(parts), dim3(WG), 0, st, P);
+                    return check_launch();
+                };
+                return sums ? run(std::true_type{}) : run(std::false_type{});
             }
-            return check_launch();
         });
         if (rc != NUQ_OK || !sums)
             return rc;
-        hipLaunchKernelGGL((k_layer_norm_finish<W>), dim3((hidden + 63u) / 64u, 2), dim3(1024), 0, st, P.partial, parts, hidden,
+        hipLaunchKernelGGL((k_layer_norm_finish<W>), dim3((hidden + 15u) / 16u, 2), dim3(1024), 0, st, P.partial, parts, hidden,
                            static_cast<W *>(dweight), static_cast<W *>(dbias));
         return check_launch();
     });

@@ -15,43 +15,51 @@ struct VecOf {
 template <class T, int N>
 using Vec = typename VecOf<T, N>::type;
 
-template <int N, class T>
+// kOnce: with the hint that the memory is touched once.
+template <int N, bool kOnce = false, class T>
 __device__ __forceinline__ void load_as_float(float (&to)[N], const T *from)
 {
-    const Vec<T, N> v = *reinterpret_cast<const Vec<T, N> *>(from);
+    Vec<T, N> v;
+    if constexpr (kOnce)
+        v = __builtin_nontemporal_load(reinterpret_cast<const Vec<T, N> *>(from));
+    else
+        v = *reinterpret_cast<const Vec<T, N> *>(from);
 #pragma unroll
     for (int e = 0; e < N; ++e)
         to[e] = (float)v[e];
 }
 
 // Rounded to the nearest T, ties to even.
-template <int N, class T>
+template <int N, bool kOnce = false, class T>
 __device__ __forceinline__ void store_from_float(T *to, const float (&from)[N])
 {
     Vec<T, N> v;
 #pragma unroll
     for (int e = 0; e < N; ++e)
         v[e] = (T)from[e];
-    *reinterpret_cast<Vec<T, N> *>(to) = v;
+    if constexpr (kOnce)
+        __builtin_nontemporal_store(v, reinterpret_cast<Vec<T, N> *>(to));
+    else
+        *reinterpret_cast<Vec<T, N> *>(to) = v;
 }
 
-// The same for the first `have` elements; the others read as 0 and are not written.
-template <int N, class T>
+// The same for the first `have` elements; the others read as 0 and are not written.  kWhole: there are N.
+template <int N, bool kWhole = false, bool kOnce = false, class T>
 __device__ __forceinline__ void load_some(float (&to)[N], const T *from, int64_t have)
 {
-    if (have >= N) {
-        load_as_float<N>(to, from);
+    if (kWhole || have >= N) {
+        load_as_float<N, kOnce>(to, from);
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
             to[e] = e < have ? (float)from[e] : 0.0f;
     }
 }
-template <int N, class T>
+template <int N, bool kWhole = false, bool kOnce = false, class T>
 __device__ __forceinline__ void store_some(T *to, const float (&from)[N], int64_t have)
 {
-    if (have >= N) {
-        store_from_float<N>(to, from);
+    if (kWhole || have >= N) {
+        store_from_float<N, kOnce>(to, from);
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)

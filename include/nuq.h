@@ -413,7 +413,8 @@ int nuq_normalized_variance(const double *sum, const double *sumsq, uint64_t d, 
  * Summed in fp64 in an order that depends on the sizes alone: equal inputs give equal bits, and no square
  * overflows.  Where the norm is not finite (or above the largest float) out[1] is NaN, which the steps
  * below take as "leave everything as it is", and NUQ_FLAG_NONFINITE is raised.  max_norm: positive,
- * infinite for the norm alone (NUQ_EINVAL otherwise).  workspace: DEVICE memory of at least
+ * infinite for the norm alone (NUQ_EINVAL otherwise, also for more than 2^19 tensors none of which lies
+ * behind another).  workspace: DEVICE memory of at least
  * NUQ_GRADIENT_NORM_WORKSPACE_BYTES bytes, 8-byte aligned, overwritten. */
 #define NUQ_GRADIENT_NORM_WORKSPACE_BYTES 65536u
 int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint32_t type, float max_norm,
@@ -468,7 +469,8 @@ int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const
  * x, residual, total, y: DEVICE, of `type`, element-aligned, row r at r * ld elements (ldx, ldr: any;
  * ldt, ldy: at least hidden).  residual and total: both or neither.  weight, bias: hidden elements of
  * weight_type (`type` or NUQ_F32), each may be NULL.  mean, rstd: `rows` floats each, may be NULL.
- * y may be x.  Statistics in fp32, the variance from centred values.  eps: finite, not negative. */
+ * y may be x, total may be x or residual.  rows below 2^31, hidden at most 2^30.  Statistics in fp32, the
+ * variance from centred values.  eps: finite, not negative. */
 int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, uint64_t ldr,
                            const void *weight, const void *bias, uint64_t rows, uint32_t hidden, float eps,
                            uint32_t type, uint32_t weight_type, void *total, uint64_t ldt, void *y,

@@ -34,14 +34,17 @@ __device__ __forceinline__ float adamw_weight(float w, float m, float v, float k
 
 constexpr uint32_t kAdamwChunk = 256u * 4u;     // elements per workgroup: four per thread
 
+// What a launch's arguments hold for one tensor, side by side: a wave fetches it at once.
+struct AdamwTensor {
+    float *w, *m, *v;
+    const void *g;
+    void *copy;
+    uint64_t n;
+    float keep;                             // 1 - alpha * lambda
+};
 struct AdamwTable {
-    float *w[kTableTensors], *m[kTableTensors], *v[kTableTensors];
-    const void *g[kTableTensors];
-    void *copy[kTableTensors];
-    uint64_t n[kTableTensors];
-    float keep[kTableTensors];              // 1 - alpha * lambda
     uint32_t start[kTableTensors];
-    uint32_t count;
+    AdamwTensor tensor[kTableTensors];
     AdamwNumbers num;
     const float *coefficient;               // c, or none
     uint32_t *flags;
@@ -51,16 +54,16 @@ static_assert(sizeof(AdamwTable) <= 4096, "a launch's arguments");
 // One pass: 28 bytes per element with 32-bit gradients.  An element whose new moments are not finite is left as it is.
 // kOnce: the call's arrays are larger than the last-level cache.  kWhole: the workgroup's elements are all there.
 template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
-__device__ __forceinline__ void adamw_chunk(const AdamwTable &P, uint32_t t, uint64_t base)
+__device__ __forceinline__ void adamw_chunk(const AdamwTable &P, const AdamwTensor &X, uint64_t base)
 {
     const uint64_t i = base + threadIdx.x * 4u;
-    const int64_t have = (int64_t)P.n[t] - (int64_t)i;
+    const int64_t have = (int64_t)X.n - (int64_t)i;
     float w[4], m[4], v[4], g[4];
-    load_some<4, kWhole, kOnce>(g, static_cast<const G *>(P.g[t]) + i, have);
-    load_some<4, kWhole, kOnce>(m, P.m[t] + i, have);
-    load_some<4, kWhole, kOnce>(v, P.v[t] + i, have);
-    load_some<4, kWhole, kOnce>(w, P.w[t] + i, have);
-    const float keep = P.keep[t], c = P.coefficient ? *P.coefficient : 1.0f;
+    load_some<4, kWhole, kOnce>(g, static_cast<const G *>(X.g) + i, have);
+    load_some<4, kWhole, kOnce>(m, X.m + i, have);
+    load_some<4, kWhole, kOnce>(v, X.v + i, have);
+    load_some<4, kWhole, kOnce>(w, X.w + i, have);
+    const float keep = X.keep, c = P.coefficient ? *P.coefficient : 1.0f;
     float m1[4], v1[4];
     uint32_t top = 0;
 #pragma unroll
@@ -88,22 +91,23 @@ __device__ __forceinline__ void adamw_chunk(const AdamwTable &P, uint32_t t, uin
             w[e] = adamw_weight(w[e], m1[e], v1[e], keep, P.num);
         }
     }
-    store_some<4, kWhole, kOnce>(P.m[t] + i, m, have);
-    store_some<4, kWhole, kOnce>(P.v[t] + i, v, have);
-    store_some<4, kWhole, kOnce>(P.w[t] + i, w, have);
+    store_some<4, kWhole, kOnce>(X.m + i, m, have);
+    store_some<4, kWhole, kOnce>(X.v + i, v, have);
+    store_some<4, kWhole, kOnce>(X.w + i, w, have);
     if constexpr (kCopy)
-        store_some<4, kWhole, kOnce>(static_cast<C *>(P.copy[t]) + i, w, have);
+        store_some<4, kWhole, kOnce>(static_cast<C *>(X.copy) + i, w, have);
 }
 
 template <class G, class C, bool kCopy, bool kOnce>
 __global__ __launch_bounds__(256) void k_adamw(const AdamwTable P)
 {
-    const uint32_t t = P.count == 1u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start, P.count, blockIdx.x));
+    const uint32_t t = tensor_of(P.start, blockIdx.x);
+    const AdamwTensor &X = P.tensor[t];
     const uint64_t base = (uint64_t)(blockIdx.x - P.start[t]) * kAdamwChunk;
-    if (base + kAdamwChunk <= P.n[t])
-        adamw_chunk<G, C, kCopy, kOnce, true>(P, t, base);
+    if (base + kAdamwChunk <= X.n)
+        adamw_chunk<G, C, kCopy, kOnce, true>(P, X, base);
     else
-        adamw_chunk<G, C, kCopy, kOnce, false>(P, t, base);
+        adamw_chunk<G, C, kCopy, kOnce, false>(P, X, base);
 }
 
 // ---- states in 8 bits ----
@@ -117,17 +121,19 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamwTable P)
 constexpr uint32_t kStateBlock = NUQ_STATE_BLOCK;
 static_assert(kStateBlock == 256, "a wave holds four elements of a block per lane");
 constexpr uint32_t kCodedChunk = 4u * kStateBlock;              // elements per workgroup: a block per wave
-constexpr uint32_t kCodedTensors = 60;
+constexpr uint32_t kCodedTensors = 58;
 
+struct AdamwCodedTensor {
+    float *w, *scales;
+    uint8_t *m, *v;
+    const void *g;
+    void *copy;
+    uint64_t n;
+    float keep;
+};
 struct AdamwCodedTable {
-    float *w[kCodedTensors], *scales[kCodedTensors];
-    uint8_t *m[kCodedTensors], *v[kCodedTensors];
-    const void *g[kCodedTensors];
-    void *copy[kCodedTensors];
-    uint64_t n[kCodedTensors];
-    float keep[kCodedTensors];
     uint32_t start[kCodedTensors];
-    uint32_t count;
+    AdamwCodedTensor tensor[kCodedTensors];
     AdamwNumbers num;
     const float *coefficient;
     uint32_t *flags;
@@ -188,14 +194,15 @@ __device__ __forceinline__ uint32_t encode_m(const float (&m)[4], float inv)
     x = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * inv * 256.0f, m[3] * inv * 256.0f, x, true);
     return (uint32_t)x;
 }
-__device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv)
+// least: 1, or 0 in a block of zeros.
+__device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv, uint32_t least)
 {
     uint32_t x = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const uint32_t bits = __builtin_bit_cast(uint32_t, v[e] * inv * 0x1p-96f);
         uint32_t code = (bits + 0x7FFFFu + ((bits >> 20) & 1u)) >> 20;
-        code = max(code, v[e] > 0.0f && inv > 0.0f ? 1u : 0u);
+        code = max(code, min(__builtin_bit_cast(uint32_t, v[e]), least));
         x |= code << (8 * e);
     }
     return x;
@@ -204,18 +211,18 @@ __device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv)
 // One pass: 16 bytes per element with 32-bit gradients.  A block whose new moments are not all finite is left as it is.
 // kOnce as above; kWhole: the wave's block is all there.
 template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
-__device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, uint32_t t, uint64_t block)
+__device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, const AdamwCodedTensor &X, uint64_t block)
 {
     const uint32_t lane = threadIdx.x % 64u;
     const uint64_t i = block * kStateBlock + lane * 4u;
-    const int64_t have = (int64_t)P.n[t] - (int64_t)i;
-    float *const scales = P.scales[t] + 2u * block;
+    const int64_t have = (int64_t)X.n - (int64_t)i;
+    float *const scales = X.scales + 2u * block;
     float w[4], g[4], m[4], v[4];
-    const uint32_t codes_m = load_codes<kWhole, kOnce>(P.m[t] + i, have), codes_v = load_codes<kWhole, kOnce>(P.v[t] + i, have);
+    const uint32_t codes_m = load_codes<kWhole, kOnce>(X.m + i, have), codes_v = load_codes<kWhole, kOnce>(X.v + i, have);
     const float old_a = scales[0], old_b = scales[1];
-    load_some<4, kWhole, kOnce>(g, static_cast<const G *>(P.g[t]) + i, have);
-    load_some<4, kWhole, kOnce>(w, P.w[t] + i, have);
-    const float keep = P.keep[t], c = P.coefficient ? *P.coefficient : 1.0f;
+    load_some<4, kWhole, kOnce>(g, static_cast<const G *>(X.g) + i, have);
+    load_some<4, kWhole, kOnce>(w, X.w + i, have);
+    const float keep = X.keep, c = P.coefficient ? *P.coefficient : 1.0f;
     decode_m(m, codes_m, old_a);
     decode_v(v, codes_v, old_b);
     uint32_t top_m = 0, top_v = 0;
@@ -231,8 +238,8 @@ __device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, uint32_t t
         top_m = top_m < 0x00800000u ? 0u : top_m;
         top_v = top_v < 0x00800000u ? 0u : top_v;
         const float a = __builtin_bit_cast(float, top_m), b = __builtin_bit_cast(float, top_v);
-        store_codes<kWhole, kOnce>(P.m[t] + i, encode_m(m, top_m ? 1.0f / a : 0.0f), have);
-        store_codes<kWhole, kOnce>(P.v[t] + i, encode_v(v, top_v ? 1.0f / b : 0.0f), have);
+        store_codes<kWhole, kOnce>(X.m + i, encode_m(m, top_m ? 1.0f / a : 0.0f), have);
+        store_codes<kWhole, kOnce>(X.v + i, encode_v(v, top_v ? 1.0f / b : 0.0f, top_v ? 1u : 0u), have);
         if (lane == 0) {
             scales[0] = a;
             scales[1] = b;
@@ -240,24 +247,25 @@ __device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, uint32_t t
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             w[e] = adamw_weight(w[e], m[e], v[e], keep, P.num);
-        store_some<4, kWhole, kOnce>(P.w[t] + i, w, have);
+        store_some<4, kWhole, kOnce>(X.w + i, w, have);
     } else if (lane == 0) {
         atomicOr(P.flags, NUQ_FLAG_NONFINITE);
     }
     if constexpr (kCopy)
-        store_some<4, kWhole, kOnce>(static_cast<C *>(P.copy[t]) + i, w, have);
+        store_some<4, kWhole, kOnce>(static_cast<C *>(X.copy) + i, w, have);
 }
 
 template <class G, class C, bool kCopy, bool kOnce>
 __global__ __launch_bounds__(256) void k_adamw_coded(const AdamwCodedTable P)
 {
-    const uint32_t t = P.count == 1u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start, P.count, blockIdx.x));
+    const uint32_t t = tensor_of(P.start, blockIdx.x);
+    const AdamwCodedTensor &X = P.tensor[t];
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-    const uint64_t block = (uint64_t)(blockIdx.x - P.start[t]) * 4u + wave, n = P.n[t];
+    const uint64_t block = (uint64_t)(blockIdx.x - P.start[t]) * 4u + wave, n = X.n;
     if ((block + 1u) * kStateBlock <= n)
-        adamw_block<G, C, kCopy, kOnce, true>(P, t, block);
+        adamw_block<G, C, kCopy, kOnce, true>(P, X, block);
     else if (block * kStateBlock < n)
-        adamw_block<G, C, kCopy, kOnce, false>(P, t, block);
+        adamw_block<G, C, kCopy, kOnce, false>(P, X, block);
 }
 
 // The values that the codes of one tensor stand for.
@@ -281,18 +289,19 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *pm, const u
 // Sums of squares in fp64 (products of fp32 values are exact there, and no square overflows): a partial per workgroup, then one
 // workgroup adds them in a fixed order.
 
-constexpr uint32_t kNormTensors = 128;
 constexpr uint32_t kNormChunk = 4096u;
 constexpr uint32_t kNormPartials = NUQ_GRADIENT_NORM_WORKSPACE_BYTES / sizeof(double);
 
+struct NormTensor {
+    const void *g;
+    uint64_t n;
+};
 struct NormTable {
-    const void *g[kNormTensors];
-    uint64_t n[kNormTensors];
-    uint32_t start[kNormTensors + 1];       // start[count]: the chunks of all
-    uint32_t count;
+    uint32_t start[kTableTensors];
+    NormTensor tensor[kTableTensors];
+    uint32_t chunks;                        // of all
     double *partial;
 };
-static_assert(sizeof(NormTable) <= 4096, "a launch's arguments");
 
 template <class G, int WG, bool kWhole>
 __device__ __forceinline__ double square_sum(const G *pg, uint64_t base, uint64_t n)
@@ -318,20 +327,13 @@ template <class G>
 __global__ __launch_bounds__(256) void k_gradient_norm(const NormTable P)
 {
     __shared__ double red[4];
-    const uint64_t chunks = P.start[P.count];
+    const uint64_t chunks = P.chunks;
     const uint32_t first = (uint32_t)(chunks * blockIdx.x / gridDim.x), last = (uint32_t)(chunks * (blockIdx.x + 1u) / gridDim.x);
-    uint32_t t = 0;
-    for (uint32_t k = 0; k < P.count; k += 64u) {           // (the last of these steps that finds anything holds it)
-        const uint32_t left = P.count - k < 64u ? P.count - k : 64u;
-        if (P.start[k] <= first)
-            t = k + (uint32_t)__builtin_amdgcn_readfirstlane((int)tensor_of(P.start + k, left, first));
-    }
     double sum = 0.0;
     for (uint32_t chunk = first; chunk < last; ++chunk) {
-        while (chunk >= P.start[t + 1u])
-            ++t;
-        const G *const pg = static_cast<const G *>(P.g[t]);
-        const uint64_t base = (uint64_t)(chunk - P.start[t]) * kNormChunk, n = P.n[t];
+        const uint32_t t = tensor_of(P.start, chunk);
+        const G *const pg = static_cast<const G *>(P.tensor[t].g);
+        const uint64_t base = (uint64_t)(chunk - P.start[t]) * kNormChunk, n = P.tensor[t].n;
         sum += base + kNormChunk <= n ? square_sum<G, 256, true>(pg, base, n) : square_sum<G, 256, false>(pg, base, n);
     }
     sum = workgroup_sum<256>(sum, red);
@@ -368,29 +370,33 @@ __global__ __launch_bounds__(1024) void k_gradient_norm_finish(const double *par
         norm_and_factor(sum, max_norm, out, flags);
 }
 
-// All of it in one workgroup, eight chunks at a time.
+// All of it in one workgroup, eight chunks at a time.  A lane holds the table's entry of one tensor: what a chunk needs comes
+// from there, without another wait for memory.
 template <class G>
 __global__ __launch_bounds__(1024) void k_gradient_norm_small(const NormTable P, float max_norm, float *out, uint32_t *flags)
 {
     constexpr int VEC = (int)kNormChunk / 1024;
+    constexpr uint32_t kAtOnce = 8;
     __shared__ double red[16];
-    const uint32_t chunks = P.start[P.count];
-    uint32_t t = 0;
+    const uint32_t lane = threadIdx.x % 64u, begin = P.start[lane], chunks = P.chunks;
+    const uint64_t where = reinterpret_cast<uint64_t>(P.tensor[lane].g), size = P.tensor[lane].n;
+    const auto of = [](uint32_t x, uint32_t t) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)t); };
+    const auto of64 = [&](uint64_t x, uint32_t t) { return (uint64_t)of((uint32_t)(x >> 32), t) << 32 | of((uint32_t)x, t); };
     double sum = 0.0;
-    for (uint32_t first = 0; first < chunks; first += 8u) {
-        float g[8][VEC];
+    for (uint32_t first = 0; first < chunks; first += kAtOnce) {
+        float g[kAtOnce][VEC];
 #pragma unroll
-        for (uint32_t k = 0; k < 8u; ++k) {
-            const uint32_t chunk = first + k < chunks ? first + k : chunks - 1u;
-            while (chunk >= P.start[t + 1u])
-                ++t;
-            const uint64_t i = (uint64_t)(chunk - P.start[t]) * kNormChunk + threadIdx.x * VEC;
-            load_some<VEC>(g[k], static_cast<const G *>(P.g[t]) + i, first + k < chunks ? (int64_t)P.n[t] - (int64_t)i : 0);
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t chunk = min(first + k, chunks - 1u);
+            const uint32_t t = (uint32_t)__popcll(__ballot(begin <= chunk)) - 1u;
+            const uint64_t i = (uint64_t)(chunk - of(begin, t)) * kNormChunk + threadIdx.x * VEC;
+            load_some<VEC>(g[k], reinterpret_cast<const G *>(of64(where, t)) + i,
+                           first + k < chunks ? (int64_t)of64(size, t) - (int64_t)i : 0);
         }
 #pragma unroll
-        for (uint32_t k = 0; k < 8u; ++k)
+        for (uint32_t k = 0; k < kAtOnce; ++k)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
+            for (int e = 0; e < VEC && first + k < chunks; ++e)
                 sum = __builtin_fma((double)g[k][e], (double)g[k][e], sum);
     }
     sum = workgroup_sum<1024>(sum, red);

@@ -209,14 +209,18 @@ struct LayerNormBackward {
     uint32_t hidden;
 };
 
+// Threads of a workgroup: more than one team shares what is written of the sums.
+template <int TEAM>
+constexpr int kBackwardWG = 512 % TEAM == 0 ? 512 : TEAM;
+
 // A team takes rows in turn, as in the forward pass, and keeps the sums of its columns in registers.  Workgroup p writes
 // partial[p].
 template <class T, class W, int TEAM, int E, int VEC, bool kSums>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward(const LayerNormBackward P)
+__global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const LayerNormBackward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
-    constexpr int NV = Shape::NV, WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM, WAVES = WG / 64;
-    constexpr bool kAhead = TEAM < 1024;                     // (sixteen waves leave too few registers for a row ahead)
+    constexpr int NV = Shape::NV, WG = kBackwardWG<TEAM>, TEAMS = WG / TEAM, WAVES = WG / 64, TEAM_WAVES = TEAM < 64 ? 1 : TEAM / 64;
+    constexpr bool kAhead = TEAM < 768 && E <= 16;           // (more leave too few registers for a row ahead)
     __shared__ float red[2][2][WAVES];
     const uint32_t hidden = P.hidden;
     const Shape S(hidden);
@@ -240,10 +244,17 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward
         load();
     if (weight)
         S.load(ws, weight);
-    while (row < P.rows) {
-        if (!kAhead)
-            load();
+    // (teams of several waves meet at a barrier in every row: a workgroup's teams take equally many turns)
+    for (uint64_t first = (uint64_t)blockIdx.x * TEAMS; first < P.rows; first += (uint64_t)gridDim.x * TEAMS) {
         const uint64_t now = row;
+        if (TEAM <= 64 && now >= P.rows)
+            break;
+        if (!kAhead && now < P.rows)
+            load();
+        if (TEAM > 64 && now >= P.rows) {                    // (only the barrier is left to meet)
+            __syncthreads();
+            break;
+        }
         const float scale = rstd;
         float n[NV][VEC], d[NV][VEC], s1 = 0.0f, s2 = 0.0f;
         Vec<T, VEC> a[NV];
@@ -279,12 +290,13 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward
                 red[turn][1][threadIdx.x / 64u] = s2;
             }
             __syncthreads();                                 // (two sets of sums: one barrier per row)
-            s1 = red[turn][0][0];
-            s2 = red[turn][1][0];
+            const uint32_t own = threadIdx.x / TEAM * TEAM_WAVES;
+            s1 = red[turn][0][own];
+            s2 = red[turn][1][own];
 #pragma unroll
-            for (int k = 1; k < WAVES; ++k) {
-                s1 += red[turn][0][k];
-                s2 += red[turn][1][k];
+            for (int k = 1; k < TEAM_WAVES; ++k) {
+                s1 += red[turn][0][own + k];
+                s2 += red[turn][1][own + k];
             }
             turn ^= 1u;
         }
@@ -302,8 +314,10 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward
     }
     if constexpr (kSums) {
         float *const out = P.partial + (uint64_t)blockIdx.x * 2u * hidden;
-        if constexpr (TEAM <= 64) {                          // the workgroup's teams, in a fixed order
-            __shared__ float all[WAVES][TEAM * E];
+        if constexpr (TEAMS > 1) {                           // the workgroup's teams, in a fixed order
+            constexpr int SETS = TEAM < 64 ? WAVES : TEAMS;  // (teams in one wave add up there)
+            __shared__ float all[SETS][TEAM * E];
+            const uint32_t set = threadIdx.x / (TEAM < 64 ? 64u : (uint32_t)TEAM);
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
                 if (which)
@@ -316,14 +330,14 @@ __global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_backward
 #pragma unroll
                         for (int off = TEAM; off < 64; off <<= 1)
                             sum += __shfl_xor(sum, off, 64);
-                        if (threadIdx.x % 64u < TEAM && S.counts(k, e))
-                            all[threadIdx.x / 64u][S.at[k] + e] = sum;
+                        if ((TEAM >= 64 || threadIdx.x % 64u < (uint32_t)TEAM) && S.counts(k, e))
+                            all[set][S.at[k] + e] = sum;
                     }
                 __syncthreads();
                 for (uint32_t c = threadIdx.x; c < hidden; c += WG) {
                     float sum = all[0][c];
 #pragma unroll
-                    for (int k = 1; k < WAVES; ++k)
+                    for (int k = 1; k < SETS; ++k)
                         sum += all[k][c];
                     out[which * hidden + c] = sum;
                 }

@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <iterator>
 #include <type_traits>
 
 #include "nuq_host.hpp"
@@ -71,6 +72,7 @@ struct AdamwCall {
     }
     float keep(uint32_t i) const { return decay ? (float)(1.0 - alpha * (double)decay[i]) : 1.0f; }
     const void *g_at(uint32_t i, uint64_t e) const { return static_cast<const char *>(g[i]) + e * width(g_type); }
+    void *copy_at(uint32_t i, uint64_t e) const { return copy ? static_cast<char *>(copy[i]) + e * 2u : nullptr; }
 
     // Whether tensor j's elements follow those of tensor i, whose run is `before` elements long, in the arrays all steps have.
     bool follows(float *const *w, uint32_t i, uint32_t j, uint64_t before) const
@@ -96,8 +98,9 @@ struct AdamwCall {
     }
 };
 
-// Chunks whose norm one workgroup takes in a launch of its own, where two launches cost more than what they win.
-constexpr uint32_t kSmallChunks = 32;
+// Chunks whose norm one workgroup takes in a launch of its own: 4.2 us up to 8 of them, 6.7 at 16, 11 at 25, where two launches take
+// 6.8 alone and 10 in a step that waits for them.
+constexpr uint32_t kSmallChunks = 24;
 
 // Walks the tensors of a call, joined where one follows another, and fills tables of at most kMost of them: put(slot, tensor,
 // elements) for each, launch(tensors, chunks) for each table.  Runs are cut so that a launch has at most 2^30 chunks.
@@ -157,7 +160,7 @@ int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint3
     double *const partial = static_cast<double *>(workspace);
     // the launches share the partials
     uint32_t launches = 0, only = 0;
-    (void)for_tables<kNormTensors>(T, n, kNormChunk, follows, [](auto...) {}, [&](uint32_t, uint32_t chunks) {
+    (void)for_tables<kTableTensors>(T, n, kNormChunk, follows, [](auto...) {}, [&](uint32_t, uint32_t chunks) {
         ++launches;
         only = chunks;
         return (int)NUQ_OK;
@@ -167,16 +170,15 @@ int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint3
         return NUQ_EINVAL;
     const uint32_t most = launches ? kNormPartials / launches : 0u;
     uint32_t used = 0;
-    const int rc = for_tables<kNormTensors>(
+    const int rc = for_tables<kTableTensors>(
         T, n, kNormChunk, follows,
         [&](uint32_t slot, uint32_t i, uint64_t at, uint64_t take, uint32_t start) {
-            P.g[slot] = static_cast<const char *>(g[i]) + at * w;
-            P.n[slot] = take;
+            P.tensor[slot] = {static_cast<const char *>(g[i]) + at * w, take};
             P.start[slot] = start;
         },
         [&](uint32_t slots, uint32_t chunks) {
-            P.start[slots] = chunks;
-            P.count = slots;
+            std::fill(P.start + slots, std::end(P.start), ~0u);
+            P.chunks = chunks;
             if (small)
                 return with_type(type, [&](auto t) {
                     hipLaunchKernelGGL(k_gradient_norm_small<typename decltype(t)::type>, dim3(1), dim3(1024), 0, st, P, max_norm,
@@ -220,17 +222,11 @@ int nuq_adamw_step(uint32_t T, float *const *w, const void *const *g, float *con
             return C.follows(w, i, j, before) && m[j] == m[i] + before && v[j] == v[i] + before;
         },
         [&](uint32_t slot, uint32_t i, uint64_t at, uint64_t take, uint32_t start) {
-            P.w[slot] = w[i] + at;
-            P.m[slot] = m[i] + at;
-            P.v[slot] = v[i] + at;
-            P.g[slot] = C.g_at(i, at);
-            P.copy[slot] = copy ? static_cast<char *>(copy[i]) + at * 2u : nullptr;
-            P.n[slot] = take;
-            P.keep[slot] = C.keep(i);
+            P.tensor[slot] = {w[i] + at, m[i] + at, v[i] + at, C.g_at(i, at), C.copy_at(i, at), take, C.keep(i)};
             P.start[slot] = start;
         },
         [&](uint32_t slots, uint32_t chunks) {
-            P.count = slots;
+            std::fill(P.start + slots, std::end(P.start), ~0u);
             return C.with_types(12, [&](auto gt, auto ct, auto has, auto once) {
                 hipLaunchKernelGGL((k_adamw<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value,
                                             decltype(once)::value>), dim3(chunks), dim3(256), 0, st, P);
@@ -266,18 +262,12 @@ int nuq_adamw_step_coded(uint32_t T, float *const *w, const void *const *g, uint
                    v[j] == v[i] + before && scales[j] == scales[i] + 2u * (before / NUQ_STATE_BLOCK);
         },
         [&](uint32_t slot, uint32_t i, uint64_t at, uint64_t take, uint32_t start) {     // (`at`: whole chunks)
-            P.w[slot] = w[i] + at;
-            P.m[slot] = m[i] + at;
-            P.v[slot] = v[i] + at;
-            P.scales[slot] = scales[i] + 2u * (at / NUQ_STATE_BLOCK);
-            P.g[slot] = C.g_at(i, at);
-            P.copy[slot] = copy ? static_cast<char *>(copy[i]) + at * 2u : nullptr;
-            P.n[slot] = take;
-            P.keep[slot] = C.keep(i);
+            P.tensor[slot] = {w[i] + at, scales[i] + 2u * (at / NUQ_STATE_BLOCK), m[i] + at, v[i] + at, C.g_at(i, at),
+                              C.copy_at(i, at), take, C.keep(i)};
             P.start[slot] = start;
         },
         [&](uint32_t slots, uint32_t chunks) {
-            P.count = slots;
+            std::fill(P.start + slots, std::end(P.start), ~0u);
             return C.with_types(6, [&](auto gt, auto ct, auto has, auto once) {
                 hipLaunchKernelGGL((k_adamw_coded<typename decltype(gt)::type, typename decltype(ct)::type, decltype(has)::value,
                                                   decltype(once)::value>), dim3(chunks), dim3(256), 0, st, P);
@@ -309,7 +299,7 @@ namespace {
 
 // The team of threads, the elements per thread and the vectors that hold a row of `hidden` elements of type T: f(team, elements,
 // vector), or f(0, 0, 0) where nothing does.
-template <class T, class F>
+template <class T, bool kBackward, class F>
 int with_row_shape(uint32_t hidden, F &&f)
 {
     using std::integral_constant;
@@ -327,8 +317,13 @@ int with_row_shape(uint32_t hidden, F &&f)
     NUQ_SHAPE(256, 8)
     NUQ_SHAPE(256, 16)
     NUQ_SHAPE(512, 16)
-    NUQ_SHAPE(768, 16)
-    NUQ_SHAPE(1024, 16)
+    if constexpr (kBackward) {
+        NUQ_SHAPE(768, 16)
+        NUQ_SHAPE(512, 32)
+    } else {
+        NUQ_SHAPE(512, 24)
+        NUQ_SHAPE(1024, 16)
+    }
 #undef NUQ_SHAPE
     return f(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 0>{});
 }
@@ -363,7 +358,7 @@ int with_types(uint32_t type, uint32_t weight_type, F &&f)
 
 bool valid_rows(uint64_t rows, uint32_t hidden, uint32_t type, uint32_t weight_type, const void *weight)
 {
-    return hidden >= 1 && hidden <= 1u << 30 && rows <= 1ull << 31 && type <= NUQ_F16 &&
+    return hidden >= 1 && hidden <= 1u << 30 && rows < 1ull << 31 && type <= NUQ_F16 &&
            (weight_type == type || weight_type == NUQ_F32) && (!weight || !off_grid(weight, width(weight_type)));
 }
 
@@ -393,7 +388,7 @@ int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, ui
     return with_types(type, weight_type, [&](auto tt, auto wt) {
         using T = typename decltype(tt)::type;
         using W = typename decltype(wt)::type;
-        return with_row_shape<T>(hidden, [&](auto team, auto elements, auto vec) {
+        return with_row_shape<T, false>(hidden, [&](auto team, auto elements, auto vec) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
             const auto run = [&](auto stream_c) {
                 constexpr bool kStream = decltype(stream_c)::value;
@@ -441,7 +436,7 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
         using T = typename decltype(tt)::type;
         using W = typename decltype(wt)::type;
         uint32_t parts = 0;
-        const int rc = rows == 0 ? (int)NUQ_OK : with_row_shape<T>(hidden, [&](auto team, auto elements, auto vec) {
+        const int rc = rows == 0 ? (int)NUQ_OK : with_row_shape<T, true>(hidden, [&](auto team, auto elements, auto vec) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
             if constexpr (TEAM == 0) {
                 parts = (uint32_t)std::min<uint64_t>(rows, kLongParts);
@@ -450,7 +445,7 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
                 hipLaunchKernelGGL((k_layer_norm_backward_long<T, W>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
                 return check_launch();
             } else {
-                constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
+                constexpr uint32_t WG = kBackwardWG<TEAM>, TEAMS = WG / TEAM;
                 const auto run = [&](auto sums_c) {
                     constexpr bool kSums = decltype(sums_c)::value;
                     const uint32_t most = resident_workgroups<k_layer_norm_backward<T, W, TEAM, E, VEC, kSums>>(WG);

@@ -125,12 +125,13 @@ __device__ __forceinline__ double workgroup_sum(double x, double *red)
 // arguments.
 constexpr uint32_t kTableTensors = 64;
 
-// start[i]: the first chunk of tensor i, start[0] = 0.  The tensor that `chunk` belongs to, the same in every lane.
-__device__ __forceinline__ uint32_t tensor_of(const uint32_t *start, uint32_t count, uint32_t chunk)
+// start[i]: the first chunk of tensor i, 2^32 - 1 where there is none.  The tensor that `chunk` belongs to: one load for all.
+template <uint32_t kTensors>
+__device__ __forceinline__ uint32_t tensor_of(const uint32_t (&start)[kTensors], uint32_t chunk)
 {
-    const uint32_t lane = threadIdx.x % 64u;
-    const bool begun = lane < count && start[lane < count ? lane : 0u] <= chunk;
-    return (uint32_t)__popcll(__ballot(begun)) - 1u;
+    static_assert(kTensors <= 64, "a tensor per lane");
+    const uint32_t lane = threadIdx.x % 64u, begin = lane < kTensors ? start[lane] : ~0u;
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)__popcll(__ballot(begin <= chunk)) - 1);
 }
 
 }  // namespace nuq

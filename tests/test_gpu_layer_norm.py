@@ -195,6 +195,15 @@ def test_results_may_stand_where_the_rows_stood(nuq):
         assert all(torch.equal(a, b) for a, b in zip(*out))
         nuq.nuq_layer_norm_forward(x, None, None, None, 1e-5, None, x, None, None)
         assert torch.equal(x, y)
+        for at in (0, 1):                                    # the sum in the place of either
+            r = rows_of(9, hidden, BF16, gen)
+            s = (y.float() + r.float()).bfloat16()
+            both = [y.clone(), r]
+            out = torch.empty_like(y)
+            nuq.nuq_layer_norm_forward(both[0], both[1], None, None, 1e-5, both[at], out, None, None)
+            want = torch.empty_like(y)
+            nuq.nuq_layer_norm_forward(s, None, None, None, 1e-5, None, want, None, None)
+            assert torch.equal(both[at], s) and torch.equal(out, want)
 
 
 def test_offsets_beyond_32_bits(nuq):

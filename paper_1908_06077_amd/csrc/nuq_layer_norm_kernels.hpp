@@ -79,11 +79,14 @@ __device__ __forceinline__ float row_sum(float x, float *red)
 }
 
 // A team takes rows in turn; the next row is on its way while one is worked on, weight and bias stay in registers.
+template <int TEAM>
+constexpr int kForwardWG = TEAM <= 64 ? 256 : TEAM;
+
 template <class T, class W, int TEAM, int E, int VEC, bool kStream>
-__global__ __launch_bounds__(TEAM < 256 ? 256 : TEAM) void k_layer_norm_forward(const LayerNormForward P)
+__global__ __launch_bounds__(kForwardWG<TEAM>) void k_layer_norm_forward(const LayerNormForward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
-    constexpr int NV = Shape::NV, TEAMS = TEAM < 256 ? 256 / TEAM : 1;
+    constexpr int NV = Shape::NV, TEAMS = kForwardWG<TEAM> / TEAM;
     __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
     const uint32_t hidden = P.hidden;
     const Shape S(hidden);
@@ -211,7 +214,7 @@ struct LayerNormBackward {
 
 // Threads of a workgroup: more than one team shares what is written of the sums.
 template <int TEAM>
-constexpr int kBackwardWG = 512 % TEAM == 0 ? 512 : TEAM;
+constexpr int kBackwardWG = TEAM < 512 ? 512 / TEAM * TEAM : TEAM;
 
 // A team takes rows in turn, as in the forward pass, and keeps the sums of its columns in registers.  Workgroup p writes
 // partial[p].
@@ -220,13 +223,23 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
     constexpr int NV = Shape::NV, WG = kBackwardWG<TEAM>, TEAMS = WG / TEAM, WAVES = WG / 64, TEAM_WAVES = TEAM < 64 ? 1 : TEAM / 64;
-    constexpr bool kAhead = TEAM < 768 && E <= 16;           // (more leave too few registers for a row ahead)
+    constexpr bool kAhead = TEAM < 1024;                     // (sixteen waves leave too few registers for a row ahead,
+    constexpr bool kInLds = kSums && TEAM >= 768;            //  and twelve for the sums too: these stand in LDS then)
+    __shared__ __align__(16) float kept[kInLds ? 2 * TEAM * E : 1];
     __shared__ float red[2][2][WAVES];
     const uint32_t hidden = P.hidden;
     const Shape S(hidden);
     const W *const weight = static_cast<const W *>(P.weight);
     const float per = 1.0f / (float)hidden;
     float dw[NV][VEC] = {}, db[NV][VEC] = {};
+    // a thread's own places in LDS
+    const auto kept_at = [&](int which, int k) { return kept + ((which * NV + k) * TEAM + (int)(threadIdx.x % TEAM)) * VEC; };
+    if constexpr (kInLds)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            store_from_float<VEC>(kept_at(0, k), dw[k]);
+            store_from_float<VEC>(kept_at(1, k), db[k]);
+        }
     uint32_t turn = 0;
     Vec<T, VEC> xs[NV], gs[NV], as[NV];
     Vec<W, VEC> ws[NV];
@@ -261,6 +274,10 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             a[k] = as[k];
+            if constexpr (kInLds) {
+                load_as_float<VEC>(dw[k], kept_at(0, k));
+                load_as_float<VEC>(db[k], kept_at(1, k));
+            }
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 n[k][e] = ((float)xs[k][e] - mean) * rstd;
@@ -274,6 +291,10 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
                 const float c = S.counts(k, e) ? d[k][e] : 0.0f;
                 s1 += c;
                 s2 = __builtin_fmaf(c, n[k][e], s2);
+            }
+            if constexpr (kInLds) {
+                store_from_float<VEC>(kept_at(0, k), dw[k]);
+                store_from_float<VEC>(kept_at(1, k), db[k]);
             }
         }
         row += (uint64_t)gridDim.x * TEAMS;
@@ -313,6 +334,12 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
         S.store(static_cast<T *>(P.dx) + now * P.ldd, d);
     }
     if constexpr (kSums) {
+        if constexpr (kInLds)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                load_as_float<VEC>(dw[k], kept_at(0, k));
+                load_as_float<VEC>(db[k], kept_at(1, k));
+            }
         float *const out = P.partial + (uint64_t)blockIdx.x * 2u * hidden;
         if constexpr (TEAMS > 1) {                           // the workgroup's teams, in a fixed order
             constexpr int SETS = TEAM < 64 ? WAVES : TEAMS;  // (teams in one wave add up there)

@@ -312,18 +312,20 @@ int with_row_shape(uint32_t hidden, F &&f)
     NUQ_SHAPE(4, 8)
     NUQ_SHAPE(16, 8)
     NUQ_SHAPE(16, 16)
-    NUQ_SHAPE(64, 8)
+    NUQ_SHAPE(32, 16)
     NUQ_SHAPE(64, 16)
-    NUQ_SHAPE(256, 8)
-    NUQ_SHAPE(256, 16)
-    NUQ_SHAPE(512, 16)
     if constexpr (kBackward) {
+        NUQ_SHAPE(256, 8)
+        NUQ_SHAPE(256, 16)
+        NUQ_SHAPE(512, 16)
         NUQ_SHAPE(768, 16)
-        NUQ_SHAPE(512, 32)
     } else {
+        NUQ_SHAPE(128, 16)
+        NUQ_SHAPE(256, 16)
+        NUQ_SHAPE(512, 16)
         NUQ_SHAPE(512, 24)
-        NUQ_SHAPE(1024, 16)
     }
+    NUQ_SHAPE(1024, 16)
 #undef NUQ_SHAPE
     return f(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 0>{});
 }
@@ -395,7 +397,7 @@ int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, ui
                 if constexpr (TEAM == 0) {
                     hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, kStream>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
                 } else {
-                    constexpr uint32_t WG = TEAM < 256 ? 256 : TEAM, TEAMS = WG / TEAM;
+                    constexpr uint32_t WG = kForwardWG<TEAM>, TEAMS = WG / TEAM;
                     const uint32_t most = resident_workgroups<k_layer_norm_forward<T, W, TEAM, E, VEC, kStream>>(WG);
                     if (!most)
                         return (int)NUQ_EHIP;

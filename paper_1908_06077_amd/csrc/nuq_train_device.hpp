@@ -79,16 +79,17 @@ __device__ __forceinline__ float dpp_move(float x)
 template <int TEAM>
 __device__ __forceinline__ float team_sum(float x)
 {
-    static_assert(TEAM == 4 || TEAM == 16 || TEAM == 64, "team");
+    static_assert(TEAM == 4 || TEAM == 16 || TEAM == 32 || TEAM == 64, "team");
     x += dpp_move<0xB1>(x);             // lane ^ 1
     x += dpp_move<0x4E>(x);             // lane ^ 2
     if constexpr (TEAM >= 16) {
         x += dpp_move<0x141>(x);        // 7 - lane of each eight
         x += dpp_move<0x140>(x);        // 15 - lane of each sixteen
     }
-    if constexpr (TEAM == 64) {
-        x += __shfl_xor(x, 16, 64);
-        x += __shfl_xor(x, 32, 64);
+    if constexpr (TEAM >= 32) {         // the sums of sixteen, read out of one lane of each
+        const auto of = [&](int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane)); };
+        const float low = of(0) + of(16), high = of(32) + of(48);
+        x = TEAM == 64 ? low + high : threadIdx.x % 64u < 32u ? low : high;
     }
     return x;
 }

@@ -303,7 +303,7 @@ struct NormTable {
     double *partial;
 };
 
-template <class G, int WG, bool kWhole>
+template <class G, int WG, bool kOnce, bool kWhole>
 __device__ __forceinline__ double square_sum(const G *pg, uint64_t base, uint64_t n)
 {
     constexpr int VEC = 16 / sizeof(G), ROWS = (int)kNormChunk / (WG * VEC);
@@ -311,7 +311,7 @@ __device__ __forceinline__ double square_sum(const G *pg, uint64_t base, uint64_
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const uint64_t i = base + (uint64_t)(r * WG + (int)threadIdx.x) * VEC;
-        load_some<VEC, kWhole>(g[r], pg + i, (int64_t)n - (int64_t)i);
+        load_some<VEC, kWhole, kOnce>(g[r], pg + i, (int64_t)n - (int64_t)i);
     }
     double sum = 0.0;
 #pragma unroll
@@ -322,8 +322,9 @@ __device__ __forceinline__ double square_sum(const G *pg, uint64_t base, uint64_
     return sum;
 }
 
-// Workgroup p takes the p-th share of the chunks and writes partial[p].
-template <class G>
+// Workgroup p takes the p-th share of the chunks and writes partial[p].  kOnce: the gradients are larger than the last-level
+// cache; smaller ones are left there for the step that follows.
+template <class G, bool kOnce>
 __global__ __launch_bounds__(256) void k_gradient_norm(const NormTable P)
 {
     __shared__ double red[4];
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(256) void k_gradient_norm(const NormTable P)
         const uint32_t t = tensor_of(P.start, chunk);
         const G *const pg = static_cast<const G *>(P.tensor[t].g);
         const uint64_t base = (uint64_t)(chunk - P.start[t]) * kNormChunk, n = P.tensor[t].n;
-        sum += base + kNormChunk <= n ? square_sum<G, 256, true>(pg, base, n) : square_sum<G, 256, false>(pg, base, n);
+        sum += base + kNormChunk <= n ? square_sum<G, 256, kOnce, true>(pg, base, n) : square_sum<G, 256, kOnce, false>(pg, base, n);
     }
     sum = workgroup_sum<256>(sum, red);
     if (threadIdx.x == 0)

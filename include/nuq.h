@@ -448,7 +448,8 @@ int nuq_adamw_step(uint32_t T, float *const *w, const void *const *g, float *con
  *     float(bits k << 20) * 2^96 * e; stored is the code k whose float(bits k << 20), which may be
  *     subnormal, is nearest to v * (1/e) * 2^-96, at least 1 where v > 0;
  * nearest with ties to even, each product and quotient rounded to fp32.  The largest element of a block
- * is held exactly.  All zeros (codes and scales) is the state before step 1.  The step uses the new m and
+ * is held exactly; what an element changes against it by less than half a step of its code in one step is
+ * lost.  All zeros (codes and scales) is the state before step 1.  The step uses the new m and
  * v before they are rounded to codes.  A block with a new m or v that is not finite keeps w, codes and
  * scales (its copy is still written) and raises NUQ_FLAG_NONFINITE.  Other arguments and errors as above. */
 #define NUQ_STATE_BLOCK 256u

@@ -6,6 +6,13 @@
 //
 // A row stays in the registers of one team of threads between its statistics and its result: read once, written once.  The
 // variance is taken of the centred values.  Statistics and sums are fp32, results are rounded to their type once.
+//
+// Bound by HBM (counted: 1.00 to 1.01 times the bytes of the rows, and the partial sums), and on rows of a few KiB by latency:
+// what a CU has in flight.  So teams are small (a wave has a row of 1024 elements, no barrier), at most sixteen elements per
+// thread keep the registers low enough for several teams per CU, a team stays for many rows with the next one's loads issued
+// before the present one's sums, and weight and bias are read once: read per row, 12.8 KB of them for each 3.2 KB row of 1600
+// in bfloat16, they took the L1 7 us of a 26 us pass.  Plain accesses: with non-temporal stores the pass on 8192 x 1600 takes
+// 18 us instead of 21.6, but an operation that reads both results behind it 19 instead of 13.
 #pragma once
 
 #include "nuq_train_device.hpp"
@@ -78,10 +85,13 @@ __device__ __forceinline__ float row_sum(float x, float *red)
     }
 }
 
-// A team takes rows in turn; the next row is on its way while one is worked on, weight and bias stay in registers.
+// Threads of a workgroup: teams of more than a wave meet at barriers and have it alone.
 template <int TEAM>
 constexpr int kForwardWG = TEAM <= 64 ? 256 : TEAM;
 
+// A team takes rows in turn; the next row is on its way while one is worked on, weight and bias stay in registers.  8192 x 1600 in
+// bfloat16 with the residual 21 us (5.0 TB/s, of which 2 us are the launch), 8192 x 12288 in float32 142 us (5.7 TB/s), one row
+// 2.1 us (a launch); one row per workgroup instead: 26.5 and 152 us.
 template <class T, class W, int TEAM, int E, int VEC, bool kStream>
 __global__ __launch_bounds__(kForwardWG<TEAM>) void k_layer_norm_forward(const LayerNormForward P)
 {
@@ -217,7 +227,9 @@ template <int TEAM>
 constexpr int kBackwardWG = TEAM < 512 ? 512 / TEAM * TEAM : TEAM;
 
 // A team takes rows in turn, as in the forward pass, and keeps the sums of its columns in registers.  Workgroup p writes
-// partial[p].
+// partial[p], 8 bytes per column; a second launch (4 to 7 us) adds the workgroups up.  8192 x 1600 in bfloat16 with a gradient to
+// add 23 us (4.9 TB/s with the partial sums), 32768 x 8192 282 us (5.8 TB/s); 4.6 TB/s at 1000 columns, 3.5 at 16384, where one
+// workgroup fills a CU.  512 workgroups: with 256 the 1600 columns take 1 us more, with 1024 2 us.
 template <class T, class W, int TEAM, int E, int VEC, bool kSums>
 __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const LayerNormBackward P)
 {

@@ -222,19 +222,21 @@ struct LayerNormBackward {
     uint32_t hidden;
 };
 
-// Threads of a workgroup: more than one team shares what is written of the sums.
-template <int TEAM>
-constexpr int kBackwardWG = TEAM < 512 ? 512 / TEAM * TEAM : TEAM;
+// Threads of a workgroup: more than one team shares what is written of the sums.  Eight elements per thread leave registers for
+// sixteen waves (8192 x 1600 in bfloat16 25.7 us, 26.6 with two workgroups of eight), sixteen for eight (twelve were 4 % slower).
+template <int TEAM, int E>
+constexpr int kBackwardWG = TEAM < 512 ? (E <= 8 ? 1024 : 512) : TEAM;
 
 // A team takes rows in turn, as in the forward pass, and keeps the sums of its columns in registers.  Workgroup p writes
 // partial[p], 8 bytes per column; a second launch (4 to 7 us) adds the workgroups up.  8192 x 1600 in bfloat16 with a gradient to
-// add 23 us (4.9 TB/s with the partial sums), 32768 x 8192 282 us (5.8 TB/s); 4.6 TB/s at 1000 columns, 3.5 at 16384, where one
-// workgroup fills a CU.  512 workgroups: with 256 the 1600 columns take 1 us more, with 1024 2 us.
+// add 22 us (5 TB/s with the partial sums), 32768 x 8192 282 us (5.8 TB/s); 4.8 TB/s at 1000 columns, 3.4 at 16384, where one
+// workgroup fills a CU.  With sixteen elements per thread the sums and operands take 160 registers, so that a CU has eight waves;
+// held to 128 they spill, and the pass takes twice as long; in LDS the sums cost 10 % (but win above 8192 columns).
 template <class T, class W, int TEAM, int E, int VEC, bool kSums>
-__global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const LayerNormBackward P)
+__global__ __launch_bounds__((kBackwardWG<TEAM, E>)) void k_layer_norm_backward(const LayerNormBackward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
-    constexpr int NV = Shape::NV, WG = kBackwardWG<TEAM>, TEAMS = WG / TEAM, WAVES = WG / 64, TEAM_WAVES = TEAM < 64 ? 1 : TEAM / 64;
+    constexpr int NV = Shape::NV, WG = kBackwardWG<TEAM, E>, TEAMS = WG / TEAM, WAVES = WG / 64, TEAM_WAVES = TEAM < 64 ? 1 : TEAM / 64;
     constexpr bool kAhead = TEAM < 1024;                     // (sixteen waves leave too few registers for a row ahead,
     constexpr bool kInLds = kSums && TEAM >= 768;            //  and twelve for the sums too: these stand in LDS then)
     __shared__ __align__(16) float kept[kInLds ? 2 * TEAM * E : 1];
@@ -262,11 +264,15 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
         rstd = P.rstd[row];
         S.load(gs, static_cast<const T *>(P.dy) + row * P.ldg);
         S.load(xs, static_cast<const T *>(P.x) + row * P.ldx);
-        if (P.add)
-            S.load(as, static_cast<const T *>(P.add) + row * P.lda);
     };
-    if (kAhead && row < P.rows)
+    const auto load_add = [&](uint64_t of) {                 // (used last in a row, so asked for when the last one is used)
+        if (P.add)
+            S.load(as, static_cast<const T *>(P.add) + of * P.lda);
+    };
+    if (kAhead && row < P.rows) {
         load();
+        load_add(row);
+    }
     if (weight)
         S.load(ws, weight);
     // (teams of several waves meet at a barrier in every row: a workgroup's teams take equally many turns)
@@ -282,10 +288,8 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
         }
         const float scale = rstd;
         float n[NV][VEC], d[NV][VEC], s1 = 0.0f, s2 = 0.0f;
-        Vec<T, VEC> a[NV];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            a[k] = as[k];
             if constexpr (kInLds) {
                 load_as_float<VEC>(dw[k], kept_at(0, k));
                 load_as_float<VEC>(db[k], kept_at(1, k));
@@ -312,6 +316,8 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
         row += (uint64_t)gridDim.x * TEAMS;
         if (kAhead && row < P.rows)
             load();
+        if (!kAhead)
+            load_add(now);
         if constexpr (TEAM <= 64) {
             s1 = team_sum<TEAM>(s1);
             s2 = team_sum<TEAM>(s2);
@@ -341,8 +347,10 @@ __global__ __launch_bounds__(kBackwardWG<TEAM>) void k_layer_norm_backward(const
             for (int e = 0; e < VEC; ++e) {
                 d[k][e] = (d[k][e] - s1 - n[k][e] * s2) * scale;
                 if (P.add)
-                    d[k][e] += (float)a[k][e];
+                    d[k][e] += (float)as[k][e];
             }
+        if (kAhead && row < P.rows)
+            load_add(row);
         S.store(static_cast<T *>(P.dx) + now * P.ldd, d);
     }
     if constexpr (kSums) {

@@ -306,11 +306,14 @@ int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const
 namespace {
 
 // The team of threads, the elements per thread and the vectors that hold a row of `hidden` elements of type T: f(team, elements,
-// vector), or f(0, 0, 0) where nothing does.  Forward and backward pass differ where registers do: between 1025 and 2048 columns
-// a forward team of 128 threads (20971 x 1600 in bfloat16 28.6 us, 32.1 with 256 threads of eight elements; the backward pass
-// gains nothing), up to 12288 columns one of 512 with 24 elements (40.8 us on 4096 rows, 44.0 with 768 of sixteen) against 768
-// of sixteen, whose sums stand in LDS.  Teams of 192 and 384 threads between were tried: 5 % less at 1300 columns, 10 % more at
-// 2500 and 5000.
+// vector), or f(0, 0, 0) where nothing does.  Forward and backward pass differ where registers do:
+//   513 to 1024 columns in float32: a backward team of 128 (33554 x 1000 with a gradient to add 105 us, 113 with a wave; in 16
+//     bits a wave, 3 % faster);
+//   1025 to 2048: a forward team of 128 (20971 x 1600 in bfloat16 28.6 us, 32.1 with 256 threads of eight elements; the backward
+//     pass gains nothing);
+//   8193 to 12288: forward 512 threads of 24 elements (40.8 us on 4096 rows in bfloat16, 44.0 with 768 of sixteen), backward 768
+//     of sixteen, whose sums stand in LDS.
+// Teams of 192 and 384 threads between were tried: 5 % less at 1300 columns, 10 % more at 2500 and 5000.
 template <class T, bool kBackward, class F>
 int with_row_shape(uint32_t hidden, F &&f)
 {
@@ -325,6 +328,8 @@ int with_row_shape(uint32_t hidden, F &&f)
     NUQ_SHAPE(16, 8)
     NUQ_SHAPE(16, 16)
     NUQ_SHAPE(32, 16)
+    if constexpr (kBackward && VEC == 4)
+        NUQ_SHAPE(128, 8)
     NUQ_SHAPE(64, 16)
     if constexpr (kBackward) {
         NUQ_SHAPE(256, 8)
@@ -462,7 +467,7 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
                 hipLaunchKernelGGL((k_layer_norm_backward_long<T, W>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
                 return check_launch();
             } else {
-                constexpr uint32_t WG = kBackwardWG<TEAM>, TEAMS = WG / TEAM;
+                constexpr uint32_t WG = kBackwardWG<TEAM, E>, TEAMS = WG / TEAM;
                 const auto run = [&](auto sums_c) {
                     constexpr bool kSums = decltype(sums_c)::value;
                     const uint32_t most = resident_workgroups<k_layer_norm_backward<T, W, TEAM, E, VEC, kSums>>(WG);

@@ -699,6 +699,10 @@ def nuq_adamw_step_coded(ws, grads, ms, vs, scales, decays, alpha: float, beta1:
 
 def nuq_adamw_state_values(m_codes: torch.Tensor, v_codes: torch.Tensor, scales: torch.Tensor, m: torch.Tensor,
                            v: torch.Tensor) -> None:
+    """m, v <- the values that the codes of one tensor (or of several, each padded to whole blocks) stand for, fp32."""
+    code = _calls.adamw_state_values(m_codes, v_codes, scales, m, v)
+    if code is not None:
+        return _check("nuq_adamw_state_values", code)
     n = m_codes.numel()
     if v_codes.numel() != n or m.numel() != n or v.numel() != n:
         raise ValueError("codes and values of one length are needed")

@@ -33,7 +33,7 @@ PyObject *g_norms, *g_bit_off, *g_words, *g_sync;                   // attribute
     X(nuq_quantize_pack_fixed_table_batch) X(nuq_unpack_accumulate_fixed_table)                                      \
     X(nuq_quantize_encode_huffman_batch) X(nuq_decode_accumulate_huffman) X(nuq_moments_accumulate)                  \
     X(nuq_gradient_norm) X(nuq_adamw_step) X(nuq_adamw_step_coded) X(nuq_state_blocks) X(nuq_layer_norm_forward)     \
-    X(nuq_layer_norm_backward)
+    X(nuq_layer_norm_backward) X(nuq_adamw_state_values)
 #define NUQ_POINTER(name) decltype(&::name) p_##name = nullptr;
 NUQ_CALLS(NUQ_POINTER)
 
@@ -494,6 +494,14 @@ PyObject *adamw_step_coded(PyObject *const *a)           // ws, grads, ms, vs, s
                   S.beta2, S.eps, S.t, S.c);
 }
 
+PyObject *adamw_state_values(PyObject *const *a)         // m_codes, v_codes, scales, m, v
+{
+    uint64_t n;
+    const uint8_t *m = address<const uint8_t>(a[0], at::kFloat8_e4m3fn, 0, &n), *v = exactly<const uint8_t>(a[1], at::kByte, n);
+    const float *scales = address<const float>(a[2], at::kFloat, 2u * p_nuq_state_blocks(n));
+    return launch(p_nuq_adamw_state_values, m, v, scales, n, exactly<float>(a[3], at::kFloat, n), exactly<float>(a[4], at::kFloat, n));
+}
+
 // `rows` rows of `hidden` elements of one type, or none (0 rows asked: as many as there are).
 struct Rows {
     void *p = nullptr;
@@ -639,6 +647,7 @@ PyMethodDef g_methods[] = {
     NUQ_METHOD(gradient_norm, 4),
     NUQ_METHOD(adamw_step, 12),
     NUQ_METHOD(adamw_step_coded, 13),
+    NUQ_METHOD(adamw_state_values, 5),
     NUQ_METHOD(layer_norm_forward, 9),
     NUQ_METHOD(layer_norm_backward, 10),
     {nullptr, nullptr, 0, nullptr},

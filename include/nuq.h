@@ -434,7 +434,8 @@ int nuq_gradient_norm(uint32_t T, const void *const *g, const uint64_t *n, uint3
  * Evaluated in fp32, one rounding per product and sum in m and v; w within a few units of the last
  * place of the subtracted term.  An element whose new m or v would not be finite keeps w, m and v
  * (its copy is still written) and raises NUQ_FLAG_NONFINITE.
- * NUQ_EINVAL: t = 0; alpha, beta or decay not finite; beta outside [0, 1); eps below 2^-126. */
+ * NUQ_EINVAL: t = 0; beta outside [0, 1); eps below 2^-126; alpha, beta, decay, or what is made of them
+ * in fp32, not finite. */
 int nuq_adamw_step(uint32_t T, float *const *w, const void *const *g, float *const *m, float *const *v,
                    void *const *copy, const uint64_t *n, const float *decay, uint32_t g_type,
                    uint32_t copy_type, double alpha, double beta1, double beta2, double eps, uint64_t t,

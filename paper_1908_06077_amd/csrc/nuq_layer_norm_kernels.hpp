@@ -198,69 +198,70 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_forward_long(const La
 {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ float red[2][kLongRowWG / 64];
-    const uint64_t row = blockIdx.x;
-    const T *x = static_cast<const T *>(P.x) + row * P.ldx;
-    float sum = 0.0f;
-    if constexpr (kStream) {
-        const T *const res = static_cast<const T *>(P.residual) + row * P.ldr;
-        T *const total = static_cast<T *>(P.total) + row * P.ldt;
-        for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-            float s[VEC], r[VEC];
-            load_as_float<VEC>(s, x + at);
-            load_as_float<VEC>(r, res + at);
+    for (uint64_t row = blockIdx.x; row < P.rows; row += gridDim.x) {
+        const T *x = static_cast<const T *>(P.x) + row * P.ldx;
+        float sum = 0.0f;
+        if constexpr (kStream) {
+            const T *const res = static_cast<const T *>(P.residual) + row * P.ldr;
+            T *const total = static_cast<T *>(P.total) + row * P.ldt;
+            for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
+                float s[VEC], r[VEC];
+                load_as_float<VEC>(s, x + at);
+                load_as_float<VEC>(r, res + at);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                s[e] = (float)(T)(s[e] + r[e]);
-                sum += (uint32_t)e >= skip ? s[e] : 0.0f;
-            }
-            store_behind<VEC>(total + at, s, skip);          // (read again by the thread that wrote it)
-        });
-        x = total;
-    } else {
+                for (int e = 0; e < VEC; ++e) {
+                    s[e] = (float)(T)(s[e] + r[e]);
+                    sum += (uint32_t)e >= skip ? s[e] : 0.0f;
+                }
+                store_behind<VEC>(total + at, s, skip);          // (read again by the thread that wrote it)
+            });
+            x = total;
+        } else {
+            for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
+                float s[VEC];
+                load_as_float<VEC>(s, x + at);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    sum += (uint32_t)e >= skip ? s[e] : 0.0f;
+            });
+        }
+        const float mean = row_sum<kLongRowWG>(sum, red[0]) / (float)P.hidden;
+        float square = 0.0f;
         for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
             float s[VEC];
             load_as_float<VEC>(s, x + at);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                sum += (uint32_t)e >= skip ? s[e] : 0.0f;
+            for (int e = 0; e < VEC; ++e) {
+                const float d = (uint32_t)e >= skip ? s[e] - mean : 0.0f;
+                square = __builtin_fmaf(d, d, square);
+            }
+        });
+        const float rstd = 1.0f / __builtin_sqrtf(row_sum<kLongRowWG>(square, red[1]) / (float)P.hidden + P.eps);
+        if (threadIdx.x == 0) {
+            if (P.mean)
+                P.mean[row] = mean;
+            if (P.rstd)
+                P.rstd[row] = rstd;
+        }
+        T *const y = static_cast<T *>(P.y) + row * P.ldy;
+        for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
+            float n[VEC], w[VEC], b[VEC];
+            load_as_float<VEC>(n, x + at);
+            if (P.weight)
+                load_as_float<VEC>(w, static_cast<const W *>(P.weight) + at);
+            if (P.bias)
+                load_as_float<VEC>(b, static_cast<const W *>(P.bias) + at);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                n[e] = (n[e] - mean) * rstd;
+                if (P.weight)
+                    n[e] *= w[e];
+                if (P.bias)
+                    n[e] += b[e];
+            }
+            store_behind<VEC>(y + at, n, skip);
         });
     }
-    const float mean = row_sum<kLongRowWG>(sum, red[0]) / (float)P.hidden;
-    float square = 0.0f;
-    for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-        float s[VEC];
-        load_as_float<VEC>(s, x + at);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float d = (uint32_t)e >= skip ? s[e] - mean : 0.0f;
-            square = __builtin_fmaf(d, d, square);
-        }
-    });
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<kLongRowWG>(square, red[1]) / (float)P.hidden + P.eps);
-    if (threadIdx.x == 0) {
-        if (P.mean)
-            P.mean[row] = mean;
-        if (P.rstd)
-            P.rstd[row] = rstd;
-    }
-    T *const y = static_cast<T *>(P.y) + row * P.ldy;
-    for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-        float n[VEC], w[VEC], b[VEC];
-        load_as_float<VEC>(n, x + at);
-        if (P.weight)
-            load_as_float<VEC>(w, static_cast<const W *>(P.weight) + at);
-        if (P.bias)
-            load_as_float<VEC>(b, static_cast<const W *>(P.bias) + at);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            n[e] = (n[e] - mean) * rstd;
-            if (P.weight)
-                n[e] *= w[e];
-            if (P.bias)
-                n[e] += b[e];
-        }
-        store_behind<VEC>(y + at, n, skip);
-    });
 }
 
 struct LayerNormBackward {
@@ -451,50 +452,51 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_backward_long(const L
 {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ float red[2][kLongRowWG / 64];
-    const uint64_t row = blockIdx.x;
-    const T *const x = static_cast<const T *>(P.x) + row * P.ldx;
-    const T *const dy = static_cast<const T *>(P.dy) + row * P.ldg;
-    const float mean = P.mean[row], rstd = P.rstd[row];
-    const auto both = [&](uint32_t at, float (&n)[VEC], float (&d)[VEC]) {
-        float w[VEC];
-        load_as_float<VEC>(n, x + at);
-        load_as_float<VEC>(d, dy + at);
-        if (P.weight)
-            load_as_float<VEC>(w, static_cast<const W *>(P.weight) + at);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            n[e] = (n[e] - mean) * rstd;
+    for (uint64_t row = blockIdx.x; row < P.rows; row += gridDim.x) {
+        const T *const x = static_cast<const T *>(P.x) + row * P.ldx;
+        const T *const dy = static_cast<const T *>(P.dy) + row * P.ldg;
+        const float mean = P.mean[row], rstd = P.rstd[row];
+        const auto both = [&](uint32_t at, float (&n)[VEC], float (&d)[VEC]) {
+            float w[VEC];
+            load_as_float<VEC>(n, x + at);
+            load_as_float<VEC>(d, dy + at);
             if (P.weight)
-                d[e] *= w[e];
-        }
-    };
-    float s1 = 0.0f, s2 = 0.0f;
-    for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-        float n[VEC], d[VEC];
-        both(at, n, d);
+                load_as_float<VEC>(w, static_cast<const W *>(P.weight) + at);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float c = (uint32_t)e >= skip ? d[e] : 0.0f;
-            s1 += c;
-            s2 = __builtin_fmaf(c, n[e], s2);
-        }
-    });
-    s1 = row_sum<kLongRowWG>(s1, red[0]) / (float)P.hidden;
-    s2 = row_sum<kLongRowWG>(s2, red[1]) / (float)P.hidden;
-    T *const dx = static_cast<T *>(P.dx) + row * P.ldd;
-    for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-        float n[VEC], d[VEC], a[VEC];
-        both(at, n, d);
-        if (P.add)
-            load_as_float<VEC>(a, static_cast<const T *>(P.add) + row * P.lda + at);
+            for (int e = 0; e < VEC; ++e) {
+                n[e] = (n[e] - mean) * rstd;
+                if (P.weight)
+                    d[e] *= w[e];
+            }
+        };
+        float s1 = 0.0f, s2 = 0.0f;
+        for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
+            float n[VEC], d[VEC];
+            both(at, n, d);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            d[e] = (d[e] - s1 - n[e] * s2) * rstd;
+            for (int e = 0; e < VEC; ++e) {
+                const float c = (uint32_t)e >= skip ? d[e] : 0.0f;
+                s1 += c;
+                s2 = __builtin_fmaf(c, n[e], s2);
+            }
+        });
+        s1 = row_sum<kLongRowWG>(s1, red[0]) / (float)P.hidden;
+        s2 = row_sum<kLongRowWG>(s2, red[1]) / (float)P.hidden;
+        T *const dx = static_cast<T *>(P.dx) + row * P.ldd;
+        for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
+            float n[VEC], d[VEC], a[VEC];
+            both(at, n, d);
             if (P.add)
-                d[e] += a[e];
-        }
-        store_behind<VEC>(dx + at, d, skip);
-    });
+                load_as_float<VEC>(a, static_cast<const T *>(P.add) + row * P.lda + at);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                d[e] = (d[e] - s1 - n[e] * s2) * rstd;
+                if (P.add)
+                    d[e] += a[e];
+            }
+            store_behind<VEC>(dx + at, d, skip);
+        });
+    }
 }
 
 // Sums over rows blockIdx.y, blockIdx.y + gridDim.y, ... of the long rows, a vector of columns per thread.

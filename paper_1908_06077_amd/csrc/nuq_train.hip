@@ -61,9 +61,9 @@ struct AdamwCall {
             return false;
         for (uint32_t i = 0; i < T; ++i)
             if (!valid_array(w[i], n[i], 4) || !valid_array(g[i], n[i], width(g_type)) ||
-                (copy && !valid_array(copy[i], n[i], 2)) || n[i] > UINT64_MAX / 16u || (decay && !std::isfinite(decay[i])))
+                (copy && !valid_array(copy[i], n[i], 2)) || n[i] > UINT64_MAX / 16u || !std::isfinite(keep(i)))
                 return false;
-        return true;
+        return std::isfinite(numbers().step);
     }
     AdamwNumbers numbers() const
     {
@@ -103,12 +103,16 @@ struct AdamwCall {
 // 6.8 alone and 10 in a step that waits for them.
 constexpr uint32_t kSmallChunks = 24;
 
+// Workgroups of 256 threads that a launch has at most: it has fewer than 2^32 threads.
+constexpr uint64_t kMostGroups = 1ull << 23;
+static_assert(kMostGroups * 256u < 1ull << 32, "threads of a launch");
+
 // Walks the tensors of a call, joined where one follows another, and fills tables of at most kMost of them: put(slot, tensor,
-// elements) for each, launch(tensors, chunks) for each table.  Runs are cut so that a launch has at most 2^30 chunks.
+// first element, elements, first chunk) for each, launch(entries, chunks) for each table.  Runs are cut so that a launch has at
+// most kMostGroups chunks.
 template <uint32_t kMost, class Follows, class Put, class Launch>
 int for_tables(uint32_t T, const uint64_t *n, uint64_t chunk, Follows &&follows, Put &&put, Launch &&launch)
 {
-    constexpr uint64_t kChunks = 1ull << 30;
     uint32_t slots = 0;
     uint64_t chunks = 0;
     const auto flush = [&]() -> int {
@@ -123,10 +127,10 @@ int for_tables(uint32_t T, const uint64_t *n, uint64_t chunk, Follows &&follows,
         while (run && j < T && (n[j] == 0 || follows(i, j, run)))
             run += n[j++];
         for (uint64_t at = 0; at < run;) {
-            if (slots == kMost || chunks == kChunks)
+            if (slots == kMost || chunks == kMostGroups)
                 if (const int rc = flush(); rc != NUQ_OK)
                     return rc;
-            const uint64_t take = std::min(run - at, (kChunks - chunks) * chunk);
+            const uint64_t take = std::min(run - at, (kMostGroups - chunks) * chunk);
             put(slots++, i, at, take, (uint32_t)chunks);
             chunks += (take + chunk - 1) / chunk;
             at += take;
@@ -290,15 +294,19 @@ int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const
 {
     if (n == 0)
         return NUQ_OK;
-    const uint64_t groups = (n + 1023u) / 1024u;
-    if (!m_codes || !v_codes || !valid_array(scales, n, 4) || !valid_array(m, n, 4) || !valid_array(v, n, 4) ||
-        groups > 0x7fffffffull)
+    if (!m_codes || !v_codes || !valid_array(scales, n, 4) || !valid_array(m, n, 4) || !valid_array(v, n, 4) || n > UINT64_MAX / 16u)
         return NUQ_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (n > kLastLevelCache / 10u)
-        hipLaunchKernelGGL(k_adamw_values<true>, dim3((uint32_t)groups), dim3(256), 0, st, m_codes, v_codes, scales, m, v, n);
-    else
-        hipLaunchKernelGGL(k_adamw_values<false>, dim3((uint32_t)groups), dim3(256), 0, st, m_codes, v_codes, scales, m, v, n);
+    const bool once = n > kLastLevelCache / 10u;
+    for (uint64_t at = 0; at < n; at += kMostGroups * 1024u) {
+        const uint64_t take = std::min(n - at, kMostGroups * 1024u);
+        const dim3 grid((uint32_t)((take + 1023u) / 1024u));
+        const float *const a = scales + 2u * (at / NUQ_STATE_BLOCK);
+        if (once)
+            hipLaunchKernelGGL(k_adamw_values<true>, grid, dim3(256), 0, st, m_codes + at, v_codes + at, a, m + at, v + at, take);
+        else
+            hipLaunchKernelGGL(k_adamw_values<false>, grid, dim3(256), 0, st, m_codes + at, v_codes + at, a, m + at, v + at, take);
+    }
     return check_launch();
 }
 
@@ -387,6 +395,8 @@ bool valid_rows(uint64_t rows, uint32_t hidden, uint32_t type, uint32_t weight_t
 constexpr uint32_t kParts = 512, kLongParts = 64;
 static_assert(kParts <= 1024, "nuq_layer_norm_workspace_bytes");
 
+dim3 long_grid(uint64_t rows) { return dim3((uint32_t)std::min<uint64_t>(rows, kMostGroups * 256u / kLongRowWG)); }
+
 }  // namespace
 
 extern "C" {
@@ -417,7 +427,7 @@ int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, ui
             const auto run = [&](auto stream_c) {
                 constexpr bool kStream = decltype(stream_c)::value;
                 if constexpr (TEAM == 0) {
-                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, kStream>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+                    hipLaunchKernelGGL((k_layer_norm_forward_long<T, W, kStream>), long_grid(rows), dim3(kLongRowWG), 0, st, P);
                 } else {
                     constexpr uint32_t WG = kForwardWG<TEAM>, TEAMS = WG / TEAM;
                     const uint32_t most = resident_workgroups<k_layer_norm_forward<T, W, TEAM, E, VEC, kStream>>(WG);
@@ -467,7 +477,7 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
                 parts = (uint32_t)std::min<uint64_t>(rows, kLongParts);
                 if (sums)
                     hipLaunchKernelGGL((k_layer_norm_columns<T>), dim3((hidden + 256u * VEC_T - 1u) / (256u * VEC_T), parts), dim3(256), 0, st, P);
-                hipLaunchKernelGGL((k_layer_norm_backward_long<T, W>), dim3((uint32_t)rows), dim3(kLongRowWG), 0, st, P);
+                hipLaunchKernelGGL((k_layer_norm_backward_long<T, W>), long_grid(rows), dim3(kLongRowWG), 0, st, P);
                 return check_launch();
             } else {
                 constexpr uint32_t WG = kBackwardWG<TEAM, E>, TEAMS = WG / TEAM;

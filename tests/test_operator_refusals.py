@@ -140,3 +140,10 @@ def test_binding_refuses_tensors_that_do_not_fit(monkeypatch):
     monkeypatch.undo()
     with pytest.raises(ValueError, match="device tensor"):
         norm(f(2, 4), None, None, None, 1e-5, None, f(2, 4), None, None)
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_adamw_numbers_that_are_none_in_fp32(which):
+    name, ok = _steps()[which]
+    for bad in (dict(alpha=1e39), dict(alpha=1e38, beta1=0.999), dict(alpha=1e10, decay=_f(3e38))):
+        assert getattr(_lib(), name)(*{**ok, **bad}.values()) == EINVAL, bad

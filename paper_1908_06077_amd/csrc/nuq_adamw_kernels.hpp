@@ -386,35 +386,49 @@ __global__ __launch_bounds__(1024) void k_gradient_norm_finish(const double *par
         norm_and_factor(sum, max_norm, out, flags);
 }
 
-// All of it in one workgroup, eight chunks at a time: 4.2 us up to 32 K elements, bound by the latency of two loads and the fp64
-// additions of one CU.  A lane holds the table's entry of one tensor: what a chunk needs comes
-// from there, without another wait for memory.
+// All of it in one workgroup, a quarter of a chunk per wave and two of them at a time: 4.1 us at 16 K elements, 4.5 at 64 K, bound by
+// the latency of two loads.  A lane holds the table's entry of one tensor: what a chunk needs comes from there, without another wait
+// for memory.  Three or six quarters at a time measured 0.1 and 0.2 us more at 64 K.
 template <class G>
 __global__ __launch_bounds__(1024) void k_gradient_norm_small(const NormTable P, float max_norm, float *out, uint32_t *flags)
 {
-    constexpr int VEC = (int)kNormChunk / 1024;
-    constexpr uint32_t kAtOnce = 8;
+    constexpr uint32_t kAtOnce = 2, kWaves = 16, kPart = kNormChunk / 4u;
     __shared__ double red[16];
-    const uint32_t lane = threadIdx.x % 64u, begin = P.start[lane], chunks = P.chunks;
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+    const uint32_t begin = P.start[lane], parts = P.chunks * 4u;
     const uint64_t where = reinterpret_cast<uint64_t>(P.tensor[lane].g), size = P.tensor[lane].n;
     const auto of = [](uint32_t x, uint32_t t) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (int)t); };
     const auto of64 = [&](uint64_t x, uint32_t t) { return (uint64_t)of((uint32_t)(x >> 32), t) << 32 | of((uint32_t)x, t); };
     double sum = 0.0;
-    for (uint32_t first = 0; first < chunks; first += kAtOnce) {
-        float g[kAtOnce][VEC];
+    for (uint32_t first = wave; first < parts; first += kAtOnce * kWaves) {
+        float g[kAtOnce][4][4] = {};
 #pragma unroll
         for (uint32_t k = 0; k < kAtOnce; ++k) {
-            const uint32_t chunk = min(first + k, chunks - 1u);
-            const uint32_t t = (uint32_t)__popcll(__ballot(begin <= chunk)) - 1u;
-            const uint64_t i = (uint64_t)(chunk - of(begin, t)) * kNormChunk + threadIdx.x * VEC;
-            load_some<VEC>(g[k], reinterpret_cast<const G *>(of64(where, t)) + i,
-                           first + k < chunks ? (int64_t)of64(size, t) - (int64_t)i : 0);
+            const uint32_t part = first + k * kWaves, chunk = part / 4u;
+            if (part < parts) {
+                const uint32_t t = (uint32_t)__popcll(__ballot(begin <= chunk)) - 1u;
+                const uint64_t at = (uint64_t)(chunk - of(begin, t)) * kNormChunk + part % 4u * kPart;
+                const G *const pg = reinterpret_cast<const G *>(of64(where, t)) + at;
+                const int64_t left = (int64_t)of64(size, t) - (int64_t)at;
+                if (left >= (int64_t)kPart) {
+#pragma unroll
+                    for (uint32_t r = 0; r < 4u; ++r)
+                        load_as_float<4>(g[k][r], pg + (r * 64u + lane) * 4u);
+                } else {
+#pragma unroll
+                    for (uint32_t r = 0; r < 4u; ++r)
+                        load_some<4>(g[k][r], pg + (r * 64u + lane) * 4u, left - (int64_t)((r * 64u + lane) * 4u));
+                }
+            }
         }
 #pragma unroll
         for (uint32_t k = 0; k < kAtOnce; ++k)
+            if (first + k * kWaves < parts)
 #pragma unroll
-            for (int e = 0; e < VEC && first + k < chunks; ++e)
-                sum = __builtin_fma((double)g[k][e], (double)g[k][e], sum);
+                for (uint32_t r = 0; r < 4u; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sum = __builtin_fma((double)g[k][r][e], (double)g[k][r][e], sum);
     }
     sum = workgroup_sum<1024>(sum, red);
     if (threadIdx.x == 0)

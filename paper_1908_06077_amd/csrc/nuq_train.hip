@@ -99,8 +99,8 @@ struct AdamwCall {
     }
 };
 
-// Chunks whose norm one workgroup takes in a launch of its own: 4.2 us up to 8 of them, 6.7 at 16, 11 at 25, where two launches take
-// 6.8 alone and 10 in a step that waits for them.
+// Chunks whose norm one workgroup takes in a launch of its own: 4.1 us at 4 of them, 4.5 at 16, 6.3 to 6.4 at 25, 9.4 at 49, where two
+// launches take 6.0 to 6.8.
 constexpr uint32_t kSmallChunks = 24;
 
 // Workgroups of 256 threads that a launch has at most: it has fewer than 2^32 threads.

@@ -221,7 +221,8 @@ __device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv, uin
 
 // One pass: 16 bytes per element with 32-bit gradients (1.56 G with gradients and a copy in bfloat16 in 3.9 ms: 6.3 TB/s; 11.7 M,
 // 187 MB, in 38 us: 4.9, of which the start and the last workgroups are some 7).  54 vector instructions per element keep the
-// SIMDs busy for less than half of that.  A block per wave: four were 4 % slower on 11.7 M elements.  A block whose new moments are not all finite is left as it is.
+// SIMDs busy for less than half of that.  A block per wave: four were 4 % slower on 11.7 M elements.  A block whose new
+// moments are not all finite is left as it is.
 // kOnce as above; kWhole: the wave's block is all there.
 template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
 __device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, const AdamwCodedTensor &X, uint64_t block)

@@ -34,9 +34,16 @@ __device__ __forceinline__ void adamw_moments(float &m, float &v, float g, const
     v = v * N.b2 + (g * g) * N.c2;
 }
 
+// The hardware's square root reads a subnormal number as 0: small ones are taken 2^32 times as large.
+__device__ __forceinline__ float square_root(float v)
+{
+    const bool small = v < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(small ? v * 0x1p32f : v) * (small ? 0x1p-16f : 1.0f);
+}
+
 __device__ __forceinline__ float adamw_weight(float w, float m, float v, float keep, const AdamwNumbers &N)
 {
-    const float u = m * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_sqrtf(v), N.root, N.eps));
+    const float u = m * __builtin_amdgcn_rcpf(__builtin_fmaf(square_root(v), N.root, N.eps));
     return __builtin_fmaf(-N.step, u, w * keep);
 }
 

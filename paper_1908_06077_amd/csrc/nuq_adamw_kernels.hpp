@@ -25,7 +25,7 @@ struct AdamwNumbers {
     float b1, c1, b2, c2;   // beta1, 1 - beta1, beta2, 1 - beta2
     float step;             // alpha / (1 - beta1^t)
     float root;             // 1 / sqrt(1 - beta2^t)
-    float eps;
+    float eps;              // (all three 2^-16 times as large where eps is huge)
 };
 
 __device__ __forceinline__ void adamw_moments(float &m, float &v, float g, const AdamwNumbers &N)

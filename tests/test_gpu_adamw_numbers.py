@@ -1,4 +1,4 @@
-"""AdamW where its numbers are extreme: second moments below the least normal float.
+"""AdamW where its numbers are extreme: second moments below the least normal float, and eps at both ends of what is accepted.
 
 Bars (u = 2^-24): 32 u of the update, of which 16 are its own roundings and 16 those of m, v and the constants; a v that is subnormal
 is held to 2^-149 (three such roundings), half of which, relative to v, the root takes over."""
@@ -43,3 +43,11 @@ def test_second_moments_below_the_least_normal_float(coded, eps):
     """v from 1.6e-41, some ten thousand times the least subnormal, through 1e-38 to 1e-36."""
     g = np.concatenate([np.geomspace(4e-20, 1e-17, 300), -np.geomspace(4e-20, 1e-17, 300)]).astype(np.float32)
     check(coded, g, 1e-3, 0.9, 0.99, eps)
+
+
+@pytest.mark.parametrize("coded", [False, True])
+@pytest.mark.parametrize("eps", [1e10, 1e25, 8e37, 3e38])
+def test_an_eps_above_every_second_moment(coded, eps):
+    """The denominator's reciprocal passes below the least normal float."""
+    g = np.geomspace(1.0, 1e18, 700).astype(np.float32)
+    check(coded, g, 1e30, 0.9, 0.99, eps)

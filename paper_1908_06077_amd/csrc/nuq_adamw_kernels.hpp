@@ -128,13 +128,16 @@ __global__ __launch_bounds__(256) void k_adamw(const AdamwTable P)
 
 // ---- states in 8 bits ----
 // Blocks of 256 elements, one per wave at a time: four elements per lane, the block's two maxima over the wave's lanes.
-//   m: nearest float8 e4m3 of (m * (1 / a)) * 256, a the block's largest |m|: steps of 1/16 to 1/8 down to a / 2^14, then of a / 2^17.
+//   m: float8 e4m3 of (m * (1 / a)) * 256, a the block's largest |m|: steps of 1/16 to 1/8 down to a / 2^14, then of a / 2^17.
 //   v: eight bits c, five of exponent and three of fraction; c stands for (the float with the bits c << 20) * 2^96 * a, a the
-//      block's largest v, whose code is 248.  Nearest code, ties to even; a v above 0 gets at least code 1: m / sqrt(v) stays
-//      bounded where m is still held.
-// The largest of a block is held exactly, so a block that shrinks or grows as a whole does so without loss.  What is lost is
-// change against the largest one that is less than half a step at once: a v that would decay by a thousandth per step beside a
-// largest one that stays keeps its code.
+//      block's largest v, whose code is 248.  A v above 0 gets at least code 1: m / sqrt(v) stays bounded where m is still held.
+// The largest of a block is held exactly, so a block that shrinks or grows as a whole does so without loss.
+//
+// Rounding.  A step replaces the share (1 - beta) / (1 - beta^t) of a moment.  From 1/16 on, which no half step of a code exceeds,
+// the nearest code is taken (ties to even).  Below that the nearest code could be the old one for good, so the code is drawn: the upper
+// or the lower one, so that the mean is kept.  With beta2 = 0.999 and gradients of one size, sqrt of v as held over sqrt of v in fp32
+// has 1 % and 99 % points of 0.76 and 1.28 (0.75 and 1.51 nearest), and after one gradient in sixteen grew fourfold the others come
+// back to a median of 0.99 (2.9 nearest).
 
 constexpr uint32_t kStateBlock = NUQ_STATE_BLOCK;
 static_assert(kStateBlock == 256, "a wave holds four elements of a block per lane");
@@ -155,6 +158,8 @@ struct AdamwCodedTable {
     AdamwNumbers num;
     const float *coefficient;
     uint32_t *flags;
+    uint64_t t;
+    uint32_t draw_m, draw_v;                // whether codes of m, of v are drawn
 };
 static_assert(sizeof(AdamwCodedTable) <= 4096, "a launch's arguments");
 
@@ -212,24 +217,60 @@ __device__ __forceinline__ uint32_t encode_m(const float (&m)[4], float inv)
     x = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * inv * 256.0f, m[3] * inv * 256.0f, x, true);
     return (uint32_t)x;
 }
-// least: 1, or 0 in a block of zeros.
-__device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv, uint32_t least)
+// kDraw: `draw` is added below the code's bits instead of half a step.  least: 1, or 0 in a block of zeros.
+template <bool kDraw>
+__device__ __forceinline__ uint32_t encode_v(const float (&v)[4], float inv, uint32_t least, const uint32_t (&draw)[4])
 {
     uint32_t x = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const uint32_t bits = __builtin_bit_cast(uint32_t, v[e] * inv * 0x1p-96f);
-        uint32_t code = (bits + 0x7FFFFu + ((bits >> 20) & 1u)) >> 20;
+        uint32_t code = (bits + (kDraw ? draw[e] : 0x7FFFFu + ((bits >> 20) & 1u))) >> 20;
         code = max(code, min(__builtin_bit_cast(uint32_t, v[e]), least));
         x |= code << (8 * e);
     }
     return x;
 }
+// The same for m: e4m3 without its sign is the float with the bits c << 20, times 2^120.
+__device__ __forceinline__ uint32_t encode_m_drawn(const float (&m)[4], float inv, const uint32_t (&draw)[4])
+{
+    uint32_t x = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t bits = __builtin_bit_cast(uint32_t, m[e] * inv * 0x1p-112f);
+        x |= (((bits & 0x7FFFFFFFu) + draw[e]) >> 20 | (bits >> 24 & 0x80u)) << (8 * e);
+    }
+    return x;
+}
+
+// Draws for a lane's four codes of v and of m: multiples of 16, and 8, below 2^20, so that what is within seven units of the last
+// place of a code's value gets that code (a code that only fades with its scale comes back with the error of five roundings).  They
+// come from the step, the block's new scales and the element's place in its block: equal inputs give equal bits, wherever the tensor
+// stands and whatever it is joined with.  The counter hash of the quantizer.
+__device__ __forceinline__ void state_draws(uint32_t (&for_v)[4], uint32_t (&for_m)[4], uint64_t t, uint32_t top_m, uint32_t top_v,
+                                            uint32_t lane)
+{
+    uint64_t z = ((uint64_t)top_m << 32 | top_v) + t * 0x9E3779B97F4A7C15ull;
+    z = (z ^ z >> 30) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ z >> 27) * 0x94D049BB133111EBull;
+    z ^= z >> 31;
+    const uint32_t first = ((uint32_t)z + lane * 4u) * 0x9E3779B1u;
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e) {
+        uint32_t x = first + e * 0x9E3779B1u;
+        x = (x ^ x >> 15 ^ (uint32_t)(z >> 32)) * 0x85EBCA6Bu;
+        x ^= x >> 16;
+        uint32_t y = x * 0x9E3779B1u;
+        y ^= y >> 15;
+        for_v[e] = (x >> 12 & 0xFFFF0u) | 8u;
+        for_m[e] = (y >> 12 & 0xFFFF0u) | 8u;
+    }
+}
 
 // One pass: 16 bytes per element with 32-bit gradients (1.56 G with gradients and a copy in bfloat16 in 3.9 ms: 6.3 TB/s; 11.7 M,
 // 187 MB, in 38 us: 4.9, of which the start and the last workgroups are some 7).  54 vector instructions per element keep the
-// SIMDs busy for less than half of that.  A block per wave: four were 4 % slower on 11.7 M elements.  A block whose new
-// moments are not all finite is left as it is.
+// SIMDs busy for less than half of that; with drawn codes 400 M elements take 1030 to 1043 us, 1026 to 1033 without.  A block per
+// wave: four were 4 % slower on 11.7 M elements.  A block whose new moments are not all finite is left as it is.
 // kOnce as above; kWhole: the wave's block is all there.
 template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
 __device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, const AdamwCodedTensor &X, uint64_t block)
@@ -259,8 +300,21 @@ __device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, const Adam
         top_m = top_m < 0x00800000u ? 0u : top_m;
         top_v = top_v < 0x00800000u ? 0u : top_v;
         const float a = __builtin_bit_cast(float, top_m), b = __builtin_bit_cast(float, top_v);
-        store_codes<kWhole, kOnce>(X.m + i, encode_m(m, top_m ? 1.0f / a : 0.0f), have);
-        store_codes<kWhole, kOnce>(X.v + i, encode_v(v, top_v ? 1.0f / b : 0.0f, top_v ? 1u : 0u), have);
+        const float inv_a = top_m ? 1.0f / a : 0.0f, inv_b = top_v ? 1.0f / b : 0.0f;
+        const uint32_t least = top_v ? 1u : 0u;
+        uint32_t new_m, new_v;
+        if (P.draw_m | P.draw_v) {
+            uint32_t for_v[4], for_m[4];
+            state_draws(for_v, for_m, P.t, top_m, top_v, lane);
+            new_m = P.draw_m ? encode_m_drawn(m, inv_a, for_m) : encode_m(m, inv_a);
+            new_v = P.draw_v ? encode_v<true>(v, inv_b, least, for_v) : encode_v<false>(v, inv_b, least, for_v);
+        } else {
+            const uint32_t none[4] = {};
+            new_m = encode_m(m, inv_a);
+            new_v = encode_v<false>(v, inv_b, least, none);
+        }
+        store_codes<kWhole, kOnce>(X.m + i, new_m, have);
+        store_codes<kWhole, kOnce>(X.v + i, new_v, have);
         if (lane == 0) {
             scales[0] = a;
             scales[1] = b;

@@ -63,16 +63,18 @@ struct AdamwCall {
             if (!valid_array(w[i], n[i], 4) || !valid_array(g[i], n[i], width(g_type)) ||
                 (copy && !valid_array(copy[i], n[i], 2)) || n[i] > UINT64_MAX / 16u || !std::isfinite(keep(i)))
                 return false;
-        return std::isfinite((float)(alpha / -std::expm1((double)t * std::log(beta1))));
+        return std::isfinite((float)(alpha / faded(beta1)));
     }
+    double faded(double beta) const { return -std::expm1((double)t * std::log(beta)); }        // 1 - beta^t
+    // Whether a step replaces less than a sixteenth of a moment.
+    bool creeps(double beta) const { return 16.0 * (1.0 - beta) < faded(beta); }
     AdamwNumbers numbers() const
     {
-        const double fade1 = -std::expm1((double)t * std::log(beta1)), fade2 = -std::expm1((double)t * std::log(beta2));
         // The hardware's reciprocal of a number above 2^126 is 0: near there the denominator is taken 2^-16 times as large, and with
         // it the step.  (The root is at most 2^64, its factor 2^27.)
         const double part = eps > 0x1p120 ? 0x1p-16 : 1.0;
-        return {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(alpha / fade1 * part),
-                (float)(1.0 / std::sqrt(fade2) * part), (float)(eps * part)};
+        return {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)(alpha / faded(beta1) * part),
+                (float)(1.0 / std::sqrt(faded(beta2)) * part), (float)(eps * part)};
     }
     float keep(uint32_t i) const { return decay ? (float)(1.0 - alpha * (double)decay[i]) : 1.0f; }
     const void *g_at(uint32_t i, uint64_t e) const { return static_cast<const char *>(g[i]) + e * width(g_type); }
@@ -266,6 +268,9 @@ int nuq_adamw_step_coded(uint32_t T, float *const *w, const void *const *g, uint
             return NUQ_EINVAL;
     AdamwCodedTable P;
     P.num = C.numbers();
+    P.t = t;
+    P.draw_m = C.creeps(beta1);
+    P.draw_v = C.creeps(beta2);
     P.coefficient = coefficient;
     P.flags = flags_ptr();
     if (!P.flags)

@@ -525,7 +525,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackw
     store_from_float<VEC>(out + P.hidden, db);
 }
 
-// dweight and dbias (blockIdx.y) from the partial sums, in a fixed order: 16 columns per workgroup, 64 threads to each.
+// dweight and dbias (blockIdx.y) from the partial sums, in a fixed order: 16 columns at a time per workgroup, 64 threads to each.
 template <class W>
 __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, W *dweight,
                                                             W *dbias)
@@ -534,32 +534,39 @@ __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial
     W *const out = blockIdx.y ? dbias : dweight;
     if (!out)
         return;
-    const uint32_t c = threadIdx.x % 16u, group = threadIdx.x / 16u, col = blockIdx.x * 16u + c;
-    float sum = 0.0f;
-    if (col < hidden) {
-        const float *const from = partial + (uint64_t)blockIdx.y * hidden + col;
-        uint32_t p = group;
-        for (; p + 192u < parts; p += 256u) {                // four loads at once
-            float x[4];
+    const uint32_t c = threadIdx.x % 16u, group = threadIdx.x / 16u;
+    for (uint32_t begin = blockIdx.x * 16u;;) {
+        const uint32_t col = begin + c;
+        float sum = 0.0f;
+        if (col < hidden) {
+            const float *const from = partial + (uint64_t)blockIdx.y * hidden + col;
+            uint32_t p = group;
+            for (; p + 192u < parts; p += 256u) {            // four loads at once
+                float x[4];
 #pragma unroll
-            for (uint32_t k = 0; k < 4u; ++k)
-                x[k] = from[(uint64_t)(p + 64u * k) * 2u * hidden];
-            sum += (x[0] + x[1]) + (x[2] + x[3]);
+                for (uint32_t k = 0; k < 4u; ++k)
+                    x[k] = from[(uint64_t)(p + 64u * k) * 2u * hidden];
+                sum += (x[0] + x[1]) + (x[2] + x[3]);
+            }
+            for (; p < parts; p += 64u)
+                sum += from[(uint64_t)p * 2u * hidden];
         }
-        for (; p < parts; p += 64u)
-            sum += from[(uint64_t)p * 2u * hidden];
-    }
-    red[group][c] = sum;
-    __syncthreads();
-    if (threadIdx.x < 64u) {                                 // one wave: four lanes to a column
-        const uint32_t cc = threadIdx.x / 4u, part = threadIdx.x % 4u, to = blockIdx.x * 16u + cc;
-        sum = 0.0f;
+        red[group][c] = sum;
+        __syncthreads();
+        if (threadIdx.x < 64u) {                             // one wave: four lanes to a column
+            const uint32_t cc = threadIdx.x / 4u, part = threadIdx.x % 4u, to = begin + cc;
+            sum = 0.0f;
 #pragma unroll
-        for (uint32_t k = 0; k < 16u; ++k)
-            sum += red[part * 16u + k][cc];
-        sum = team_sum<4>(sum);
-        if (part == 0 && to < hidden)
-            out[to] = (W)sum;
+            for (uint32_t k = 0; k < 16u; ++k)
+                sum += red[part * 16u + k][cc];
+            sum = team_sum<4>(sum);
+            if (part == 0 && to < hidden)
+                out[to] = (W)sum;
+        }
+        begin += gridDim.x * 16u;                            // (hidden is at most 2^30, a grid's columns 2^24)
+        if (begin >= hidden)
+            break;
+        __syncthreads();
     }
 }
 

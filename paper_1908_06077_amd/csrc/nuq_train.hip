@@ -503,7 +503,8 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
         });
         if (rc != NUQ_OK || !sums)
             return rc;
-        hipLaunchKernelGGL((k_layer_norm_finish<W>), dim3((hidden + 15u) / 16u, 2), dim3(1024), 0, st, P.partial, parts, hidden,
+        const uint32_t groups = (uint32_t)std::min<uint64_t>((hidden + 15u) / 16u, kMostGroups * 256u / 1024u / 2u);
+        hipLaunchKernelGGL((k_layer_norm_finish<W>), dim3(groups, 2), dim3(1024), 0, st, P.partial, parts, hidden,
                            static_cast<W *>(dweight), static_cast<W *>(dbias));
         return check_launch();
     });

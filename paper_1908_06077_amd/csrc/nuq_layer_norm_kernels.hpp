@@ -167,7 +167,8 @@ __global__ __launch_bounds__(kForwardWG<TEAM>) void k_layer_norm_forward(const L
 }
 
 // Rows that no team's registers hold: a workgroup reads its row three times, from cache where it fits (1024 x 32768 in bfloat16
-// 44.5 us, 3.0 TB/s of the bytes of one reading, 107 us with single elements instead of 16 bytes).
+// 44.5 us, 3.0 TB/s of the bytes of one reading, 107 us with single elements instead of 16 bytes).  A thread's part of a row has no
+// bound, so it adds up in fp64 what its vectors sum to in fp32: the error does not grow with the row.
 constexpr int kLongRowWG = 1024;
 
 // f(first column, elements to leave out) for the thread's vectors of VEC neighbouring elements of a row of at least VEC.  The last
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_forward_long(const La
     __shared__ float red[2][kLongRowWG / 64];
     for (uint64_t row = blockIdx.x; row < P.rows; row += gridDim.x) {
         const T *x = static_cast<const T *>(P.x) + row * P.ldx;
-        float sum = 0.0f;
+        double all = 0.0;
         if constexpr (kStream) {
             const T *const res = static_cast<const T *>(P.residual) + row * P.ldr;
             T *const total = static_cast<T *>(P.total) + row * P.ldt;
@@ -208,35 +209,39 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_forward_long(const La
                 float s[VEC], r[VEC];
                 load_as_float<VEC>(s, x + at);
                 load_as_float<VEC>(r, res + at);
+                float sum = 0.0f;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     s[e] = (float)(T)(s[e] + r[e]);
                     sum += (uint32_t)e >= skip ? s[e] : 0.0f;
                 }
+                all += sum;
                 store_behind<VEC>(total + at, s, skip);          // (read again by the thread that wrote it)
             });
             x = total;
         } else {
             for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-                float s[VEC];
+                float s[VEC], sum = 0.0f;
                 load_as_float<VEC>(s, x + at);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
                     sum += (uint32_t)e >= skip ? s[e] : 0.0f;
+                all += sum;
             });
         }
-        const float mean = row_sum<kLongRowWG>(sum, red[0]) / (float)P.hidden;
-        float square = 0.0f;
+        const float mean = row_sum<kLongRowWG>((float)all, red[0]) / (float)P.hidden;
+        all = 0.0;
         for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-            float s[VEC];
+            float s[VEC], square = 0.0f;
             load_as_float<VEC>(s, x + at);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const float d = (uint32_t)e >= skip ? s[e] - mean : 0.0f;
                 square = __builtin_fmaf(d, d, square);
             }
+            all += square;
         });
-        const float rstd = 1.0f / __builtin_sqrtf(row_sum<kLongRowWG>(square, red[1]) / (float)P.hidden + P.eps);
+        const float rstd = 1.0f / __builtin_sqrtf(row_sum<kLongRowWG>((float)all, red[1]) / (float)P.hidden + P.eps);
         if (threadIdx.x == 0) {
             if (P.mean)
                 P.mean[row] = mean;
@@ -469,9 +474,9 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_backward_long(const L
                     d[e] *= w[e];
             }
         };
-        float s1 = 0.0f, s2 = 0.0f;
+        double all1 = 0.0, all2 = 0.0;
         for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
-            float n[VEC], d[VEC];
+            float n[VEC], d[VEC], s1 = 0.0f, s2 = 0.0f;
             both(at, n, d);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
@@ -479,9 +484,11 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_backward_long(const L
                 s1 += c;
                 s2 = __builtin_fmaf(c, n[e], s2);
             }
+            all1 += s1;
+            all2 += s2;
         });
-        s1 = row_sum<kLongRowWG>(s1, red[0]) / (float)P.hidden;
-        s2 = row_sum<kLongRowWG>(s2, red[1]) / (float)P.hidden;
+        const float s1 = row_sum<kLongRowWG>((float)all1, red[0]) / (float)P.hidden;
+        const float s2 = row_sum<kLongRowWG>((float)all2, red[1]) / (float)P.hidden;
         T *const dx = static_cast<T *>(P.dx) + row * P.ldd;
         for_row<VEC, kLongRowWG>(P.hidden, [&](uint32_t at, uint32_t skip) {
             float n[VEC], d[VEC], a[VEC];

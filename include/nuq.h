@@ -487,7 +487,7 @@ int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, ui
  * and d = dy * weight:  dx = rstd * (d - mean(d) - n * mean(d n)) (+ add), the gradient of x and of
  * residual alike; add: the gradient that arrives through total, may be NULL.  dweight = sum over rows of
  * dy * n, dbias = sum of dy (hidden elements of weight_type, each may be NULL): summed in fp32 in a fixed
- * order, rounded once.  dx may be dy.  Row strides as above (ldg of dy, ldx, lda of add: any; ldd of dx
+ * order, with at most rows / 256 + 64 roundings of the summed magnitudes, rounded once.  dx may be dy.  Row strides as above (ldg of dy, ldx, lda of add: any; ldd of dx
  * at least hidden).  workspace: DEVICE memory, nuq_layer_norm_workspace_bytes(rows, hidden) bytes,
  * 16-byte aligned, overwritten; may be NULL where neither dweight nor dbias is asked for. */
 uint64_t nuq_layer_norm_workspace_bytes(uint64_t rows, uint32_t hidden);

@@ -506,7 +506,8 @@ __global__ __launch_bounds__(kLongRowWG) void k_layer_norm_backward_long(const L
     }
 }
 
-// Sums over rows blockIdx.y, blockIdx.y + gridDim.y, ... of the long rows, a vector of columns per thread.
+// Sums over rows blockIdx.y, blockIdx.y + gridDim.y, ... of the long rows, a vector of columns per thread; in pieces of 32 rows, which
+// keep what rounding adds up to at 32 and a 2048th of the rows.
 template <class T>
 __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackward P)
 {
@@ -516,15 +517,23 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackw
         return;
     const uint32_t at = min(col, P.hidden - VEC);
     float dw[VEC] = {}, db[VEC] = {};
-    for (uint64_t row = blockIdx.y; row < P.rows; row += gridDim.y) {
-        float n[VEC], d[VEC];
-        load_as_float<VEC>(d, static_cast<const T *>(P.dy) + row * P.ldg + at);
-        load_as_float<VEC>(n, static_cast<const T *>(P.x) + row * P.ldx + at);
-        const float mean = P.mean[row], rstd = P.rstd[row];
+    for (uint64_t row = blockIdx.y; row < P.rows;) {
+        float w[VEC] = {}, b[VEC] = {};
+        for (uint32_t k = 0; k < 32u && row < P.rows; ++k, row += gridDim.y) {
+            float n[VEC], d[VEC];
+            load_as_float<VEC>(d, static_cast<const T *>(P.dy) + row * P.ldg + at);
+            load_as_float<VEC>(n, static_cast<const T *>(P.x) + row * P.ldx + at);
+            const float mean = P.mean[row], rstd = P.rstd[row];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                w[e] = __builtin_fmaf(d[e], (n[e] - mean) * rstd, w[e]);
+                b[e] += d[e];
+            }
+        }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            dw[e] = __builtin_fmaf(d[e], (n[e] - mean) * rstd, dw[e]);
-            db[e] += d[e];
+            dw[e] += w[e];
+            db[e] += b[e];
         }
     }
     float *const out = P.partial + (uint64_t)blockIdx.y * 2u * P.hidden + at;

@@ -73,3 +73,19 @@ def test_gradients_of_long_rows_far_from_zero(nuq, hidden):
     bar = q * (36 * U * (s1.abs() + n.abs() * a2) + 8 * U * (d.abs() + s1.abs() + (n * s2).abs()))
     want = q * (d - s1 - n * s2)
     close(dx, want, bar + U * want.abs())
+
+
+def test_weight_gradients_of_many_long_rows(nuq):
+    """60 000 rows whose gradients repeat, so that an addition's rounding repeats too.  64 groups of rows, each in pieces of 32 rows:
+    32 + rows / 2048 additions, then 20 that add up the groups."""
+    rows, hidden = 60_000, 16_400
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    line = 0.05 + 0.1 * torch.rand(hidden, generator=gen, device=DEV)
+    x, dy = torch.full((rows, hidden), 1.5, device=DEV), line.expand(rows, hidden).contiguous()
+    mean, rstd = torch.full((rows,), 0.5, device=DEV), torch.ones(rows, device=DEV)      # n = 1
+    dw, db = torch.empty(hidden, device=DEV), torch.empty(hidden, device=DEV)
+    ws = torch.empty(nuq.nuq_layer_norm_workspace_bytes(rows, hidden), dtype=torch.uint8, device=DEV)
+    nuq.nuq_layer_norm_backward(dy, x, None, mean, rstd, None, torch.empty_like(x), dw, db, ws)
+    want = rows * line.double()
+    for got in (dw, db):
+        close(got, want, want * U * (52 + rows / 2048 + 2))

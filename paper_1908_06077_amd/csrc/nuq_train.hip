@@ -345,9 +345,11 @@ int with_row_shape(uint32_t hidden, F &&f)
     NUQ_SHAPE(16, 8)
     NUQ_SHAPE(16, 16)
     NUQ_SHAPE(32, 16)
-    if constexpr (kBackward && VEC == 4)
+    if constexpr (kBackward && VEC == 4) {
         NUQ_SHAPE(128, 8)
-    NUQ_SHAPE(64, 16)
+    } else {
+        NUQ_SHAPE(64, 16)
+    }
     if constexpr (kBackward) {
         NUQ_SHAPE(256, 8)
         NUQ_SHAPE(256, 16)

@@ -411,9 +411,11 @@ int nuq_normalized_variance(const double *sum, const double *sumsq, uint64_t d, 
 /* The norm of T tensors taken as one vector, and the factor that clips them.  g: HOST array of T device
  * pointers, element-aligned (NULL where n is 0); n: HOST array of T counts; type: NUQ_F32, NUQ_BF16 or
  * NUQ_F16.  out (DEVICE, 2 floats): out[0] = sqrt(sum of all g_i^2), out[1] = min(1, max_norm / out[0]).
- * Summed in fp64 in an order that depends on the sizes alone: equal inputs give equal bits, and no square
- * overflows.  Where the norm is not finite (or above the largest float) out[1] is NaN, which the steps
- * below take as "leave everything as it is", and NUQ_FLAG_NONFINITE is raised.  max_norm: positive,
+ * Summed in fp64 in an order that depends on the sizes and on which tensors lie directly behind one another
+ * in memory (those are taken as one): the same tensors give the same bits, equal values elsewhere the same
+ * norm but for the rounding of fp64 sums, rounded once to fp32.  No square overflows.  Where the norm is not
+ * finite (or above the largest float) out[1] is NaN, which the steps below take as "leave everything as it
+ * is", and NUQ_FLAG_NONFINITE is raised.  max_norm: positive,
  * infinite for the norm alone (NUQ_EINVAL otherwise, also for more than 2^19 tensors none of which lies
  * behind another).  workspace: DEVICE memory of at least
  * NUQ_GRADIENT_NORM_WORKSPACE_BYTES bytes, 8-byte aligned, overwritten. */

@@ -60,7 +60,8 @@ class DataParallelAdamW(DataParallelSGD):
         self.average = torch.empty_like(w)
         views = lambda flat: [flat[o:o + n] for n, o in zip(sizes, starts)]  # noqa: E731
         self.ws, self.grads = views(w), views(self.average)
-        self.norm = torch.empty(2, dtype=torch.float32, device=w.device)         # norm of the last average, factor on it
+        # norm of the last average, factor on it; NaN before the first step, and where nothing is clipped
+        self.norm = torch.full((2,), float("nan"), dtype=torch.float32, device=w.device)
         self.workspace = torch.empty(nuq.GRADIENT_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=w.device)
 
     def apply(self, messages: list[nuq.Message]) -> None:

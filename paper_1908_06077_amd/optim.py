@@ -113,7 +113,7 @@ class NUQSGD(_Workers):
 
 class NUQAdamW(_Workers):
     """AdamW on the average of K coded gradients.  max_norm: that average is scaled down to this norm (`norm` holds the norm of
-    the last one and the factor, on the device).  state_bits: 32, or 8 for moments in codes with scales per block."""
+    the last one and the factor, on the device; NaN without max_norm).  state_bits: 32, or 8 for moments in codes with scales per block."""
 
     def __init__(self, params, K: int, lr: float, betas: tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 1e-2, bucket: int = 8192, s: int = 3, sync_stride: int = 256,

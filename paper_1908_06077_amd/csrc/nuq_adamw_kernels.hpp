@@ -67,7 +67,7 @@ struct AdamwTable {
 static_assert(sizeof(AdamwTable) <= 4096, "a launch's arguments");
 
 // One pass: 28 bytes per element with 32-bit gradients (25.6 M elements in 110 us: 6.5 TB/s; 1.56 G with gradients and a copy in
-// bfloat16 in 6.9 to 7.5 ms: 5.8 to 6.3).  An element whose new moments are not finite is left as it is.
+// bfloat16 in 6.9 to 7.6 ms: 5.8 to 6.3).  An element whose new moments are not finite is left as it is.
 // kOnce: the call's arrays are larger than the last-level cache.  kWhole: the workgroup's elements are all there.
 template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
 __device__ __forceinline__ void adamw_chunk(const AdamwTable &P, const AdamwTensor &X, uint64_t base)
@@ -268,9 +268,10 @@ __device__ __forceinline__ void state_draws(uint32_t (&for_v)[4], uint32_t (&for
 }
 
 // One pass: 16 bytes per element with 32-bit gradients (1.56 G with gradients and a copy in bfloat16 in 3.9 ms: 6.3 TB/s; 11.7 M,
-// 187 MB, in 38 us: 4.9, of which the start and the last workgroups are some 7).  54 vector instructions per element keep the
-// SIMDs busy for less than half of that; with drawn codes 400 M elements take 1030 to 1043 us, 1026 to 1033 without.  A block per
-// wave: four were 4 % slower on 11.7 M elements.  A block whose new moments are not all finite is left as it is.
+// 187 MB, in 37 us: 5.0, of which the start and the last workgroups are some 7).  53 vector instructions per element keep the
+// SIMDs busy for less than half of that, 58 with drawn codes of v, 69 of both: 400 M elements take 1030 to 1043 us with them, 1026 to
+// 1033 without.  A block per wave: four were 4 % slower on 11.7 M elements.  A block whose new moments are not all finite is left as
+// it is.
 // kOnce as above; kWhole: the wave's block is all there.
 template <class G, class C, bool kCopy, bool kOnce, bool kWhole>
 __device__ __forceinline__ void adamw_block(const AdamwCodedTable &P, const AdamwCodedTensor &X, uint64_t block)
@@ -363,7 +364,7 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *pm, const u
 // ---- the norm of all gradients ----
 // Sums of squares in fp64 (products of fp32 values are exact there, and no square overflows): a partial per workgroup, then one
 // workgroup adds them in a fixed order (a second launch of 4 us: a count of finished workgroups would have to be zero before
-// the first call, and the workspace is the caller's).  Bound by HBM: 6.2 GB in 0.90 to 0.92 ms, 6.8 TB/s with non-temporal
+// the first call, and the workspace is the caller's).  Bound by HBM: 6.2 GB in 0.90 to 0.93 ms, 6.7 to 6.9 TB/s with non-temporal
 // loads, 6.0 without; 102 MB in 18 us.
 
 constexpr uint32_t kNormChunk = 4096u;

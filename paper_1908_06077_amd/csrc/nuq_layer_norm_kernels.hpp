@@ -90,7 +90,7 @@ template <int TEAM>
 constexpr int kForwardWG = TEAM <= 64 ? 256 : TEAM;
 
 // A team takes rows in turn; the next row is on its way while one is worked on, weight and bias stay in registers.  8192 x 1600 in
-// bfloat16 with the residual 21 us (5.0 TB/s, of which 2 us are the launch), 8192 x 12288 in float32 142 us (5.7 TB/s), one row
+// bfloat16 with the residual 21.7 us (4.8 TB/s, of which 2 us are the launch), 8192 x 12288 in float32 142 us (5.7 TB/s), one row
 // 2.1 us (a launch); one row per workgroup instead: 26.5 and 152 us.
 template <class T, class W, int TEAM, int E, int VEC, bool kStream>
 __global__ __launch_bounds__(kForwardWG<TEAM>) void k_layer_norm_forward(const LayerNormForward P)
@@ -284,10 +284,11 @@ template <int TEAM, int E>
 constexpr int kBackwardWG = TEAM < 512 ? (E <= 8 ? 1024 : 512) : TEAM;
 
 // A team takes rows in turn, as in the forward pass, and keeps the sums of its columns in registers.  Workgroup p writes
-// partial[p], 8 bytes per column; a second launch (4 to 7 us) adds the workgroups up.  8192 x 1600 in bfloat16 with a gradient to
-// add 22 us (5 TB/s with the partial sums), 32768 x 8192 282 us (5.8 TB/s); 4.8 TB/s at 1000 columns, 3.4 at 16384, where one
-// workgroup fills a CU.  With sixteen elements per thread the sums and operands take 160 registers, so that a CU has eight waves;
-// held to 128 they spill, and the pass takes twice as long; in LDS the sums cost 10 % (but win above 8192 columns).
+// partial[p], 8 bytes per column; a second launch (4 to 12 us) adds the workgroups up.  8192 x 1600 in bfloat16 with a gradient to
+// add 22.5 us (4.8 TB/s with the partial sums), 32768 x 8192 282 us (5.8 TB/s), 33554 x 1000 in float32 101 us (5.3), 4096 x 16384 in
+// bfloat16, where one workgroup fills a CU, 84 us (4.8).  With sixteen elements per thread the sums and operands take 160 registers,
+// so that a CU has eight waves; held to 128 they spill, and the pass takes twice as long; in LDS the sums cost 10 % (but win above
+// 8192 columns).
 template <class T, class W, int TEAM, int E, int VEC, bool kSums>
 __global__ __launch_bounds__((kBackwardWG<TEAM, E>)) void k_layer_norm_backward(const LayerNormBackward P)
 {

@@ -499,6 +499,64 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
                             uint64_t ldd, void *dweight, void *dbias, void *workspace,
                             uint64_t workspace_bytes, nuq_stream_t stream);
 
+/* ---- between the blocks of a transformer: dropout, norms around the residual sum -------------------- */
+
+/* Dropout of `rows` rows of `hidden` elements, from a mask that is computed and never stored.  Element (r, c) is kept iff
+ * u >= T, T = floor(p 2^24 + 1/2), u the upper 24 bits of a hash of (seed, *step, r, c): with
+ *   z = seed + *step * 0xD1342543DE82EF95 + (r + 1) * 0x9E3779B97F4A7C15                       (modulo 2^64)
+ *   z = (z ^ z >> 30) * 0xBF58476D1CE4E5B9;  z = (z ^ z >> 27) * 0x94D049BB133111EB;  z ^= z >> 31
+ *   x = ((uint32_t)z + c) * 0x9E3779B1;  x = (x ^ x >> 15 ^ z >> 32) * 0x85EBCA6B;  u = (x ^ x >> 16) >> 8      (modulo 2^32)
+ * y = (kept ? x * 2^24 / (2^24 - T) : 0) + residual, in fp32, rounded once.  What is dropped counts as 0, also a NaN.  The gradient
+ * is the same call on dy, without a residual: the same seed and step give the same mask.  p: 0 (all is kept) to 1.  step: DEVICE
+ * int64, NULL for 0; it is read when the kernel runs, so that a captured graph draws anew where the program moves it.
+ * x, residual (may be NULL), y: DEVICE, of `type`, element-aligned, row r at r * ld elements (ldx, ldr: any; ldy: at least hidden).
+ * y may be x or residual.  rows and hidden below 2^31. */
+int nuq_dropout(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, uint64_t rows, uint32_t hidden,
+                uint32_t type, double p, uint64_t seed, const int64_t *step, void *y, uint64_t ldy, nuq_stream_t stream);
+
+/* The seam between two blocks: the norm of a branch x (inner), gate, dropout, scales and the residual sum, and the norm of the sum
+ * (outer) that the next block begins with.  Per row
+ *   n1 = N(x), b = n1 * inner_weight + inner_bias        (without an inner norm b = x)
+ *   total = residual_scale * residual + scale * drop(gate * b), rounded to `type`
+ *   y = N(total) * outer_weight + outer_bias             (without an outer norm there is no y)
+ * N(s) = (s - mean) / sqrt(mean of (s - mean)^2 + eps); NUQ_RMS_NORM takes 0 for the mean.  drop: as nuq_dropout, of the same element
+ * (r, c).  inner, outer: NUQ_NO_NORM, NUQ_LAYER_NORM or NUQ_RMS_NORM, one of them at least a norm.  residual may be NULL (taken as
+ * 0), and so may each weight, bias and the gate: `hidden` elements of weight_type (`type` or NUQ_F32).  stats: [4][rows] floats, or
+ * NULL: the inner norm's mean and 1 / sqrt(...), the outer norm's; what a norm does not have is not written.
+ * Rows, strides and aliases as in nuq_layer_norm_forward: y may be x, total may be x or residual.  rows below 2^31, hidden at most
+ * NUQ_RESIDUAL_NORM_MAX_HIDDEN.  In fp32 throughout, variances from centred values, total and y rounded once; eps: finite, not negative;
+ * scale, residual_scale: finite. */
+#define NUQ_NO_NORM 0u
+#define NUQ_LAYER_NORM 1u
+#define NUQ_RMS_NORM 2u
+#define NUQ_RESIDUAL_NORM_MAX_HIDDEN 16384u
+int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, uint32_t inner,
+                              const void *inner_weight, const void *inner_bias, const void *gate, uint32_t outer,
+                              const void *outer_weight, const void *outer_bias, uint64_t rows, uint32_t hidden,
+                              float eps, float scale, float residual_scale, double p, uint64_t seed,
+                              const int64_t *step, uint32_t type, uint32_t weight_type, void *total, uint64_t ldt,
+                              void *y, uint64_t ldy, float *stats, nuq_stream_t stream);
+
+/* Its gradients, from dy (NULL without an outer norm), dtotal, the gradient that arrives through total (may be NULL where there is
+ * an outer norm), the forward's x, total and stats, and the same vectors, scales, p, seed and step.  With n2 = N(total), d = dy *
+ * outer_weight, rstd the outer norm's:
+ *   dt = dtotal + rstd * (d - mean(d) - n2 * mean(d n2));   dresidual = residual_scale * dt (may be NULL)
+ *   g = scale * drop(dt);  h = g * gate;   dx = rstd1 * (h' - mean(h') - n1 * mean(h' n1)),  h' = h * inner_weight  (or h)
+ * (mean(d) and mean(h') fall away with NUQ_RMS_NORM), and the sums over rows, each of which may be NULL:  dinner_weight of h n1,
+ * dinner_bias of h, dgate of g b, douter_weight of dy n2, douter_bias of dy: in fp32 in a fixed order, with at most rows / 256 + 64
+ * roundings of the summed magnitudes, rounded once.  dx may be dy or x, dresidual may be dtotal or total, at the same stride (not
+ * where a sum is asked for over more than 8192 columns: NUQ_EINVAL); the two must not overlap.  workspace: DEVICE memory of nuq_residual_norm_workspace_bytes(rows, hidden) bytes, 16-byte aligned,
+ * overwritten; may be NULL where no sum is asked for. */
+uint64_t nuq_residual_norm_workspace_bytes(uint64_t rows, uint32_t hidden);
+int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal, uint64_t lda, const void *x, uint64_t ldx,
+                               const void *total, uint64_t ldt, uint32_t inner, const void *inner_weight,
+                               const void *inner_bias, const void *gate, uint32_t outer, const void *outer_weight,
+                               uint64_t rows, uint32_t hidden, float scale, float residual_scale, double p, uint64_t seed,
+                               const int64_t *step, uint32_t type, uint32_t weight_type, const float *stats, void *dx,
+                               uint64_t ldd, void *dresidual, uint64_t lde, void *dinner_weight, void *dinner_bias,
+                               void *dgate, void *douter_weight, void *douter_bias, void *workspace,
+                               uint64_t workspace_bytes, nuq_stream_t stream);
+
 /* ---- errors ---------------------------------------------------------------------- */
 
 /* Waits for `stream`, copies the sticky device flags of the current device to

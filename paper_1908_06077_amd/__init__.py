@@ -20,6 +20,8 @@ from .binding import (  # noqa: F401
     nuq_gradient_norm, GRADIENT_NORM_WORKSPACE_BYTES, nuq_adamw_step, nuq_adamw_step_coded, nuq_adamw_state_values,
     nuq_state_blocks, STATE_BLOCK,
     nuq_layer_norm_forward, nuq_layer_norm_backward, nuq_layer_norm_workspace_bytes,
+    nuq_dropout, nuq_residual_norm_forward, nuq_residual_norm_backward, nuq_residual_norm_workspace_bytes,
+    NO_NORM, LAYER_NORM, RMS_NORM, RESIDUAL_NORM_MAX_HIDDEN,
     nuq_last_error_flags, library_path, exported_symbols,
     nuq_encode_shape, nuq_decode_tile, nuq_timing_begin, nuq_timing_collect, T_NORMS, T_QUANTIZE, T_ENCODE, T_QUANTIZE_ENCODE, T_DECODE,
 )

@@ -92,6 +92,13 @@ _SIGNATURES = {
     "nuq_layer_norm_workspace_bytes": (_u64, [_u64, _u32]),
     "nuq_layer_norm_backward": (_i32, [_vp, _u64, _vp, _u64, _vp, _vp, _vp, _vp, _u64, _u64, _u32, _u32, _u32, _vp, _u64, _vp,
                                        _vp, _vp, _u64, _vp]),
+    "nuq_dropout": (_i32, [_vp, _u64, _vp, _u64, _u64, _u32, _u32, _f64, _u64, _vp, _vp, _u64, _vp]),
+    "nuq_residual_norm_forward": (_i32, [_vp, _u64, _vp, _u64, _u32, _vp, _vp, _vp, _u32, _vp, _vp, _u64, _u32, _f32, _f32, _f32,
+                                         _f64, _u64, _vp, _u32, _u32, _vp, _u64, _vp, _u64, _vp, _vp]),
+    "nuq_residual_norm_workspace_bytes": (_u64, [_u64, _u32]),
+    "nuq_residual_norm_backward": (_i32, [_vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _u32, _vp, _vp, _vp, _u32, _vp, _u64, _u32,
+                                          _f32, _f32, _f64, _u64, _vp, _u32, _u32, _vp, _vp, _u64, _vp, _u64, _vp, _vp, _vp, _vp,
+                                          _vp, _vp, _u64, _vp]),
     "nuq_last_error_flags": (_i32, [_vp, _vp]),
     "nuq_encode_shape": (_i32, [_u32, _u32, _u64, _u32, _u32, _u32, _vp, _u32, _vp]),
     "nuq_decode_tile": (_u32, [_u32, _u64, _u32, _u32, _u32, _i32, _u32]),
@@ -794,6 +801,98 @@ def nuq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Ten
                                         _vector(dweight, kind, hidden, "dweight"), _vector(dbias, kind, hidden, "dbias"),
                                         _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                                         _stream()))
+
+
+# ------------------------------------------ dropout, norms around the residual sum
+
+NO_NORM, LAYER_NORM, RMS_NORM = 0, 1, 2
+RESIDUAL_NORM_MAX_HIDDEN = 16384
+
+
+def _step(step: torch.Tensor | None) -> int:
+    return _ptr(step, torch.int64, 0 if step is None else 1, "step")
+
+
+def _maybe_rows(t: torch.Tensor | None, like: torch.Tensor, what: str) -> tuple[int, int]:
+    hidden = like.shape[-1]
+    return (0, 0) if t is None else _rows(t, like.dtype, like.numel() // hidden, hidden, what)
+
+
+def _some_rows(x: torch.Tensor) -> None:
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x: expected rows of one element or more")
+
+
+def nuq_dropout(x: torch.Tensor, residual: torch.Tensor | None, p: float, seed: int, step: torch.Tensor | None,
+                y: torch.Tensor) -> None:
+    """y <- x [..., hidden] where kept, with its scale, 0 elsewhere, plus residual; the mask follows from seed, *step and the place."""
+    code = _calls.dropout(x, residual, p, seed, step, y)
+    if code is not None:
+        return _check("nuq_dropout", code)
+    _some_rows(x)
+    hidden = x.shape[-1]
+    _check("nuq_dropout",
+           _lib.nuq_dropout(*_maybe_rows(x, x, "x"), *_maybe_rows(residual, x, "residual"), x.numel() // hidden, hidden, _type(x, "x"),
+                            float(p), seed & (1 << 64) - 1, _step(step), *_maybe_rows(y, x, "y"), _stream()))
+
+
+def nuq_residual_norm_forward(x: torch.Tensor, residual: torch.Tensor | None, inner: int, inner_weight: torch.Tensor | None,
+                              inner_bias: torch.Tensor | None, gate: torch.Tensor | None, outer: int,
+                              outer_weight: torch.Tensor | None, outer_bias: torch.Tensor | None, eps: float, scale: float,
+                              residual_scale: float, p: float, seed: int, step: torch.Tensor | None, total: torch.Tensor,
+                              y: torch.Tensor | None, stats: torch.Tensor | None) -> None:
+    """total <- residual_scale residual + scale drop(gate norm(x)), y <- norm(total); stats [4, rows]: what backward needs of the norms."""
+    code = _calls.residual_norm_forward(x, residual, inner, inner_weight, inner_bias, gate, outer, outer_weight, outer_bias, eps, scale,
+                                        residual_scale, p, seed, step, total, y, stats)
+    if code is not None:
+        return _check("nuq_residual_norm_forward", code)
+    _some_rows(x)
+    hidden = x.shape[-1]
+    rows = x.numel() // hidden
+    vectors = {"inner_weight": inner_weight, "inner_bias": inner_bias, "gate": gate, "outer_weight": outer_weight, "outer_bias": outer_bias}
+    kind = _weight_dtype(x, *vectors.values())
+    w1, b1, g, w2, b2 = (_vector(v, kind, hidden, name) for name, v in vectors.items())
+    px, ldx = _maybe_rows(x, x, "x")
+    _check("nuq_residual_norm_forward",
+           _lib.nuq_residual_norm_forward(px, ldx, *_maybe_rows(residual, x, "residual"), inner, w1, b1, g, outer, w2, b2, rows, hidden,
+                                          float(eps), float(scale), float(residual_scale), float(p), seed & (1 << 64) - 1, _step(step),
+                                          _type(x, "x"), _TYPES[kind], *_maybe_rows(total, x, "total"), *_maybe_rows(y, x, "y"),
+                                          _vector(stats, torch.float32, 4 * rows, "stats"), _stream()))
+
+
+def nuq_residual_norm_workspace_bytes(rows: int, hidden: int) -> int:
+    return _lib.nuq_residual_norm_workspace_bytes(rows, hidden)
+
+
+def nuq_residual_norm_backward(dy: torch.Tensor | None, dtotal: torch.Tensor | None, x: torch.Tensor, total: torch.Tensor | None,
+                               inner: int, inner_weight: torch.Tensor | None, inner_bias: torch.Tensor | None,
+                               gate: torch.Tensor | None, outer: int, outer_weight: torch.Tensor | None, scale: float,
+                               residual_scale: float, p: float, seed: int, step: torch.Tensor | None, stats: torch.Tensor,
+                               dx: torch.Tensor, dresidual: torch.Tensor | None, dinner_weight: torch.Tensor | None,
+                               dinner_bias: torch.Tensor | None, dgate: torch.Tensor | None, douter_weight: torch.Tensor | None,
+                               douter_bias: torch.Tensor | None, workspace: torch.Tensor | None) -> None:
+    """dx, dresidual <- the gradients of branch and stream from those of y and total; the others <- those of the vectors."""
+    code = _calls.residual_norm_backward(dy, dtotal, x, total, inner, inner_weight, inner_bias, gate, outer, outer_weight, scale,
+                                         residual_scale, p, seed, step, stats, dx, dresidual, dinner_weight, dinner_bias, dgate,
+                                         douter_weight, douter_bias, workspace)
+    if code is not None:
+        return _check("nuq_residual_norm_backward", code)
+    _some_rows(x)
+    hidden = x.shape[-1]
+    rows = x.numel() // hidden
+    vectors = {"inner_weight": inner_weight, "inner_bias": inner_bias, "gate": gate, "outer_weight": outer_weight,
+               "dinner_weight": dinner_weight, "dinner_bias": dinner_bias, "dgate": dgate, "douter_weight": douter_weight,
+               "douter_bias": douter_bias}
+    kind = _weight_dtype(x, *vectors.values())
+    w1, b1, g, w2, *gradients = (_vector(v, kind, hidden, name) for name, v in vectors.items())
+    px, ldx = _maybe_rows(x, x, "x")
+    _check("nuq_residual_norm_backward",
+           _lib.nuq_residual_norm_backward(*_maybe_rows(dy, x, "dy"), *_maybe_rows(dtotal, x, "dtotal"), px, ldx,
+                                           *_maybe_rows(total, x, "total"), inner, w1, b1, g, outer, w2, rows, hidden, float(scale),
+                                           float(residual_scale), float(p), seed & (1 << 64) - 1, _step(step), _type(x, "x"),
+                                           _TYPES[kind], _vector(stats, torch.float32, 4 * rows, "stats"), *_maybe_rows(dx, x, "dx"),
+                                           *_maybe_rows(dresidual, x, "dresidual"), *gradients, _ptr(workspace),
+                                           0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
 
 
 def nuq_last_error_flags() -> int:

@@ -33,7 +33,8 @@ PyObject *g_norms, *g_bit_off, *g_words, *g_sync;                   // attribute
     X(nuq_quantize_pack_fixed_table_batch) X(nuq_unpack_accumulate_fixed_table)                                      \
     X(nuq_quantize_encode_huffman_batch) X(nuq_decode_accumulate_huffman) X(nuq_moments_accumulate)                  \
     X(nuq_gradient_norm) X(nuq_adamw_step) X(nuq_adamw_step_coded) X(nuq_state_blocks) X(nuq_layer_norm_forward)     \
-    X(nuq_layer_norm_backward) X(nuq_adamw_state_values)
+    X(nuq_layer_norm_backward) X(nuq_adamw_state_values) X(nuq_dropout) X(nuq_residual_norm_forward)                 \
+    X(nuq_residual_norm_backward)
 #define NUQ_POINTER(name) decltype(&::name) p_##name = nullptr;
 NUQ_CALLS(NUQ_POINTER)
 
@@ -596,6 +597,65 @@ PyObject *layer_norm_backward(PyObject *const *a)        // dy, x, weight, mean,
                   bytes);
 }
 
+// What dropout draws from: p, seed, step.
+struct Drawn {
+    double p;
+    uint64_t seed;
+    const int64_t *step = nullptr;
+    Drawn(PyObject *p_, PyObject *seed_, PyObject *step_) : p(real(p_))
+    {
+        need(PyLong_CheckExact(seed_));
+        seed = PyLong_AsUnsignedLongLongMask(seed_);              // modulo 2^64
+        if (step_ != Py_None)
+            step = address<const int64_t>(step_, at::kLong, 1);
+    }
+};
+
+PyObject *dropout(PyObject *const *a)                    // x, residual, p, seed, step, y
+{
+    const Rows x(a[0], nullptr), residual(a[1], &x), y(a[5], &x);
+    need(x.hidden > 0 && y.hidden > 0);
+    const Drawn d(a[2], a[3], a[4]);
+    return launch(p_nuq_dropout, x.p, x.ld, residual.p, residual.ld, x.rows, x.hidden, type_of(x.type), d.p, d.seed, d.step, y.p, y.ld);
+}
+
+// x, residual, inner, inner_weight, inner_bias, gate, outer, outer_weight, outer_bias, eps, scale, residual_scale, p, seed, step, total,
+// y, stats
+PyObject *residual_norm_forward(PyObject *const *a)
+{
+    const Rows x(a[0], nullptr), residual(a[1], &x), total(a[15], &x), y(a[16], &x);
+    need(x.hidden > 0 && total.hidden > 0);
+    const Vector w1(a[3], x.hidden), b1(a[4], x.hidden), gate(a[5], x.hidden), w2(a[7], x.hidden), b2(a[8], x.hidden),
+        stats(a[17], 4u * x.rows);
+    const Drawn d(a[12], a[13], a[14]);
+    return launch(p_nuq_residual_norm_forward, x.p, x.ld, residual.p, residual.ld, u32(a[2]), w1.p, b1.p, gate.p, u32(a[6]), w2.p, b2.p,
+                  x.rows, x.hidden, (float)real(a[9]), (float)real(a[10]), (float)real(a[11]), d.p, d.seed, d.step, type_of(x.type),
+                  weight_type(x.type, {&w1, &b1, &gate, &w2, &b2}), total.p, total.ld, y.p, y.ld, stats.floats());
+}
+
+// dy, dtotal, x, total, inner, inner_weight, inner_bias, gate, outer, outer_weight, scale, residual_scale, p, seed, step, stats, dx,
+// dresidual, dinner_weight, dinner_bias, dgate, douter_weight, douter_bias, workspace
+PyObject *residual_norm_backward(PyObject *const *a)
+{
+    const Rows x(a[2], nullptr), dy(a[0], &x), dtotal(a[1], &x), total(a[3], &x), dx(a[16], &x), dresidual(a[17], &x);
+    need(x.hidden > 0 && dx.hidden > 0);
+    const Vector w1(a[5], x.hidden), b1(a[6], x.hidden), gate(a[7], x.hidden), w2(a[9], x.hidden), stats(a[15], 4u * x.rows),
+        dw1(a[18], x.hidden), db1(a[19], x.hidden), dgate(a[20], x.hidden), dw2(a[21], x.hidden), db2(a[22], x.hidden);
+    need(stats.there);
+    const Drawn d(a[12], a[13], a[14]);
+    void *ws = nullptr;
+    uint64_t bytes = 0;
+    if (a[23] != Py_None) {
+        const Bytes b(a[23]);
+        ws = b.p;
+        bytes = b.n;
+    }
+    return launch(p_nuq_residual_norm_backward, dy.p, dy.ld, dtotal.p, dtotal.ld, x.p, x.ld, total.p, total.ld, u32(a[4]), w1.p, b1.p,
+                  gate.p, u32(a[8]), w2.p, x.rows, x.hidden, (float)real(a[10]), (float)real(a[11]), d.p, d.seed, d.step,
+                  type_of(x.type), weight_type(x.type, {&w1, &b1, &gate, &w2, &dw1, &db1, &dgate, &dw2, &db2}), stats.floats(), dx.p,
+                  dx.ld, dresidual.p, dresidual.ld, dw1.p, db1.p, dgate.p, dw2.p, db2.p, ws, bytes);
+}
+
 // bind(addresses of the entry points in NUQ_CALLS' order, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -650,6 +710,9 @@ PyMethodDef g_methods[] = {
     NUQ_METHOD(adamw_state_values, 5),
     NUQ_METHOD(layer_norm_forward, 9),
     NUQ_METHOD(layer_norm_backward, 10),
+    NUQ_METHOD(dropout, 6),
+    NUQ_METHOD(residual_norm_forward, 18),
+    NUQ_METHOD(residual_norm_backward, 24),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nuq_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -542,13 +542,12 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackw
     store_from_float<VEC>(out + P.hidden, db);
 }
 
-// dweight and dbias (blockIdx.y) from the partial sums, in a fixed order: 16 columns at a time per workgroup, 64 threads to each.
+// out <- the sums of `parts` vectors of `hidden` floats that stand `stride` floats apart, in a fixed order: 16 columns at a time per
+// workgroup of 1024, 64 threads to each.
 template <class W>
-__global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, W *dweight,
-                                                            W *dbias)
+__device__ __forceinline__ void column_totals(const float *partial, uint64_t stride, uint32_t parts, uint32_t hidden, W *out)
 {
     __shared__ float red[64][17];
-    W *const out = blockIdx.y ? dbias : dweight;
     if (!out)
         return;
     const uint32_t c = threadIdx.x % 16u, group = threadIdx.x / 16u;
@@ -556,17 +555,17 @@ __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial
         const uint32_t col = begin + c;
         float sum = 0.0f;
         if (col < hidden) {
-            const float *const from = partial + (uint64_t)blockIdx.y * hidden + col;
+            const float *const from = partial + col;
             uint32_t p = group;
             for (; p + 192u < parts; p += 256u) {            // four loads at once
                 float x[4];
 #pragma unroll
                 for (uint32_t k = 0; k < 4u; ++k)
-                    x[k] = from[(uint64_t)(p + 64u * k) * 2u * hidden];
+                    x[k] = from[(p + 64u * k) * stride];
                 sum += (x[0] + x[1]) + (x[2] + x[3]);
             }
             for (; p < parts; p += 64u)
-                sum += from[(uint64_t)p * 2u * hidden];
+                sum += from[p * stride];
         }
         red[group][c] = sum;
         __syncthreads();
@@ -585,6 +584,14 @@ __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial
             break;
         __syncthreads();
     }
+}
+
+// dweight and dbias (blockIdx.y) from the partial sums.
+template <class W>
+__global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, W *dweight,
+                                                            W *dbias)
+{
+    column_totals(partial + (uint64_t)blockIdx.y * hidden, 2ull * hidden, parts, hidden, blockIdx.y ? dbias : dweight);
 }
 
 }  // namespace nuq

@@ -8,38 +8,19 @@
 #include <iterator>
 #include <type_traits>
 
-#include "nuq_host.hpp"
-
 #include "nuq_adamw_kernels.hpp"
 #include "nuq_layer_norm_kernels.hpp"
+#include "nuq_train_host.hpp"
 
 namespace {
 
 using namespace nuq;
-
-template <class T>
-struct Type {
-    using type = T;
-};
-
-// f(Type<element>) for one of the three element types.
-template <class F>
-int with_type(uint32_t type, F &&f)
-{
-    return type == NUQ_F32 ? f(Type<float>{}) : type == NUQ_BF16 ? f(Type<__bf16>{}) : f(Type<_Float16>{});
-}
-
-uint32_t width(uint32_t type) { return type == NUQ_F32 ? 4u : 2u; }
 
 // Arrays that fit this are read and written plainly: they may still be there, and stay for what comes next.  Larger ones take
 // non-temporal loads and stores: an AdamW step on 25.6 M elements (409 MB) 163 -> 130 us, on 1.56 G 8.10 -> 7.52 ms; on 117 MB
 // of 8-bit states, weights and gradients they cost 2 %.  Between (134 to 300 MB) they win 5 % where the arrays have left the cache
 // and lose 20 % where they have not.
 constexpr uint64_t kLastLevelCache = 256ull << 20;
-
-bool off_grid(const void *p, uint32_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1u)) != 0; }
-
-bool valid_array(const void *p, uint64_t n, uint32_t bytes) { return n == 0 || (p && !off_grid(p, bytes)); }
 
 // What a step's launches have in common, and what the step's arguments are checked for.
 struct AdamwCall {
@@ -107,10 +88,6 @@ struct AdamwCall {
 // Chunks whose norm one workgroup takes in a launch of its own: 4.1 us at 4 of them, 4.5 at 16, 6.3 to 6.4 at 25, 9.4 at 49, where two
 // launches take 6.0 to 6.8.
 constexpr uint32_t kSmallChunks = 24;
-
-// Workgroups of 256 threads that a launch has at most: it has fewer than 2^32 threads.
-constexpr uint64_t kMostGroups = 1ull << 23;
-static_assert(kMostGroups * 256u < 1ull << 32, "threads of a launch");
 
 // Walks the tensors of a call, joined where one follows another, and fills tables of at most kMost of them: put(slot, tensor,
 // first element, elements, first chunk) for each, launch(entries, chunks) for each table.  Runs are cut so that a launch has at
@@ -364,34 +341,6 @@ int with_row_shape(uint32_t hidden, F &&f)
     NUQ_SHAPE(1024, 16)
 #undef NUQ_SHAPE
     return f(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 0>{});
-}
-
-// Workgroups of `threads` threads of a kernel that the current device holds at once (0 on error), looked up once per kernel and
-// device.
-template <auto kernel>
-uint32_t resident_workgroups(uint32_t threads)
-{
-    static std::atomic<uint32_t> known[64];
-    int dev = 0, per_cu = 0, cus = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0)
-        return 0;
-    uint32_t have = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0u;
-    if (!have) {
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, reinterpret_cast<const void *>(kernel), (int)threads, 0) != hipSuccess ||
-            hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || per_cu < 1 || cus < 1)
-            return 0;
-        have = (uint32_t)per_cu * (uint32_t)cus;
-        if (dev < 64)
-            known[dev].store(have, std::memory_order_relaxed);
-    }
-    return have;
-}
-
-// f(Type<element>, Type<weight>)
-template <class F>
-int with_types(uint32_t type, uint32_t weight_type, F &&f)
-{
-    return with_type(type, [&](auto t) { return weight_type == type ? f(t, t) : f(t, Type<float>{}); });
 }
 
 bool valid_rows(uint64_t rows, uint32_t hidden, uint32_t type, uint32_t weight_type, const void *weight)

@@ -1,0 +1,103 @@
+"""What dropout's and the residual norm's entry points refuse, on the host and before anything is launched."""
+import pytest
+import torch
+
+import paper_1908_06077_amd as nuq
+
+EINVAL, ECAPACITY = -1, -2
+NAN = float("nan")
+
+
+def _lib():
+    from paper_1908_06077_amd import binding
+    return binding._lib
+
+
+def test_dropout():
+    call = _lib().nuq_dropout
+    ok = dict(x=16, ldx=8, residual=None, ldr=0, rows=2, hidden=8, type=0, p=0.1, seed=1, step=None, y=16, ldy=8, stream=None)
+    assert call(*{**ok, "rows": 0}.values()) == 0 and call(*{**ok, "hidden": 0, "ldy": 0}.values()) == 0      # nothing to do
+    for bad in (dict(x=None), dict(x=18), dict(y=None), dict(y=18), dict(ldy=7), dict(residual=18), dict(type=3), dict(p=-0.1),
+                dict(p=1.1), dict(p=NAN), dict(step=20), dict(rows=2 ** 31), dict(hidden=2 ** 31), dict(x=17, type=1)):
+        assert call(*{**ok, **bad}.values()) == EINVAL, bad
+
+
+FORWARD = dict(x=16, ldx=8, residual=16, ldr=8, inner=1, w1=None, b1=None, gate=None, outer=1, w2=None, b2=None, rows=2, hidden=8, eps=1e-5,
+               scale=1.0, residual_scale=1.0, p=0.1, seed=1, step=None, type=0, weight_type=0, total=16, ldt=8, y=16, ldy=8, stats=16,
+               stream=None)
+BACKWARD = dict(dy=16, ldg=8, dtotal=16, lda=8, x=16, ldx=8, total=16, ldt=8, inner=1, w1=None, b1=None, gate=None, outer=1, w2=None, rows=2,
+                hidden=8, scale=1.0, residual_scale=1.0, p=0.1, seed=1, step=None, type=0, weight_type=0, stats=16, dx=16, ldd=8,
+                dresidual=16, lde=8, dw1=16, db1=16, dgate=16, dw2=16, db2=16, workspace=64, bytes=320, stream=None)
+BOTH = (dict(x=None), dict(x=18), dict(hidden=0), dict(hidden=16385), dict(rows=2 ** 31), dict(type=3), dict(type=1, weight_type=2),
+        dict(inner=3), dict(outer=3), dict(inner=0, outer=0, y=None, dy=None), dict(w1=18), dict(b1=18), dict(gate=18), dict(w2=18),
+        dict(scale=NAN), dict(residual_scale=float("inf")), dict(p=-0.1), dict(p=NAN), dict(p=1.01), dict(step=12), dict(stats=18),
+        dict(inner=0, w1=16), dict(inner=0, b1=16), dict(type=1, weight_type=1, gate=17))
+
+
+def test_residual_norm_forward():
+    call = _lib().nuq_residual_norm_forward
+    assert call(*{**FORWARD, "rows": 0}.values()) == 0                        # nothing to do
+    for bad in BOTH + (dict(total=None), dict(total=18), dict(y=None), dict(y=18), dict(ldt=7), dict(ldy=7), dict(residual=18),
+                       dict(eps=-1.0), dict(eps=NAN), dict(outer=0), dict(outer=0, y=None, w2=16), dict(outer=0, y=None, b2=16),
+                       dict(b2=18)):
+        bad = {k: v for k, v in bad.items() if k in FORWARD}
+        assert call(*{**FORWARD, **bad}.values()) == EINVAL, bad
+
+
+def test_residual_norm_backward():
+    size = nuq.nuq_residual_norm_workspace_bytes
+    assert size(2, 8) == 2 * 8 * 20 and size(10 ** 6, 8) == 1024 * 160 and size(3, 10 ** 4) == 3 * 20 * 10 ** 4 + 24
+    call = _lib().nuq_residual_norm_backward
+    bare = dict(dw1=None, db1=None, dw2=None, db2=None)
+    for bad in BOTH + (dict(dy=None), dict(dy=18), dict(total=None), dict(dx=None), dict(dx=18), dict(ldd=7), dict(lde=7), dict(stats=None),
+                       dict(dresidual=18), dict(dw1=18), dict(db1=18), dict(dgate=18), dict(dw2=18), dict(db2=18), dict(workspace=None),
+                       dict(workspace=72), dict(dtotal=18), {**bare, "outer": 0}, {**bare, "outer": 0, "dy": None, "dtotal": None},
+                       dict(inner=0), dict(outer=0, dy=None)):
+        bad = {k: v for k, v in bad.items() if k in BACKWARD}
+        assert call(*{**BACKWARD, **bad}.values()) == EINVAL, bad
+    wide = dict(hidden=9000, ldg=9000, lda=9000, ldx=9000, ldt=9000, ldd=9000, lde=9000, bytes=10 ** 7, dx=32, dresidual=48)
+    for bad in (dict(dx=16), dict(dresidual=16)):                             # the sums of wide rows: not from rows that were replaced
+        assert call(*{**BACKWARD, **wide, **bad}.values()) == EINVAL, bad
+    assert call(*{**BACKWARD, "bytes": 319}.values()) == ECAPACITY
+
+
+def test_binding_refuses_tensors_that_do_not_fit(monkeypatch):
+    """Host tensors stand in for device tensors: every call here ends in the wrapper."""
+    from paper_1908_06077_amd import binding
+    monkeypatch.setattr(binding, "_on_device", lambda t: True)
+    f = lambda *k: torch.zeros(*k)  # noqa: E731
+    i = torch.zeros(1, dtype=torch.int64)
+
+    def forward(x=f(2, 4), residual=None, w1=None, gate=None, w2=None, step=None, total=f(2, 4), y=f(2, 4), stats=f(4, 2)):
+        nuq.nuq_residual_norm_forward(x, residual, 1, w1, None, gate, 1, w2, None, 1e-5, 1.0, 1.0, 0.1, 3, step, total, y, stats)
+
+    def backward(dy=f(2, 4), dtotal=None, x=f(2, 4), total=f(2, 4), stats=f(4, 2), dx=f(2, 4), dresidual=None, dgate=None):
+        nuq.nuq_residual_norm_backward(dy, dtotal, x, total, 1, None, None, None, 1, None, 1.0, 1.0, 0.1, 3, None, stats, dx, dresidual, None,
+                                       None, dgate, None, None, None)
+    cases = [
+        ("one element or more", lambda: nuq.nuq_dropout(f(2, 0), None, 0.1, 1, None, f(2, 0))),
+        ("residual: expected 2 rows", lambda: nuq.nuq_dropout(f(2, 4), f(2, 5), 0.1, 1, None, f(2, 4))),
+        ("y: expected dtype", lambda: nuq.nuq_dropout(f(2, 4), None, 0.1, 1, None, f(2, 4).half())),
+        ("step: expected dtype", lambda: nuq.nuq_dropout(f(2, 4), None, 0.1, 1, f(1), f(2, 4))),
+        ("step holds 0", lambda: nuq.nuq_dropout(f(2, 4), None, 0.1, 1, i[:0], f(2, 4))),
+        ("expected float32", lambda: nuq.nuq_dropout(f(2, 4).double(), None, 0.1, 1, i, f(2, 4).double())),
+        ("residual: expected dtype", lambda: forward(residual=f(2, 4).half())),
+        ("gate holds 3", lambda: forward(gate=f(3))),
+        ("weight and bias", lambda: forward(w1=f(4).half())),
+        ("outer_weight: expected dtype", lambda: forward(x=f(2, 4).half(), gate=f(4), w2=f(4).half())),
+        ("total: expected 2 rows", lambda: forward(total=f(3, 4))),
+        ("stats holds", lambda: forward(stats=f(3, 2))),
+        ("step: expected dtype", lambda: forward(step=f(1))),
+        ("contiguous rows", lambda: forward(y=f(4, 2).t())),
+        ("dtotal: expected 2 rows", lambda: backward(dtotal=f(1, 4))),
+        ("total: expected dtype", lambda: backward(total=f(2, 4).half())),
+        ("stats is needed|stats holds", lambda: backward(stats=f(2, 2))),
+        ("dresidual: expected", lambda: backward(dresidual=f(2, 3))),
+        ("dgate holds", lambda: backward(dgate=f(5))),
+    ]
+    for want, call in cases:
+        with pytest.raises(ValueError, match=want):
+            call()
+    monkeypatch.undo()
+    with pytest.raises(ValueError, match="device tensor"):
+        forward()

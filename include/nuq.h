@@ -557,6 +557,40 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
                                void *dgate, void *douter_weight, void *douter_bias, void *workspace,
                                uint64_t workspace_bytes, nuq_stream_t stream);
 
+/* ---- the loss of a language model ----------------------------------------------------------------- */
+
+/* Softmax cross entropy of `rows` rows x of `hidden` elements against the `vocab` rows of weight, z = x weight^T, without z in memory.
+ * With t = target[r], e = smoothing, per row
+ *   lse = log sum over v of exp(z_v);   loss = lse - (1 - e) z_t - e mean(z)
+ * and 0 for a row whose target is `ignore`.  A target outside the vocabulary that is not `ignore` makes the row's loss NaN and raises
+ * NUQ_FLAG_MALFORMED.  x, weight: DEVICE, of `type`, element-aligned, row r at r * ld elements (ldx, ldw: any).  target: DEVICE int64.
+ * loss (may be NULL), lse: `rows` floats.  mean (may be NULL): 2 floats, the mean loss over the rows that are not ignored, and 1 / their
+ * number (0 and 1 where there are none).  Products of operands of 16 bits are exact and summed in fp32 on the matrix cores, fp32 operands
+ * are multiplied in fp32; exponentials and sums in fp32, the mean in fp64 in a fixed order.  rows at most 2^20, hidden 2^16, vocab 2^24,
+ * rows * vocab 2^38; smoothing from 0, below 1.  workspace: DEVICE memory of nuq_linear_cross_entropy_workspace_bytes(..., 0) bytes,
+ * 16-byte aligned, overwritten; it holds two or three numbers per row and 64 or 128 entries of the vocabulary, and a copy of x or weight
+ * where 16-byte loads do not take it as it stands (its address, stride or width no multiple of 16 bytes). */
+uint64_t nuq_linear_cross_entropy_workspace_bytes(const void *x, uint64_t ldx, const void *weight, uint64_t ldw,
+                                                  uint64_t rows, uint32_t hidden, uint32_t vocab, uint32_t type,
+                                                  int backward);
+int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *weight, uint64_t ldw, uint64_t rows,
+                                     uint32_t hidden, uint32_t vocab, uint32_t type, const int64_t *target, int64_t ignore,
+                                     float smoothing, float *loss, float *lse, float *mean, void *workspace,
+                                     uint64_t workspace_bytes, nuq_stream_t stream);
+
+/* Its gradients, from the forward's lse:  with g the gradient of a row's loss, 0 where the target is `ignore` or outside the vocabulary,
+ *   d_v = exp(z_v - lse) - e / vocab - (1 - e) [v = t];   dx = g sum over v of d_v weight_v;   dweight_v = sum over rows of g d_v x
+ * dx: rows at ldd >= hidden elements, dweight: vocab rows at lde >= hidden, of `type`, each may be NULL; they must not overlap the
+ * inputs.  g = *grad, or grad[r] where grad_per_row, times mean[1] where there is a mean (the forward's: the gradient of the mean loss).
+ * The logits are made again, a piece of the vocabulary at a time.  d is rounded to `type` (fp16: 2^14 d; dweight: d times g over the
+ * largest |g|), sums are fp32, and results are rounded once.  A row that is ignored takes no part, whatever x holds there.  The order of
+ * all sums is fixed.  workspace: as above, of nuq_linear_cross_entropy_workspace_bytes(..., 1) bytes. */
+int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *weight, uint64_t ldw, uint64_t rows,
+                                      uint32_t hidden, uint32_t vocab, uint32_t type, const int64_t *target,
+                                      int64_t ignore, float smoothing, const float *lse, const float *grad,
+                                      int grad_per_row, const float *mean, void *dx, uint64_t ldd, void *dweight,
+                                      uint64_t lde, void *workspace, uint64_t workspace_bytes, nuq_stream_t stream);
+
 /* ---- errors ---------------------------------------------------------------------- */
 
 /* Waits for `stream`, copies the sticky device flags of the current device to

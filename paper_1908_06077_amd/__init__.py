@@ -22,6 +22,7 @@ from .binding import (  # noqa: F401
     nuq_layer_norm_forward, nuq_layer_norm_backward, nuq_layer_norm_workspace_bytes,
     nuq_dropout, nuq_residual_norm_forward, nuq_residual_norm_backward, nuq_residual_norm_workspace_bytes,
     NO_NORM, LAYER_NORM, RMS_NORM, RESIDUAL_NORM_MAX_HIDDEN,
+    nuq_linear_cross_entropy_forward, nuq_linear_cross_entropy_backward, nuq_linear_cross_entropy_workspace_bytes,
     nuq_last_error_flags, library_path, exported_symbols,
     nuq_encode_shape, nuq_decode_tile, nuq_timing_begin, nuq_timing_collect, T_NORMS, T_QUANTIZE, T_ENCODE, T_QUANTIZE_ENCODE, T_DECODE,
 )

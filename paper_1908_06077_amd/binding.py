@@ -99,6 +99,11 @@ _SIGNATURES = {
     "nuq_residual_norm_backward": (_i32, [_vp, _u64, _vp, _u64, _vp, _u64, _vp, _u64, _u32, _vp, _vp, _vp, _u32, _vp, _u64, _u32,
                                           _f32, _f32, _f64, _u64, _vp, _u32, _u32, _vp, _vp, _u64, _vp, _u64, _vp, _vp, _vp, _vp,
                                           _vp, _vp, _u64, _vp]),
+    "nuq_linear_cross_entropy_workspace_bytes": (_u64, [_vp, _u64, _vp, _u64, _u64, _u32, _u32, _u32, _i32]),
+    "nuq_linear_cross_entropy_forward": (_i32, [_vp, _u64, _vp, _u64, _u64, _u32, _u32, _u32, _vp, ctypes.c_int64, _f32, _vp, _vp, _vp,
+                                                _vp, _u64, _vp]),
+    "nuq_linear_cross_entropy_backward": (_i32, [_vp, _u64, _vp, _u64, _u64, _u32, _u32, _u32, _vp, ctypes.c_int64, _f32, _vp, _vp, _i32,
+                                                 _vp, _vp, _u64, _vp, _u64, _vp, _u64, _vp]),
     "nuq_last_error_flags": (_i32, [_vp, _vp]),
     "nuq_encode_shape": (_i32, [_u32, _u32, _u64, _u32, _u32, _u32, _vp, _u32, _vp]),
     "nuq_decode_tile": (_u32, [_u32, _u64, _u32, _u32, _u32, _i32, _u32]),
@@ -893,6 +898,64 @@ def nuq_residual_norm_backward(dy: torch.Tensor | None, dtotal: torch.Tensor | N
                                            _TYPES[kind], _vector(stats, torch.float32, 4 * rows, "stats"), *_maybe_rows(dx, x, "dx"),
                                            *_maybe_rows(dresidual, x, "dresidual"), *gradients, _ptr(workspace),
                                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+
+
+# ------------------------------------------ the loss of a language model
+
+def _loss_rows(x: torch.Tensor, weight: torch.Tensor):
+    """(x's address and stride, weight's, rows, hidden, vocabulary, type)"""
+    _some_rows(x)
+    if weight.dim() != 2 or weight.shape[0] < 1:
+        raise ValueError("weight: expected rows of the vocabulary, got %s" % (tuple(weight.shape),))
+    hidden = x.shape[-1]
+    return (*_maybe_rows(x, x, "x"), *_rows(weight, x.dtype, weight.shape[0], hidden, "weight"), x.numel() // hidden, hidden,
+            weight.shape[0], _type(x, "x"))
+
+
+def _targets(target: torch.Tensor, rows: int) -> int:
+    if target.numel() != rows:
+        raise ValueError("target holds %d elements, %d are needed" % (target.numel(), rows))
+    return _ptr(target, torch.int64, 0, "target")
+
+
+def nuq_linear_cross_entropy_workspace_bytes(x: torch.Tensor, weight: torch.Tensor, backward: bool) -> int:
+    return _lib.nuq_linear_cross_entropy_workspace_bytes(*_loss_rows(x, weight), int(backward))
+
+
+def nuq_linear_cross_entropy_forward(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, ignore: int, smoothing: float,
+                                     loss: torch.Tensor | None, lse: torch.Tensor, mean: torch.Tensor | None,
+                                     workspace: torch.Tensor) -> None:
+    """loss, lse <- softmax cross entropy of x weight^T and its log-sum-exp, per row; mean <- the mean loss, 1 / rows that count."""
+    code = _calls.linear_cross_entropy_forward(x, weight, target, ignore, smoothing, loss, lse, mean, workspace)
+    if code is not None:
+        return _check("nuq_linear_cross_entropy_forward", code)
+    shape = _loss_rows(x, weight)
+    rows = shape[4]
+    _check("nuq_linear_cross_entropy_forward",
+           _lib.nuq_linear_cross_entropy_forward(*shape, _targets(target, rows), ignore, float(smoothing),
+                                                 _vector(loss, torch.float32, rows, "loss"), _vector(lse, torch.float32, rows, "lse"),
+                                                 _vector(mean, torch.float32, 2, "mean"), _ptr(workspace),
+                                                 workspace.numel() * workspace.element_size(), _stream()))
+
+
+def nuq_linear_cross_entropy_backward(x: torch.Tensor, weight: torch.Tensor, target: torch.Tensor, ignore: int, smoothing: float,
+                                      lse: torch.Tensor, grad: torch.Tensor, mean: torch.Tensor | None, dx: torch.Tensor | None,
+                                      dweight: torch.Tensor | None, workspace: torch.Tensor) -> None:
+    """dx, dweight <- the gradients of rows and weights; grad: of the loss, one number or one per row, times mean[1] where given."""
+    code = _calls.linear_cross_entropy_backward(x, weight, target, ignore, smoothing, lse, grad, mean, dx, dweight, workspace)
+    if code is not None:
+        return _check("nuq_linear_cross_entropy_backward", code)
+    shape = _loss_rows(x, weight)
+    rows, hidden, vocab = shape[4:7]
+    if grad.numel() not in (1, rows):
+        raise ValueError("grad holds %d elements, 1 or %d are needed" % (grad.numel(), rows))
+    pw, ldw = _rows(dweight, x.dtype, vocab, hidden, "dweight") if dweight is not None else (0, 0)
+    _check("nuq_linear_cross_entropy_backward",
+           _lib.nuq_linear_cross_entropy_backward(*shape, _targets(target, rows), ignore, float(smoothing),
+                                                  _vector(lse, torch.float32, rows, "lse"), _ptr(grad, torch.float32, 0, "grad"),
+                                                  int(grad.numel() != 1), _vector(mean, torch.float32, 2, "mean"),
+                                                  *_maybe_rows(dx, x, "dx"), pw, ldw, _ptr(workspace),
+                                                  workspace.numel() * workspace.element_size(), _stream()))
 
 
 def nuq_last_error_flags() -> int:

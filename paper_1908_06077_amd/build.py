@@ -8,7 +8,7 @@ import subprocess
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(HERE, "csrc", x) for x in ("nuq.hip", "nuq_train.hip", "nuq_block.hip")]
+SRCS = [os.path.join(HERE, "csrc", x) for x in ("nuq.hip", "nuq_train.hip", "nuq_block.hip", "nuq_loss.hip")]
 LIB = os.path.join(HERE, "libnuq.so")
 CALLS_SRC = os.path.join(HERE, "csrc", "nuq_calls.cpp")
 CALLS = os.path.join(HERE, "_nuq_calls" + sysconfig.get_config_var("EXT_SUFFIX"))       # it serves one Python only, and one torch

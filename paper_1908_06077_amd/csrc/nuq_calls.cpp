@@ -34,7 +34,7 @@ PyObject *g_norms, *g_bit_off, *g_words, *g_sync;                   // attribute
     X(nuq_quantize_encode_huffman_batch) X(nuq_decode_accumulate_huffman) X(nuq_moments_accumulate)                  \
     X(nuq_gradient_norm) X(nuq_adamw_step) X(nuq_adamw_step_coded) X(nuq_state_blocks) X(nuq_layer_norm_forward)     \
     X(nuq_layer_norm_backward) X(nuq_adamw_state_values) X(nuq_dropout) X(nuq_residual_norm_forward)                 \
-    X(nuq_residual_norm_backward)
+    X(nuq_residual_norm_backward) X(nuq_linear_cross_entropy_forward) X(nuq_linear_cross_entropy_backward)
 #define NUQ_POINTER(name) decltype(&::name) p_##name = nullptr;
 NUQ_CALLS(NUQ_POINTER)
 
@@ -656,6 +656,53 @@ PyObject *residual_norm_backward(PyObject *const *a)
                   dx.ld, dresidual.p, dresidual.ld, dw1.p, db1.p, dgate.p, dw2.p, db2.p, ws, bytes);
 }
 
+int64_t number(PyObject *o)
+{
+    need(PyLong_CheckExact(o));
+    const long long x = PyLong_AsLongLong(o);
+    need(!PyErr_Occurred());
+    return x;
+}
+
+// Rows and the vocabulary's, of one width and type.
+struct LossRows {
+    Rows x, w;
+    LossRows(PyObject *x_, PyObject *w_) : x(x_, nullptr), w(w_, nullptr)
+    {
+        need(x.hidden > 0 && w.hidden == x.hidden && w.type == x.type && w.rows > 0 && w.rows <= UINT32_MAX);
+        need(THPVariable_Unpack(w_).dim() == 2);
+    }
+    uint32_t vocab() const { return (uint32_t)w.rows; }
+};
+
+// x, weight, target, ignore, smoothing, loss, lse, mean, workspace
+PyObject *linear_cross_entropy_forward(PyObject *const *a)
+{
+    const LossRows r(a[0], a[1]);
+    const Vector loss(a[5], r.x.rows), lse(a[6], r.x.rows), mean(a[7], 2);
+    need(lse.there);
+    const Bytes ws(a[8]);
+    return launch(p_nuq_linear_cross_entropy_forward, r.x.p, r.x.ld, r.w.p, r.w.ld, r.x.rows, r.x.hidden, r.vocab(), type_of(r.x.type),
+                  exactly<const int64_t>(a[2], at::kLong, r.x.rows), number(a[3]), (float)real(a[4]), loss.floats(), lse.floats(),
+                  mean.floats(), ws.p, ws.n);
+}
+
+// x, weight, target, ignore, smoothing, lse, grad, mean, dx, dweight, workspace
+PyObject *linear_cross_entropy_backward(PyObject *const *a)
+{
+    const LossRows r(a[0], a[1]);
+    const Vector lse(a[5], r.x.rows), mean(a[7], 2);
+    need(lse.there);
+    uint64_t grads;
+    const float *const grad = address<const float>(a[6], at::kFloat, 0, &grads);
+    need(grads == 1 || grads == r.x.rows);
+    const Rows dx(a[8], &r.x), dw(a[9], &r.w);
+    const Bytes ws(a[10]);
+    return launch(p_nuq_linear_cross_entropy_backward, r.x.p, r.x.ld, r.w.p, r.w.ld, r.x.rows, r.x.hidden, r.vocab(), type_of(r.x.type),
+                  exactly<const int64_t>(a[2], at::kLong, r.x.rows), number(a[3]), (float)real(a[4]), lse.floats(), grad,
+                  (int)(grads != 1), mean.floats(), dx.p, dx.ld, dw.p, dw.ld, ws.p, ws.n);
+}
+
 // bind(addresses of the entry points in NUQ_CALLS' order, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -713,6 +760,8 @@ PyMethodDef g_methods[] = {
     NUQ_METHOD(dropout, 6),
     NUQ_METHOD(residual_norm_forward, 18),
     NUQ_METHOD(residual_norm_backward, 24),
+    NUQ_METHOD(linear_cross_entropy_forward, 9),
+    NUQ_METHOD(linear_cross_entropy_backward, 11),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nuq_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,358 @@
+// C ABI of softmax cross entropy over a large vocabulary (see include/nuq.h): argument checks, the workspace, pieces of the vocabulary
+// and launches.  A source file of its own, so that it is built beside the others.
+#include "../../include/nuq.h"
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "nuq_loss_kernels.hpp"
+#include "nuq_train_host.hpp"
+
+namespace {
+
+using namespace nuq;
+
+constexpr uint32_t kMostLossRows = 1u << 20, kMostHidden = 1u << 16, kMostVocab = 1u << 24;
+constexpr uint64_t kMostTiles = 1ull << 22;                  // of a launch: fewer than 2^32 threads
+
+uint64_t up(uint64_t n, uint64_t m) { return (n + m - 1) / m * m; }
+uint32_t over(uint64_t n, uint64_t m) { return (uint32_t)((n + m - 1) / m); }
+
+struct LossShape {
+    const void *x, *w;
+    uint64_t ldx, ldw;
+    uint32_t rows, hidden, vocab, type;
+
+    bool valid(uint64_t all_rows) const
+    {
+        return all_rows <= kMostLossRows && hidden >= 1 && hidden <= kMostHidden && vocab >= 1 && vocab <= kMostVocab && type <= NUQ_F16 &&
+               (uint64_t)rows * vocab <= 1ull << 38;
+    }
+    uint32_t bytes() const { return width(type); }
+    // Whether loads of 16 bytes take the rows as they stand.
+    bool whole(const void *p, uint64_t ld) const
+    {
+        return !off_grid(p, 16) && ld * bytes() % 16u == 0 && hidden * bytes() % 16u == 0 && ld * bytes() < 1u << 22;
+    }
+    bool pack_x() const { return !whole(x, ldx); }
+    bool pack_w() const { return !whole(w, ldw); }
+    uint64_t packed() const { return up(hidden, 64); }       // elements of a packed row
+    uint64_t padded_rows() const { return up(rows, 64); }
+};
+
+// Parts of a workspace one after the other, each at a multiple of 256 bytes.
+struct Parts {
+    char *base;
+    uint64_t used = 0;
+    template <class T>
+    T *take(uint64_t n)
+    {
+        T *const p = reinterpret_cast<T *>(base + used);
+        used = up(used + n * sizeof(T), 256);
+        return p;
+    }
+};
+
+// Columns of rows that a workgroup takes, and the logits' groups: of 64 of the vocabulary where a wave has all of the rows.
+uint32_t group_of(uint32_t rows) { return rows <= 64 ? 64 : 128; }
+
+struct ForwardParts {
+    char *x, *w;
+    float2 *part;
+    float *sums, *of_target, *row_loss;
+    uint32_t groups;
+    uint64_t used;
+    ForwardParts(const LossShape &S, void *workspace, bool smooth)
+    {
+        Parts P{static_cast<char *>(workspace)};
+        x = P.take<char>(S.pack_x() ? S.rows * S.packed() * S.bytes() : 0);
+        w = P.take<char>(S.pack_w() ? S.vocab * S.packed() * S.bytes() : 0);
+        groups = over(S.vocab, group_of(S.rows));
+        part = P.take<float2>((uint64_t)groups * S.rows);
+        sums = P.take<float>(smooth ? (uint64_t)groups * S.rows : 0);
+        of_target = P.take<float>(S.rows);
+        row_loss = P.take<float>(S.rows);
+        used = P.used;
+    }
+};
+
+// How many ways a product whose tiles leave CUs idle splits its depth (`steps` of it): as many workgroups as fill whole rounds of 256,
+// three hundredths of the time for another set of sums to write and add.
+uint32_t splits_of(uint64_t tiles, uint32_t steps, uint32_t most_splits)
+{
+    uint32_t best = 1;
+    double most = 0.0;
+    for (uint32_t s = 1; s <= std::max(1u, std::min(most_splits, steps / 8u)); ++s) {
+        const double used = (double)(tiles * s) / (double)((tiles * s + 255u) / 256u * 256u) / (1.0 + 0.03 * (s - 1));
+        if (used > most * 1.001) {
+            most = used;
+            best = s;
+        }
+    }
+    return best;
+}
+
+// A piece of the vocabulary: d, once by rows and once by the vocabulary, stays in the last-level cache between the launch that writes
+// it and the products that read it, and is wide enough to fill the device.
+uint32_t piece_of(const LossShape &S)
+{
+    const uint64_t fits = (160ull << 20) / (2u * S.padded_rows() * S.bytes()) / 256u * 256u;
+    const uint64_t most = std::min<uint64_t>(std::max<uint64_t>(fits, 2048u), 1u << 20), pieces = over(S.vocab, most);
+    return (uint32_t)std::min<uint64_t>(up(over(S.vocab, pieces), 256u), up(S.vocab, 64));
+}
+
+uint32_t tile_rows(uint32_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+
+struct BackwardParts {
+    char *x, *w, *d, *dt, *xt, *wt;
+    int32_t *code;
+    float *factor, *scale, *largest, *sums;
+    uint32_t piece, splits, each;
+    uint64_t ld_sums, used;
+    BackwardParts(const LossShape &S, void *workspace)
+    {
+        Parts P{static_cast<char *>(workspace)};
+        const uint64_t R = S.padded_rows(), b = S.bytes();
+        piece = piece_of(S);
+        const uint64_t wide = up(piece, 64);
+        x = P.take<char>(S.pack_x() ? S.rows * S.packed() * b : 0);
+        w = P.take<char>(S.pack_w() ? S.vocab * S.packed() * b : 0);
+        code = P.take<int32_t>(R);
+        factor = P.take<float>(R);
+        scale = P.take<float>(R);
+        largest = P.take<float>(1);
+        xt = P.take<char>(S.hidden * R * b);
+        wt = P.take<char>(S.hidden * wide * b);
+        d = P.take<char>(R * wide * b);
+        dt = P.take<char>(R * wide * b);
+        const uint32_t steps = over(wide * b, 128);
+        splits = splits_of((uint64_t)over(S.hidden, S.rows > 128 && S.hidden <= 128 ? 128 : 256) * over(S.rows, tile_rows(S.rows)), steps,
+                           1u + (uint32_t)std::min<uint64_t>(63u, (4ull << 20) / (4u * S.rows * up(S.hidden, 4))));
+        each = over(steps, splits) * 8u;                     // chunks
+        ld_sums = up(S.hidden, 4);
+        sums = P.take<float>(splits * S.rows * ld_sums);
+        used = P.used;
+    }
+};
+
+// f(Type<tile>) for a product of many columns, by its rows, and for one of many rows, by its columns.
+template <class T, class F>
+int with_rows(uint32_t rows, F &&f)
+{
+    return rows > 128  ? f(Type<ProductTile<T, 256, 256, 2, 4>>{})
+           : rows > 64 ? f(Type<ProductTile<T, 256, 128, 2, 2>>{})
+           : rows > 32 ? f(Type<ProductTile<T, 256, 64, 4, 1>>{})
+                       : f(Type<ProductTile<T, 256, 32, 4, 1>>{});
+}
+template <class T, class F>
+int with_columns(uint32_t columns, F &&f)
+{
+    return columns > 128 ? f(Type<ProductTile<T, 256, 256, 2, 4>>{}) : f(Type<ProductTile<T, 128, 256, 2, 4>>{});
+}
+
+template <class T>
+int pack(const void *from, uint64_t ld, uint64_t rows, uint32_t columns, char *to, uint64_t to_ld, hipStream_t st)
+{
+    const uint64_t vectors = rows * (to_ld * sizeof(T) / 16u);
+    hipLaunchKernelGGL(k_loss_pack<T>, dim3((uint32_t)std::min<uint64_t>((vectors + 255u) / 256u, 16384u)), dim3(256), 0, st,
+                       static_cast<const T *>(from), ld, rows, columns, reinterpret_cast<T *>(to), (uint32_t)to_ld);
+    return check_launch();
+}
+
+template <class T>
+int transpose(const void *from, uint64_t ld, uint32_t rows, uint32_t columns, const int32_t *code, char *to, uint64_t to_ld, hipStream_t st)
+{
+    hipLaunchKernelGGL(k_loss_transpose<T>, dim3((columns + 63u) / 64u, (uint32_t)(to_ld / 64u)), dim3(256), 0, st,
+                       static_cast<const T *>(from), ld, rows, columns, code, reinterpret_cast<T *>(to), (uint32_t)to_ld);
+    return check_launch();
+}
+
+// The rows and weights as the products take them: packed into the workspace where they do not stand so.
+template <class T>
+int operands(const LossShape &S, char *x, char *w, LossOperands &O, hipStream_t st)
+{
+    O = {S.x, S.w, (uint32_t)(S.ldx * sizeof(T)), (uint32_t)(S.ldw * sizeof(T)), over((uint64_t)S.hidden * sizeof(T), 16), S.rows, S.vocab, 0, 0};
+    if (S.pack_x()) {
+        if (const int rc = pack<T>(S.x, S.ldx, S.rows, S.hidden, x, S.packed(), st); rc != NUQ_OK)
+            return rc;
+        O.x = x;
+        O.stride_x = (uint32_t)(S.packed() * sizeof(T));
+    }
+    if (S.pack_w()) {
+        if (const int rc = pack<T>(S.w, S.ldw, S.vocab, S.hidden, w, S.packed(), st); rc != NUQ_OK)
+            return rc;
+        O.w = w;
+        O.stride_w = (uint32_t)(S.packed() * sizeof(T));
+    }
+    return NUQ_OK;
+}
+
+bool valid_loss(const LossShape &S, uint64_t rows, const int64_t *target, float smoothing, const float *lse, const void *workspace)
+{
+    if (!S.valid(rows) || !(smoothing >= 0.0f && smoothing < 1.0f) || !valid_array(S.w, 1, S.bytes()))
+        return false;
+    return rows == 0 || (valid_array(S.x, 1, S.bytes()) && valid_array(target, 1, 8) && valid_array(lse, 1, 4) &&
+                         valid_array(workspace, 1, 16));
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t nuq_linear_cross_entropy_workspace_bytes(const void *x, uint64_t ldx, const void *weight, uint64_t ldw, uint64_t rows,
+                                                  uint32_t hidden, uint32_t vocab, uint32_t type, int backward)
+{
+    const LossShape S{x, weight, ldx, ldw, (uint32_t)rows, hidden, vocab, type};
+    if (!S.valid(rows) || rows == 0)
+        return 0;
+    return backward ? BackwardParts(S, nullptr).used : ForwardParts(S, nullptr, true).used;
+}
+
+int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *weight, uint64_t ldw, uint64_t rows, uint32_t hidden,
+                                     uint32_t vocab, uint32_t type, const int64_t *target, int64_t ignore, float smoothing, float *loss,
+                                     float *lse, float *mean, void *workspace, uint64_t workspace_bytes, nuq_stream_t stream)
+{
+    const LossShape S{x, weight, ldx, ldw, (uint32_t)rows, hidden, vocab, type};
+    if (!valid_loss(S, rows, target, smoothing, lse, workspace) || off_grid(loss, 4) || off_grid(mean, 4))
+        return NUQ_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    LossJoin J{target, nullptr, nullptr, nullptr, loss, lse, loss, mean, flags_ptr(), ignore, S.rows, vocab, 0, smoothing};
+    if (!J.flags)
+        return NUQ_EHIP;
+    if (rows == 0) {
+        if (mean)
+            hipLaunchKernelGGL(k_loss_mean, dim3(1), dim3(1024), 0, st, J);
+        return check_launch();
+    }
+    const bool smooth = smoothing > 0.0f;
+    const ForwardParts W(S, workspace, smooth);
+    if (workspace_bytes < W.used)
+        return NUQ_ECAPACITY;
+    int rc = with_type(type, [&](auto tt) {
+        using T = typename decltype(tt)::type;
+        LossForward P{{}, target, W.part, W.sums, W.of_target};
+        if (const int done = operands<T>(S, W.x, W.w, P.O, st); done != NUQ_OK)
+            return done;
+        return with_rows<T>(S.rows, [&](auto tile) {
+            using Tile = typename decltype(tile)::type;
+            P.O.mt = over(vocab, Tile::BM);
+            P.O.nt = over(rows, Tile::BN);
+            const dim3 grid(P.O.mt * P.O.nt);
+            if (smooth)
+                hipLaunchKernelGGL((k_loss_logits<T, Tile, true>), grid, dim3(Tile::THREADS), 0, st, P);
+            else
+                hipLaunchKernelGGL((k_loss_logits<T, Tile, false>), grid, dim3(Tile::THREADS), 0, st, P);
+            return check_launch();
+        });
+    });
+    if (rc != NUQ_OK)
+        return rc;
+    J.part = W.part;
+    J.sums = smooth ? W.sums : nullptr;
+    J.of_target = W.of_target;
+    J.row_loss = loss ? loss : W.row_loss;
+    J.groups = W.groups;
+    if (rows <= 16) {
+        hipLaunchKernelGGL(k_loss_join<true>, dim3(1), dim3(1024), 0, st, J);
+        return check_launch();
+    }
+    hipLaunchKernelGGL(k_loss_join<false>, dim3(over(rows, 16)), dim3(1024), 0, st, J);
+    if (mean)
+        hipLaunchKernelGGL(k_loss_mean, dim3(1), dim3(1024), 0, st, J);
+    return check_launch();
+}
+
+int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *weight, uint64_t ldw, uint64_t rows, uint32_t hidden,
+                                      uint32_t vocab, uint32_t type, const int64_t *target, int64_t ignore, float smoothing,
+                                      const float *lse, const float *grad, int grad_per_row, const float *mean, void *dx, uint64_t ldd,
+                                      void *dweight, uint64_t lde, void *workspace, uint64_t workspace_bytes, nuq_stream_t stream)
+{
+    const LossShape S{x, weight, ldx, ldw, (uint32_t)rows, hidden, vocab, type};
+    const uint32_t b = width(type);
+    if (!valid_loss(S, rows, target, smoothing, lse, workspace) || (rows > 0 && !valid_array(grad, 1, 4)) || off_grid(mean, 4) ||
+        off_grid(dx, b) || off_grid(dweight, b) || (dx && rows > 1 && ldd < hidden) || (dweight && vocab > 1 && lde < hidden))
+        return NUQ_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    LossRows R{target, grad, mean, nullptr, nullptr, nullptr, nullptr, flags_ptr(), ignore, S.rows, (uint32_t)S.padded_rows(), vocab,
+               grad_per_row != 0, type == NUQ_F16 ? 1.0f / kGradientScale<_Float16> : 1.0f};
+    if (!R.flags)
+        return NUQ_EHIP;
+    if (rows == 0)                                           // sums over no rows
+        return !dweight ? (int)NUQ_OK : with_type(type, [&](auto tt) {
+            using T = typename decltype(tt)::type;
+            using Tile = ProductTile<T, 256, 256, 2, 4>;
+            LossProduct P{weight, weight, 16, 16, 0, 0, hidden, vocab, over(hidden, Tile::BM), over(vocab, Tile::BN), dweight, lde, 0, nullptr};
+            hipLaunchKernelGGL((k_loss_product<T, Tile, T, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
+            return check_launch();
+        });
+    const BackwardParts W(S, workspace);
+    if (workspace_bytes < W.used)
+        return NUQ_ECAPACITY;
+    if (!dx && !dweight)
+        return NUQ_OK;
+    R.code = W.code;
+    R.factor = W.factor;
+    R.scale = W.scale;
+    R.largest = W.largest;
+    hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(1024), 0, st, R);
+    if (const int rc = check_launch(); rc != NUQ_OK)
+        return rc;
+    return with_type(type, [&](auto tt) {
+        using T = typename decltype(tt)::type;
+        LossGradient G{{}, W.code, W.factor, lse, W.d, W.dt, 0, R.padded, 0, smoothing / (float)vocab, 1.0f - smoothing};
+        int rc = operands<T>(S, W.x, W.w, G.O, st);
+        if (rc == NUQ_OK && dweight)
+            rc = transpose<T>(x, ldx, S.rows, hidden, W.code, W.xt, R.padded, st);
+        const char *const all = static_cast<const char *>(G.O.w);
+        for (uint32_t first = 0; rc == NUQ_OK && first < vocab; first += W.piece) {
+            const uint32_t here = std::min(W.piece, vocab - first);
+            G.first = first;
+            G.O.w = all + (uint64_t)first * G.O.stride_w;
+            G.O.vocab = here;
+            G.padded_vocab = (uint32_t)up(here, 64);
+            rc = with_rows<T>(S.rows, [&](auto tile) {
+                using Tile = typename decltype(tile)::type;
+                G.O.mt = over(here, Tile::BM);
+                G.O.nt = over(R.padded, Tile::BN);
+                hipLaunchKernelGGL((k_loss_gradient<T, Tile>), dim3(G.O.mt * G.O.nt), dim3(Tile::THREADS), 0, st, G);
+                return check_launch();
+            });
+            if (rc == NUQ_OK && dweight)
+                rc = with_columns<T>(hidden, [&](auto tile) {
+                    using Tile = typename decltype(tile)::type;
+                    const uint32_t stride = R.padded * (uint32_t)sizeof(T);
+                    LossProduct P{W.xt, W.dt, stride, stride, stride / 16u, stride / 16u, hidden, here, over(hidden, Tile::BM),
+                                  over(here, Tile::BN), static_cast<T *>(dweight) + first * lde, lde, 0, W.largest};
+                    hipLaunchKernelGGL((k_loss_product<T, Tile, T, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
+                    return check_launch();
+                });
+            if (rc == NUQ_OK && dx)
+                rc = transpose<T>(static_cast<const T *>(weight) + first * ldw, ldw, here, hidden, nullptr, W.wt, G.padded_vocab, st);
+            if (rc == NUQ_OK && dx) {
+                const auto product = [&](auto tile) {
+                    using Tile = typename decltype(tile)::type;
+                    const uint32_t stride = G.padded_vocab * (uint32_t)sizeof(T);
+                    LossProduct P{W.wt, W.d, stride, stride, stride / 16u, W.each, hidden, S.rows, over(hidden, Tile::BM),
+                                  over(rows, Tile::BN), W.sums, W.ld_sums, rows * W.ld_sums, nullptr};
+                    const dim3 grid(P.mt * P.nt * W.splits);
+                    if (first)
+                        hipLaunchKernelGGL((k_loss_product<T, Tile, float, true>), grid, dim3(Tile::THREADS), 0, st, P);
+                    else
+                        hipLaunchKernelGGL((k_loss_product<T, Tile, float, false>), grid, dim3(Tile::THREADS), 0, st, P);
+                    return check_launch();
+                };
+                rc = rows > 128 ? with_columns<T>(hidden, product) : with_rows<T>(S.rows, product);
+            }
+        }
+        if (rc == NUQ_OK && dx) {
+            const uint64_t vectors = rows * over(hidden, 4);
+            hipLaunchKernelGGL(k_loss_rows_gradient<T>, dim3((uint32_t)std::min<uint64_t>((vectors + 255u) / 256u, 16384u)), dim3(256), 0, st,
+                               W.sums, W.ld_sums, rows * W.ld_sums, W.splits, W.code, W.scale, S.rows, hidden, static_cast<T *>(dx), ldd);
+            rc = check_launch();
+        }
+        return rc;
+    });
+}
+
+}  // extern "C"

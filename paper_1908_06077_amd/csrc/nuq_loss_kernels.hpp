@@ -1,0 +1,441 @@
+// Softmax cross entropy of rows x against the weights w of a large vocabulary, with its gradients; the logits z = x w^T are never in
+// memory.
+//
+//   lse = log sum over v of exp(z_v);  loss = lse - (1 - e) z_t - e mean(z)          (t the target, e the smoothing)
+//   d_v = exp(z_v - lse) - e / V - (1 - e) [v = t];  dx = g d w;  dw = sum over rows of g d x        (g the loss's gradient)
+//
+// Forward a workgroup makes a tile of logits on the matrix cores and leaves two numbers per row and group of the vocabulary, the
+// largest logit and the sum of exp(z - largest); a second launch joins them.  Backward the vocabulary goes through in pieces: a
+// launch makes a piece's logits again and writes d, rounded to the operands' type (its products sum over rows or the vocabulary in
+// fp32, and a rounding of 2^-9 or 2^-12 of each term is what the operands have too); two products take it to dx and dw.
+// Bound by the matrix cores: 2 N V H operations forward, 6 N V H backward; on few rows by reading w.
+#pragma once
+
+#include "nuq_product_device.hpp"
+#include "nuq_train_device.hpp"
+
+namespace nuq {
+
+constexpr float kLog2E = 1.44269504088896340736f;
+
+// What d is multiplied with before it is rounded: of a vocabulary of 50000 most d are near 2^-16, where fp16 has two bits left.
+template <class T>
+constexpr float kGradientScale = __is_same(T, _Float16) ? 0x1p14f : 1.0f;
+
+// Rows of the caller or of the workspace: stride in bytes, a multiple of 16.
+struct LossOperands {
+    const void *x, *w;
+    uint32_t stride_x, stride_w, chunks;       // chunks: 16-byte pieces of a row
+    uint32_t rows, vocab;
+    uint32_t mt, nt;                           // tiles
+};
+
+struct LossForward {
+    LossOperands O;
+    const int64_t *target;
+    float2 *part;                              // [groups][rows]: largest logit, sum of exp(z - largest)
+    float *sums;                               // [groups][rows]: sum of logits, where targets are smoothed
+    float *of_target;                          // [rows]: the target's logit
+};
+
+// The tile's rows of the vocabulary, and of x: none behind the last.
+template <class Tile>
+__device__ __forceinline__ void logits_tile(Tile &tile, const LossOperands &O, uint32_t m0, uint32_t n0, char *lds)
+{
+    tile.run({static_cast<const char *>(O.w) + (uint64_t)m0 * O.stride_w, O.stride_w, min((uint32_t)Tile::BM, O.vocab - m0)},
+             {static_cast<const char *>(O.x) + (uint64_t)n0 * O.stride_x, O.stride_x, n0 < O.rows ? min((uint32_t)Tile::BN, O.rows - n0) : 0u},
+             O.chunks, lds);
+}
+
+// The sum of exp(z - base) needs a base that is finite.
+__device__ __forceinline__ float finite_base(float top) { return __builtin_isinf(top) ? 0.0f : top; }
+
+// f(m of the wave's rows, block, register) for the sixteen values of a block, m in 0 .. BM / WM - 1 less four times the lane's half.
+template <class F>
+__device__ __forceinline__ void for_block(int i, F &&f)
+{
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        f((uint32_t)(i * 32 + r / 4 * 8 + r % 4), r);
+}
+
+template <class T, class Tile, bool kSmooth>
+__global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward P)
+{
+    __shared__ __align__(16) char lds[Tile::LDS];
+    uint32_t bm, bn;
+    tile_of(blockIdx.x, P.O.mt, P.O.nt, bm, bn);
+    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN;
+    Tile tile;
+    logits_tile(tile, P.O, m0, n0, lds);
+    constexpr uint32_t GROUP = Tile::BM / Tile::WM;
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u)), half = lane / 32u * 4u;
+    const uint32_t mw = m0 + wave / Tile::WN * GROUP;
+    if (mw >= P.O.vocab)
+        return;
+    const uint32_t there = min(GROUP, P.O.vocab - mw);
+    const uint64_t group = mw / GROUP;
+#pragma unroll
+    for (int j = 0; j < Tile::NI; ++j) {
+        const uint32_t n = n0 + wave % Tile::WN * (Tile::BN / Tile::WN) + j * 32u + lane % 32u;
+        const bool row = n < P.O.rows;
+        const int64_t target = row ? P.target[n] : -1;
+        const uint32_t at = (uint64_t)target - mw < there ? (uint32_t)((uint64_t)target - mw) : ~0u;
+        float top = -__builtin_inff(), sum = 0.0f, all = 0.0f, wanted = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Tile::MI; ++i)
+            for_block(i, [&](uint32_t m, int r) {
+                float z = tile.acc[i][j][r];
+                m += half;
+                if (m == at)
+                    wanted = z;
+                if constexpr (kSmooth)
+                    all += m < there ? z : 0.0f;
+                if (there < GROUP)
+                    tile.acc[i][j][r] = z = m < there ? z : -__builtin_inff();
+                top = fmaxf(top, z);
+            });
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float base = finite_base(top);
+#pragma unroll
+        for (int i = 0; i < Tile::MI; ++i)
+            for_block(i, [&](uint32_t, int r) { sum += __builtin_amdgcn_exp2f((tile.acc[i][j][r] - base) * kLog2E); });
+        sum += __shfl_xor(sum, 32, 64);
+        if constexpr (kSmooth)
+            all += __shfl_xor(all, 32, 64);
+        if (row && at != ~0u && (at & 4u) == half)
+            P.of_target[n] = wanted;
+        if (row && half == 0u) {
+            P.part[group * P.O.rows + n] = make_float2(top, sum);
+            if constexpr (kSmooth)
+                P.sums[group * P.O.rows + n] = all;
+        }
+    }
+}
+
+struct LossJoin {
+    const int64_t *target;
+    const float2 *part;
+    const float *sums, *of_target;             // sums: where targets are smoothed
+    float *loss, *lse;                         // loss: may be none
+    float *row_loss;                           // workspace, may be loss
+    float *mean;                               // [2], may be none: the mean loss, and 1 / rows that count
+    uint32_t *flags;
+    int64_t ignore;
+    uint32_t rows, vocab, groups;
+    float smoothing;
+};
+
+// The mean over the rows that count, in a fixed order in fp64, by one workgroup of 1024.
+__device__ __forceinline__ void loss_mean(const LossJoin &P)
+{
+    __shared__ double red[2][16];
+    double sum = 0.0, count = 0.0;
+    for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u)
+        if (P.target[n] != P.ignore) {
+            sum += (double)P.row_loss[n];
+            count += 1.0;
+        }
+    sum = workgroup_sum<1024>(sum, red[0]);
+    count = workgroup_sum<1024>(count, red[1]);
+    if (threadIdx.x == 0) {
+        const double part = count > 0.0 ? 1.0 / count : 1.0;
+        P.mean[0] = (float)(sum * part);
+        P.mean[1] = (float)part;
+    }
+}
+
+// Sixteen rows per workgroup, 64 threads to each.  kAlone: there are no more rows, and the mean is taken here.
+template <bool kAlone>
+__global__ __launch_bounds__(1024) void k_loss_join(const LossJoin P)
+{
+    __shared__ float tops[64][17], sums[64][17], alls[64][17];
+    const uint32_t r = threadIdx.x % 16u, of = threadIdx.x / 16u, n = blockIdx.x * 16u + r;
+    const bool row = n < P.rows;
+    float top = -__builtin_inff(), sum = 0.0f, all = 0.0f;
+    if (row)
+        for (uint32_t g = of; g < P.groups; g += 64u) {
+            const float2 p = P.part[(uint64_t)g * P.rows + n];
+            const float higher = fmaxf(top, p.x), base = finite_base(higher);
+            sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2E) + p.y * __builtin_amdgcn_exp2f((p.x - base) * kLog2E);
+            top = higher;
+            if (P.sums)
+                all += P.sums[(uint64_t)g * P.rows + n];
+        }
+    tops[of][r] = top;
+    sums[of][r] = sum;
+    alls[of][r] = all;
+    __syncthreads();
+    if (of == 0 && row) {
+        for (uint32_t k = 1; k < 64u; ++k)
+            top = fmaxf(top, tops[k][r]);
+        const float base = finite_base(top);
+        float total = 0.0f, logits = 0.0f;
+        for (uint32_t k = 0; k < 64u; ++k) {
+            total += sums[k][r] * __builtin_amdgcn_exp2f((tops[k][r] - base) * kLog2E);
+            logits += alls[k][r];
+        }
+        const float lse = top == __builtin_inff() && total == total ? top : base + logf(total);
+        const int64_t t = P.target[n];
+        float loss = 0.0f;
+        if (t != P.ignore) {
+            if (t >= 0 && t < (int64_t)P.vocab) {
+                loss = (1.0f - P.smoothing) * (lse - P.of_target[n]);
+                if (P.sums)
+                    loss += P.smoothing * (lse - logits / (float)P.vocab);
+            } else {
+                loss = __builtin_nanf("");
+                atomicOr(P.flags, (uint32_t)NUQ_FLAG_MALFORMED);
+            }
+        }
+        P.lse[n] = lse;
+        P.row_loss[n] = loss;
+        if (P.loss)
+            P.loss[n] = loss;
+    }
+    if constexpr (kAlone) {
+        if (!P.mean)
+            return;
+        __syncthreads();                                     // (one workgroup: it reads what it wrote)
+        loss_mean(P);
+    }
+}
+
+__global__ __launch_bounds__(1024) void k_loss_mean(const LossJoin P) { loss_mean(P); }
+
+// Per row what the gradients need: the target, or -1 for a row without one; g over the largest |g|; g over the gradients' scale.
+struct LossRows {
+    const int64_t *target;
+    const float *grad, *mean;                  // grad: one number, or one per row; mean: may be none, mean[1] is multiplied in
+    int32_t *code;
+    float *factor, *scale;
+    float *largest;                            // [1]: the largest |g| over the gradients' scale
+    uint32_t *flags;
+    int64_t ignore;
+    uint32_t rows, padded, vocab;              // padded: the arrays' length, a multiple of 64
+    bool per_row;
+    float inverse;                             // of the gradients' scale
+};
+
+// One workgroup.  Behind the last row there are rows without a target.
+__global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
+{
+    __shared__ float tops[16];
+    const float part = P.mean ? P.mean[1] : 1.0f;
+    float top = 0.0f;
+    if (P.per_row) {
+        bool lost = false;
+        for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u)
+            if (P.target[n] != P.ignore) {
+                const float g = fabsf(P.grad[n] * part);
+                lost |= !(g < __builtin_inff());
+                top = fmaxf(top, g);
+            }
+        top = lost ? __builtin_nanf("") : top;
+        for (int off = 32; off > 0; off >>= 1) {
+            const float other = __shfl_xor(top, off, 64);
+            top = top == top && !(other <= top) ? other : top;
+        }
+        if (threadIdx.x % 64u == 0)
+            tops[threadIdx.x / 64u] = top;
+        __syncthreads();
+        for (int k = 0; k < 16; ++k)
+            top = top == top && !(tops[k] <= top) ? tops[k] : top;
+    } else {
+        top = P.grad[0] * part;
+    }
+    bool bad = false;
+    for (uint32_t n = threadIdx.x; n < P.padded; n += 1024u) {
+        int32_t code = -1;
+        float factor = 0.0f, scale = 0.0f;
+        if (n < P.rows && P.target[n] != P.ignore) {
+            const int64_t t = P.target[n];
+            if (t >= 0 && t < (int64_t)P.vocab) {
+                code = (int32_t)t;
+                const float g = P.per_row ? P.grad[n] * part : top;
+                factor = !P.per_row ? 1.0f : top == 0.0f ? 0.0f : g / top;
+                scale = g * P.inverse;
+            } else {
+                bad = true;
+            }
+        }
+        P.code[n] = code;
+        P.factor[n] = factor;
+        P.scale[n] = scale;
+    }
+    if (bad)
+        atomicOr(P.flags, (uint32_t)NUQ_FLAG_MALFORMED);
+    if (threadIdx.x == 0)
+        *P.largest = top * P.inverse;
+}
+
+// Rows as the products take them: at a stride that is a multiple of 16 bytes, zeros behind their end.
+template <class T>
+__global__ __launch_bounds__(256) void k_loss_pack(const T *from, uint64_t ld, uint64_t rows, uint32_t columns, T *to, uint32_t to_ld)
+{
+    constexpr uint32_t VEC = 16u / sizeof(T);
+    const uint32_t per = to_ld / VEC;
+    for (uint64_t v = (uint64_t)blockIdx.x * 256u + threadIdx.x; v < rows * per; v += (uint64_t)gridDim.x * 256u) {
+        const uint64_t row = v / per;
+        const uint32_t at = (uint32_t)(v % per) * VEC;
+        float x[VEC];
+        load_some<(int)VEC>(x, from + row * ld + at, (int64_t)columns - at);
+        store_from_float<(int)VEC>(to + row * to_ld + at, x);
+    }
+}
+
+// to[c][r] = from[r][c], zeros for rows behind the last one and for rows without a target; `to_ld` is a multiple of 64.  A workgroup
+// has 64 x 64 elements.
+template <class T>
+__global__ __launch_bounds__(256) void k_loss_transpose(const T *from, uint64_t ld, uint32_t rows, uint32_t columns, const int32_t *code,
+                                                        T *to, uint32_t to_ld)
+{
+    constexpr uint32_t VEC = 16u / sizeof(T), PER = 64u / VEC, STEP = 256u / PER;
+    __shared__ __align__(16) T tile[64][64 + VEC];
+    const uint32_t r0 = blockIdx.y * 64u, c0 = blockIdx.x * 64u, part = threadIdx.x % PER * VEC;
+    for (uint32_t k = threadIdx.x / PER; k < 64u; k += STEP) {
+        const uint32_t row = r0 + k;
+        float x[VEC] = {};
+        if (row < rows && c0 + part < columns && (!code || code[row] >= 0))
+            load_some<(int)VEC>(x, from + (uint64_t)row * ld + c0 + part, (int64_t)columns - c0 - part);
+#pragma unroll
+        for (uint32_t e = 0; e < VEC; ++e)
+            tile[part + e][k] = (T)x[e];
+    }
+    __syncthreads();
+    for (uint32_t k = threadIdx.x / PER; k < 64u && c0 + k < columns; k += STEP)
+        *reinterpret_cast<Chunk *>(to + (uint64_t)(c0 + k) * to_ld + r0 + part) = *reinterpret_cast<const Chunk *>(&tile[k][part]);
+}
+
+struct LossGradient {
+    LossOperands O;                            // w, vocab: of the piece
+    const int32_t *code;
+    const float *factor, *lse;
+    void *d, *dt;                              // d[rows padded][piece padded], dt[piece][rows padded], both padded to 64, dt times factor
+    uint32_t first;                            // of the vocabulary
+    uint32_t padded_rows, padded_vocab;
+    float smoothed, wanted;                    // e / V, 1 - e
+};
+
+template <class T, class Tile>
+__global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradient P)
+{
+    __shared__ __align__(16) char lds[Tile::LDS];
+    uint32_t bm, bn;
+    tile_of(blockIdx.x, P.O.mt, P.O.nt, bm, bn);
+    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN;
+    Tile tile;
+    logits_tile(tile, P.O, m0, n0, lds);
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u)), half = lane / 32u * 4u;
+    const uint32_t mw = m0 + wave / Tile::WN * (Tile::BM / Tile::WM);
+#pragma unroll
+    for (int j = 0; j < Tile::NI; ++j) {
+        const uint32_t n = n0 + wave % Tile::WN * (Tile::BN / Tile::WN) + j * 32u + lane % 32u;
+        if (n >= P.padded_rows)
+            continue;
+        const int32_t code = P.code[n];
+        const float lse = code >= 0 ? P.lse[n] : 0.0f, factor = P.factor[n];
+        const uint32_t target = (uint32_t)code - P.first;    // (no place in the piece where there is none)
+        T *const d = static_cast<T *>(P.d) + (uint64_t)n * P.padded_vocab, *const dt = static_cast<T *>(P.dt) + n;
+#pragma unroll
+        for (int i = 0; i < Tile::MI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t m = mw + i * 32u + q * 8u + half;
+                float x[4];
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; ++e) {
+                    float v = __builtin_amdgcn_exp2f((tile.acc[i][j][q * 4 + e] - lse) * kLog2E) - P.smoothed;
+                    if (m + e == target)
+                        v -= P.wanted;
+                    x[e] = code >= 0 && m + e < P.O.vocab ? v * kGradientScale<T> : 0.0f;
+                }
+                if (m < P.padded_vocab)
+                    store_from_float<4>(d + m, x);
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; ++e)
+                    if (m + e < P.O.vocab)
+                        dt[(uint64_t)(m + e) * P.padded_rows] = (T)(x[e] * factor);
+            }
+    }
+}
+
+// out[n][m] (+)= sum over k of a[m][k] b[n][k] times *scale, for n below `rows` and m below `columns`; workgroups of split s take
+// the chunks of k from s * each on and write the s-th of the outputs.
+struct LossProduct {
+    const void *a, *b;
+    uint32_t stride_a, stride_b, chunks, each;
+    uint32_t columns, rows, mt, nt;
+    void *out;
+    uint64_t ld, next;                         // elements from row to row, from split to split
+    const float *scale;
+};
+
+template <class T, class Tile, class O, bool kAdd>
+__global__ __launch_bounds__(Tile::THREADS) void k_loss_product(const LossProduct P)
+{
+    __shared__ __align__(16) char lds[Tile::LDS];
+    const uint32_t all = P.mt * P.nt, split = blockIdx.x / all;
+    uint32_t bm, bn;
+    tile_of(blockIdx.x % all, P.mt, P.nt, bm, bn);
+    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN, begin = min(split * P.each, P.chunks);
+    Tile tile;
+    tile.run({static_cast<const char *>(P.a) + (uint64_t)m0 * P.stride_a + begin * 16u, P.stride_a, min((uint32_t)Tile::BM, P.columns - m0)},
+             {static_cast<const char *>(P.b) + (uint64_t)n0 * P.stride_b + begin * 16u, P.stride_b, min((uint32_t)Tile::BN, P.rows - n0)},
+             min(P.each, P.chunks - begin), lds);
+    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u)), half = lane / 32u * 4u;
+    const uint32_t mw = m0 + wave / Tile::WN * (Tile::BM / Tile::WM);
+    const float scale = P.scale ? *P.scale : 1.0f;
+    O *const out = static_cast<O *>(P.out) + split * P.next;
+#pragma unroll
+    for (int j = 0; j < Tile::NI; ++j) {
+        const uint32_t n = n0 + wave % Tile::WN * (Tile::BN / Tile::WN) + j * 32u + lane % 32u;
+        if (n >= P.rows)
+            continue;
+#pragma unroll
+        for (int i = 0; i < Tile::MI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t m = mw + i * 32u + q * 8u + half;
+                if (m >= P.columns)
+                    continue;
+                const int64_t have = (int64_t)P.columns - m;
+                O *const to = out + n * P.ld + m;
+                float x[4], before[4] = {};
+                if constexpr (kAdd)
+                    load_some<4>(before, to, have);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] = tile.acc[i][j][q * 4 + e] * scale + before[e];
+                store_some<4>(to, x, have);
+            }
+    }
+}
+
+// dx[n][m] <- scale[n] times the sum of the splits; 0 in a row without a target.
+template <class T>
+__global__ __launch_bounds__(256) void k_loss_rows_gradient(const float *sums, uint64_t ld, uint64_t next, uint32_t splits,
+                                                            const int32_t *code, const float *scale, uint32_t rows, uint32_t hidden,
+                                                            T *dx, uint64_t ldd)
+{
+    const uint32_t per = (hidden + 3u) / 4u;
+    for (uint64_t v = (uint64_t)blockIdx.x * 256u + threadIdx.x; v < (uint64_t)rows * per; v += (uint64_t)gridDim.x * 256u) {
+        const uint32_t n = (uint32_t)(v / per), at = (uint32_t)(v % per) * 4u;
+        float x[4] = {};
+        if (code[n] >= 0) {
+            for (uint32_t s = 0; s < splits; ++s) {
+                float y[4];
+                load_as_float<4>(y, sums + s * next + n * ld + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] += y[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] *= scale[n];
+        }
+        store_some<4>(dx + n * ldd + at, x, (int64_t)hidden - at);
+    }
+}
+
+}  // namespace nuq

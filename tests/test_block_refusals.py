@@ -101,3 +101,56 @@ def test_binding_refuses_tensors_that_do_not_fit(monkeypatch):
     monkeypatch.undo()
     with pytest.raises(ValueError, match="device tensor"):
         forward()
+
+
+LOSS = dict(x=256, ldx=8, weight=256, ldw=8, rows=2, hidden=8, vocab=10, type=0, target=16, ignore=-100, smoothing=0.0)
+LOSS_FORWARD = {**LOSS, **dict(loss=None, lse=16, mean=None, workspace=256, bytes=10 ** 6, stream=None)}
+LOSS_BACKWARD = {**LOSS, **dict(lse=16, grad=16, per_row=0, mean=None, dx=16, ldd=8, dweight=16, lde=8, workspace=256, bytes=10 ** 9, stream=None)}
+
+
+def test_linear_cross_entropy():
+    size = _lib().nuq_linear_cross_entropy_workspace_bytes
+    shape = (256, 64, 256, 64, 100, 64, 1000, 1)
+    assert 0 < size(*shape, 0) < size(*shape, 1) < 10 ** 7
+    assert size(258, *shape[1:], 0) >= size(*shape, 0) + 100 * 128            # rows that have to be laid out anew
+    assert size(*shape[:4], 0, *shape[5:], 1) == 0 and size(*shape[:6], 0, 1, 0) == 0
+    forward, backward = _lib().nuq_linear_cross_entropy_forward, _lib().nuq_linear_cross_entropy_backward
+    both = (dict(x=None), dict(x=258), dict(weight=None), dict(weight=257), dict(rows=2 ** 20 + 1), dict(hidden=0), dict(hidden=2 ** 16 + 1),
+            dict(vocab=0), dict(vocab=2 ** 24 + 1), dict(type=3), dict(target=None), dict(target=20), dict(smoothing=-0.1),
+            dict(smoothing=1.0), dict(smoothing=NAN), dict(lse=None), dict(lse=18), dict(mean=18), dict(workspace=None), dict(workspace=264),
+            dict(rows=2 ** 20, vocab=2 ** 19))
+    for bad in both + (dict(loss=18),):
+        assert forward(*{**LOSS_FORWARD, **bad}.values()) == EINVAL, bad
+    for bad in both + (dict(grad=None), dict(grad=18), dict(dx=18), dict(dweight=18), dict(ldd=7), dict(lde=7)):
+        assert backward(*{**LOSS_BACKWARD, **bad}.values()) == EINVAL, bad
+
+
+def test_linear_cross_entropy_binding(monkeypatch):
+    from paper_1908_06077_amd import binding
+    monkeypatch.setattr(binding, "_on_device", lambda t: True)
+    f = lambda *k: torch.zeros(*k)  # noqa: E731
+    ws, t = torch.zeros(10 ** 6, dtype=torch.uint8), torch.zeros(2, dtype=torch.int64)
+
+    def forward(x=f(2, 4), w=f(9, 4), target=t, loss=None, lse=f(2), mean=None):
+        nuq.nuq_linear_cross_entropy_forward(x, w, target, -100, 0.0, loss, lse, mean, ws)
+
+    def backward(grad=f(1), dx=f(2, 4), dw=f(9, 4), lse=f(2)):
+        nuq.nuq_linear_cross_entropy_backward(f(2, 4), f(9, 4), t, -100, 0.0, lse, grad, None, dx, dw, ws)
+    cases = [
+        ("one element or more", lambda: forward(x=f(2, 0), w=f(9, 0))),
+        ("rows of the vocabulary", lambda: forward(w=f(9, 2, 4))),
+        ("rows of the vocabulary", lambda: forward(w=f(0, 4))),
+        ("weight: expected 9 rows of 4", lambda: forward(w=f(9, 5))),
+        ("weight: expected dtype", lambda: forward(w=f(9, 4).half())),
+        ("target holds 3", lambda: forward(target=torch.zeros(3, dtype=torch.int64))),
+        ("target: expected dtype", lambda: forward(target=t.int())),
+        ("loss holds 3", lambda: forward(loss=f(3))),
+        ("lse holds 1", lambda: forward(lse=f(1))),
+        ("mean holds 1", lambda: forward(mean=f(1))),
+        ("grad holds 3", lambda: backward(grad=f(3))),
+        ("dx: expected 2 rows", lambda: backward(dx=f(2, 5))),
+        ("dweight: expected 9 rows", lambda: backward(dw=f(8, 4))),
+    ]
+    for want, call in cases:
+        with pytest.raises(ValueError, match=want):
+            call()

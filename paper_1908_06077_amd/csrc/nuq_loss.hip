@@ -38,7 +38,6 @@ struct LossShape {
     bool pack_x() const { return !whole(x, ldx); }
     bool pack_w() const { return !whole(w, ldw); }
     uint64_t packed() const { return up(hidden, 64); }       // elements of a packed row
-    uint64_t padded_rows() const { return up(rows, 64); }
 };
 
 // Parts of a workspace one after the other, each at a multiple of 256 bytes.
@@ -93,19 +92,35 @@ uint32_t splits_of(uint64_t tiles, uint32_t steps, uint32_t most_splits)
     return best;
 }
 
-// A piece of the vocabulary: d, once by rows and once by the vocabulary, stays in the last-level cache between the launch that writes
-// it and the products that read it, and is wide enough to fill the device.
+uint32_t tile_rows(uint32_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+uint32_t tile_columns(uint32_t columns) { return columns <= 128 ? 128 : 256; }
+
+// Entries of the vocabulary whose d is in the workspace at a time: at most 160 MiB of them (2048 at least), and of those numbers the one
+// whose three products take the fewest steps of rounds of 256 tiles.
 uint32_t piece_of(const LossShape &S)
 {
-    const uint64_t fits = (160ull << 20) / (2u * S.padded_rows() * S.bytes()) / 256u * 256u;
-    const uint64_t most = std::min<uint64_t>(std::max<uint64_t>(fits, 2048u), 1u << 20), pieces = over(S.vocab, most);
-    return (uint32_t)std::min<uint64_t>(up(over(S.vocab, pieces), 256u), up(S.vocab, 64));
+    const uint64_t row = (uint64_t)S.rows * S.bytes(), most = std::min<uint64_t>(std::max<uint64_t>((160ull << 20) / row, 2048u), 1u << 20) / 256u;
+    const uint64_t all = over(S.vocab, 256);
+    if (all <= most)
+        return (uint32_t)up(S.vocab, 64);
+    const uint64_t nt = over(S.rows, tile_rows(S.rows)), ht = over(S.hidden, tile_columns(S.hidden)), depth = 128 / S.bytes();
+    const auto rounds = [](uint64_t tiles) { return (tiles + 255u) / 256u; };
+    const auto steps = [&](uint64_t tiles) {                 // of a piece of so many tiles
+        return rounds(tiles * nt) * (over(S.hidden, depth) + 3u) + rounds(tiles * ht) * over(S.rows, depth) + rounds(ht * nt) * tiles * 256u / depth;
+    };
+    uint64_t best = most, least = ~0ull;
+    for (uint64_t tiles = most; tiles >= std::max<uint64_t>(most / 2u, 8u); --tiles) {
+        const uint64_t cost = all / tiles * steps(tiles) + (all % tiles ? steps(all % tiles) : 0u);
+        if (cost < least) {
+            least = cost;
+            best = tiles;
+        }
+    }
+    return (uint32_t)(best * 256u);
 }
 
-uint32_t tile_rows(uint32_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
-
 struct BackwardParts {
-    char *x, *w, *d, *dt, *xt, *wt;
+    char *x, *w, *d, *clean;
     int32_t *code;
     float *factor, *scale, *largest, *sums;
     uint32_t piece, splits, each;
@@ -113,23 +128,21 @@ struct BackwardParts {
     BackwardParts(const LossShape &S, void *workspace)
     {
         Parts P{static_cast<char *>(workspace)};
-        const uint64_t R = S.padded_rows(), b = S.bytes();
+        const uint64_t b = S.bytes();
         piece = piece_of(S);
         const uint64_t wide = up(piece, 64);
         x = P.take<char>(S.pack_x() ? S.rows * S.packed() * b : 0);
         w = P.take<char>(S.pack_w() ? S.vocab * S.packed() * b : 0);
-        code = P.take<int32_t>(R);
-        factor = P.take<float>(R);
-        scale = P.take<float>(R);
+        code = P.take<int32_t>(S.rows);
+        factor = P.take<float>(S.rows);
+        scale = P.take<float>(S.rows);
         largest = P.take<float>(1);
-        xt = P.take<char>(S.hidden * R * b);
-        wt = P.take<char>(S.hidden * wide * b);
-        d = P.take<char>(R * wide * b);
-        dt = P.take<char>(R * wide * b);
-        const uint32_t steps = over(wide * b, 128);
-        splits = splits_of((uint64_t)over(S.hidden, S.rows > 128 && S.hidden <= 128 ? 128 : 256) * over(S.rows, tile_rows(S.rows)), steps,
-                           1u + (uint32_t)std::min<uint64_t>(63u, (4ull << 20) / (4u * S.rows * up(S.hidden, 4))));
-        each = over(steps, splits) * 8u;                     // chunks
+        clean = P.take<char>(S.rows * S.packed() * b);
+        d = P.take<char>(S.rows * wide * b);
+        const uint32_t depth = 128u / (uint32_t)b, steps = over(wide, depth);
+        splits = splits_of((uint64_t)over(S.hidden, S.rows > 128 ? tile_columns(S.hidden) : 256) * over(S.rows, tile_rows(S.rows)), steps,
+                           1u + (uint32_t)std::min<uint64_t>(63u, std::max<uint64_t>(4ull << 20, S.rows * wide * b) / (4u * S.rows * up(S.hidden, 4))));
+        each = over(steps, splits) * depth;
         ld_sums = up(S.hidden, 4);
         sums = P.take<float>(splits * S.rows * ld_sums);
         used = P.used;
@@ -137,34 +150,27 @@ struct BackwardParts {
 };
 
 // f(Type<tile>) for a product of many columns, by its rows, and for one of many rows, by its columns.
-template <class T, class F>
+template <class T, bool kAcrossA, class F>
 int with_rows(uint32_t rows, F &&f)
 {
-    return rows > 128  ? f(Type<ProductTile<T, 256, 256, 2, 4>>{})
-           : rows > 64 ? f(Type<ProductTile<T, 256, 128, 2, 2>>{})
-           : rows > 32 ? f(Type<ProductTile<T, 256, 64, 4, 1>>{})
-                       : f(Type<ProductTile<T, 256, 32, 4, 1>>{});
+    return rows > 128  ? f(Type<ProductTile<T, 256, 256, 2, 4, kAcrossA>>{})
+           : rows > 64 ? f(Type<ProductTile<T, 256, 128, 2, 2, kAcrossA>>{})
+           : rows > 32 ? f(Type<ProductTile<T, 256, 64, 4, 1, kAcrossA>>{})
+                       : f(Type<ProductTile<T, 256, 32, 4, 1, kAcrossA>>{});
 }
-template <class T, class F>
+template <class T, bool kAcrossB, class F>
 int with_columns(uint32_t columns, F &&f)
 {
-    return columns > 128 ? f(Type<ProductTile<T, 256, 256, 2, 4>>{}) : f(Type<ProductTile<T, 128, 256, 2, 4>>{});
+    return columns > 128 ? f(Type<ProductTile<T, 256, 256, 2, 4, true, kAcrossB>>{}) : f(Type<ProductTile<T, 128, 256, 2, 4, true, kAcrossB>>{});
 }
 
 template <class T>
-int pack(const void *from, uint64_t ld, uint64_t rows, uint32_t columns, char *to, uint64_t to_ld, hipStream_t st)
+int pack(const void *from, uint64_t ld, uint64_t rows, uint32_t columns, char *to, uint64_t to_ld, const int32_t *code, const float *factor,
+         hipStream_t st)
 {
     const uint64_t vectors = rows * (to_ld * sizeof(T) / 16u);
     hipLaunchKernelGGL(k_loss_pack<T>, dim3((uint32_t)std::min<uint64_t>((vectors + 255u) / 256u, 16384u)), dim3(256), 0, st,
-                       static_cast<const T *>(from), ld, rows, columns, reinterpret_cast<T *>(to), (uint32_t)to_ld);
-    return check_launch();
-}
-
-template <class T>
-int transpose(const void *from, uint64_t ld, uint32_t rows, uint32_t columns, const int32_t *code, char *to, uint64_t to_ld, hipStream_t st)
-{
-    hipLaunchKernelGGL(k_loss_transpose<T>, dim3((columns + 63u) / 64u, (uint32_t)(to_ld / 64u)), dim3(256), 0, st,
-                       static_cast<const T *>(from), ld, rows, columns, code, reinterpret_cast<T *>(to), (uint32_t)to_ld);
+                       static_cast<const T *>(from), ld, rows, columns, reinterpret_cast<T *>(to), (uint32_t)to_ld, code, factor);
     return check_launch();
 }
 
@@ -174,13 +180,13 @@ int operands(const LossShape &S, char *x, char *w, LossOperands &O, hipStream_t 
 {
     O = {S.x, S.w, (uint32_t)(S.ldx * sizeof(T)), (uint32_t)(S.ldw * sizeof(T)), over((uint64_t)S.hidden * sizeof(T), 16), S.rows, S.vocab, 0, 0};
     if (S.pack_x()) {
-        if (const int rc = pack<T>(S.x, S.ldx, S.rows, S.hidden, x, S.packed(), st); rc != NUQ_OK)
+        if (const int rc = pack<T>(S.x, S.ldx, S.rows, S.hidden, x, S.packed(), nullptr, nullptr, st); rc != NUQ_OK)
             return rc;
         O.x = x;
         O.stride_x = (uint32_t)(S.packed() * sizeof(T));
     }
     if (S.pack_w()) {
-        if (const int rc = pack<T>(S.w, S.ldw, S.vocab, S.hidden, w, S.packed(), st); rc != NUQ_OK)
+        if (const int rc = pack<T>(S.w, S.ldw, S.vocab, S.hidden, w, S.packed(), nullptr, nullptr, st); rc != NUQ_OK)
             return rc;
         O.w = w;
         O.stride_w = (uint32_t)(S.packed() * sizeof(T));
@@ -234,16 +240,19 @@ int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *we
         LossForward P{{}, target, W.part, W.sums, W.of_target};
         if (const int done = operands<T>(S, W.x, W.w, P.O, st); done != NUQ_OK)
             return done;
-        return with_rows<T>(S.rows, [&](auto tile) {
+        return with_rows<T, false>(S.rows, [&](auto tile) {
             using Tile = typename decltype(tile)::type;
             P.O.mt = over(vocab, Tile::BM);
             P.O.nt = over(rows, Tile::BN);
-            const dim3 grid(P.O.mt * P.O.nt);
-            if (smooth)
-                hipLaunchKernelGGL((k_loss_logits<T, Tile, true>), grid, dim3(Tile::THREADS), 0, st, P);
-            else
-                hipLaunchKernelGGL((k_loss_logits<T, Tile, false>), grid, dim3(Tile::THREADS), 0, st, P);
-            return check_launch();
+            const auto run = [&](auto smooth_c) {
+                constexpr bool kSmooth = decltype(smooth_c)::value;
+                const uint32_t most = resident_workgroups<k_loss_logits<T, Tile, kSmooth>>(Tile::THREADS);
+                if (!most)
+                    return (int)NUQ_EHIP;
+                hipLaunchKernelGGL((k_loss_logits<T, Tile, kSmooth>), dim3(std::min(P.O.mt * P.O.nt, most)), dim3(Tile::THREADS), 0, st, P);
+                return check_launch();
+            };
+            return smooth ? run(std::true_type{}) : run(std::false_type{});
         });
     });
     if (rc != NUQ_OK)
@@ -274,16 +283,16 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
         off_grid(dx, b) || off_grid(dweight, b) || (dx && rows > 1 && ldd < hidden) || (dweight && vocab > 1 && lde < hidden))
         return NUQ_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    LossRows R{target, grad, mean, nullptr, nullptr, nullptr, nullptr, flags_ptr(), ignore, S.rows, (uint32_t)S.padded_rows(), vocab,
+    LossRows R{target, grad, mean, nullptr, nullptr, nullptr, nullptr, flags_ptr(), ignore, S.rows, vocab,
                grad_per_row != 0, type == NUQ_F16 ? 1.0f / kGradientScale<_Float16> : 1.0f};
     if (!R.flags)
         return NUQ_EHIP;
     if (rows == 0)                                           // sums over no rows
         return !dweight ? (int)NUQ_OK : with_type(type, [&](auto tt) {
             using T = typename decltype(tt)::type;
-            using Tile = ProductTile<T, 256, 256, 2, 4>;
-            LossProduct P{weight, weight, 16, 16, 0, 0, hidden, vocab, over(hidden, Tile::BM), over(vocab, Tile::BN), dweight, lde, 0, nullptr};
-            hipLaunchKernelGGL((k_loss_product<T, Tile, T, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
+            using Tile = ProductTile<T, 256, 256, 2, 4, true, true>;
+            LossProduct P{weight, weight, 16, 16, 0, 0, 0, 0, 0, hidden, vocab, over(hidden, Tile::BM), over(vocab, Tile::BN), dweight, lde, 0, nullptr};
+            hipLaunchKernelGGL((k_loss_product<T, Tile, T, true, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
             return check_launch();
         });
     const BackwardParts W(S, workspace);
@@ -300,10 +309,11 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
         return rc;
     return with_type(type, [&](auto tt) {
         using T = typename decltype(tt)::type;
-        LossGradient G{{}, W.code, W.factor, lse, W.d, W.dt, 0, R.padded, 0, smoothing / (float)vocab, 1.0f - smoothing};
+        constexpr uint32_t VEC = 16u / sizeof(T);
+        LossGradient G{{}, W.code, lse, W.d, 0, 0, smoothing / (float)vocab, 1.0f - smoothing};
         int rc = operands<T>(S, W.x, W.w, G.O, st);
         if (rc == NUQ_OK && dweight)
-            rc = transpose<T>(x, ldx, S.rows, hidden, W.code, W.xt, R.padded, st);
+            rc = pack<T>(x, ldx, rows, hidden, W.clean, S.packed(), W.code, W.factor, st);
         const char *const all = static_cast<const char *>(G.O.w);
         for (uint32_t first = 0; rc == NUQ_OK && first < vocab; first += W.piece) {
             const uint32_t here = std::min(W.piece, vocab - first);
@@ -311,38 +321,40 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
             G.O.w = all + (uint64_t)first * G.O.stride_w;
             G.O.vocab = here;
             G.padded_vocab = (uint32_t)up(here, 64);
-            rc = with_rows<T>(S.rows, [&](auto tile) {
+            const uint32_t stride_d = G.padded_vocab * (uint32_t)sizeof(T);
+            rc = with_rows<T, false>(S.rows, [&](auto tile) {
                 using Tile = typename decltype(tile)::type;
                 G.O.mt = over(here, Tile::BM);
-                G.O.nt = over(R.padded, Tile::BN);
-                hipLaunchKernelGGL((k_loss_gradient<T, Tile>), dim3(G.O.mt * G.O.nt), dim3(Tile::THREADS), 0, st, G);
+                G.O.nt = over(rows, Tile::BN);
+                const uint32_t most = resident_workgroups<k_loss_gradient<T, Tile>>(Tile::THREADS);
+                if (!most)
+                    return (int)NUQ_EHIP;
+                hipLaunchKernelGGL((k_loss_gradient<T, Tile>), dim3(std::min(G.O.mt * G.O.nt, most)), dim3(Tile::THREADS), 0, st, G);
                 return check_launch();
             });
             if (rc == NUQ_OK && dweight)
-                rc = with_columns<T>(hidden, [&](auto tile) {
+                rc = with_columns<T, true>(hidden, [&](auto tile) {
                     using Tile = typename decltype(tile)::type;
-                    const uint32_t stride = R.padded * (uint32_t)sizeof(T);
-                    LossProduct P{W.xt, W.dt, stride, stride, stride / 16u, stride / 16u, hidden, here, over(hidden, Tile::BM),
-                                  over(here, Tile::BN), static_cast<T *>(dweight) + first * lde, lde, 0, W.largest};
-                    hipLaunchKernelGGL((k_loss_product<T, Tile, T, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
+                    LossProduct P{W.clean, W.d, (uint32_t)(S.packed() * sizeof(T)), stride_d, (uint32_t)S.packed() / VEC, G.padded_vocab / VEC,
+                                  S.rows, S.rows, (uint32_t)up(rows, 64), hidden, here, over(hidden, Tile::BM), over(here, Tile::BN),
+                                  static_cast<T *>(dweight) + first * lde, lde, 0, W.largest};
+                    hipLaunchKernelGGL((k_loss_product<T, Tile, T, true, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
                     return check_launch();
                 });
-            if (rc == NUQ_OK && dx)
-                rc = transpose<T>(static_cast<const T *>(weight) + first * ldw, ldw, here, hidden, nullptr, W.wt, G.padded_vocab, st);
             if (rc == NUQ_OK && dx) {
                 const auto product = [&](auto tile) {
                     using Tile = typename decltype(tile)::type;
-                    const uint32_t stride = G.padded_vocab * (uint32_t)sizeof(T);
-                    LossProduct P{W.wt, W.d, stride, stride, stride / 16u, W.each, hidden, S.rows, over(hidden, Tile::BM),
-                                  over(rows, Tile::BN), W.sums, W.ld_sums, rows * W.ld_sums, nullptr};
+                    LossProduct P{G.O.w, W.d, G.O.stride_w, stride_d, S.pack_w() ? (uint32_t)S.packed() / VEC : hidden / VEC, 0, here,
+                                  G.padded_vocab, W.each, hidden, S.rows, over(hidden, Tile::BM), over(rows, Tile::BN), W.sums, W.ld_sums,
+                                  rows * W.ld_sums, nullptr};
                     const dim3 grid(P.mt * P.nt * W.splits);
                     if (first)
-                        hipLaunchKernelGGL((k_loss_product<T, Tile, float, true>), grid, dim3(Tile::THREADS), 0, st, P);
+                        hipLaunchKernelGGL((k_loss_product<T, Tile, float, false, true>), grid, dim3(Tile::THREADS), 0, st, P);
                     else
-                        hipLaunchKernelGGL((k_loss_product<T, Tile, float, false>), grid, dim3(Tile::THREADS), 0, st, P);
+                        hipLaunchKernelGGL((k_loss_product<T, Tile, float, false, false>), grid, dim3(Tile::THREADS), 0, st, P);
                     return check_launch();
                 };
-                rc = rows > 128 ? with_columns<T>(hidden, product) : with_rows<T>(S.rows, product);
+                rc = rows > 128 ? with_columns<T, false>(hidden, product) : with_rows<T, true>(S.rows, product);
             }
         }
         if (rc == NUQ_OK && dx) {

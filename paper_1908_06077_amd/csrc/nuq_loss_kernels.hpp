@@ -38,19 +38,36 @@ struct LossForward {
     float *of_target;                          // [rows]: the target's logit
 };
 
-// The tile's rows of the vocabulary, and of x: none behind the last.
+// The tiles of logits that a workgroup makes: every gridDim.x-th, the first step of the next one on its way while one is worked on.
 template <class Tile>
-__device__ __forceinline__ void logits_tile(Tile &tile, const LossOperands &O, uint32_t m0, uint32_t n0, char *lds)
-{
-    tile.run({static_cast<const char *>(O.w) + (uint64_t)m0 * O.stride_w, O.stride_w, min((uint32_t)Tile::BM, O.vocab - m0)},
-             {static_cast<const char *>(O.x) + (uint64_t)n0 * O.stride_x, O.stride_x, n0 < O.rows ? min((uint32_t)Tile::BN, O.rows - n0) : 0u},
-             O.chunks, lds);
-}
+struct LogitTiles {
+    const LossOperands &O;
+    uint32_t id, m0, n0;
+    __device__ __forceinline__ LogitTiles(const LossOperands &o, Tile &tile) : O(o), id(blockIdx.x) { begin(tile); }
+    __device__ __forceinline__ void begin(Tile &tile)
+    {
+        tile_of(id, O.mt, O.nt, m0, n0);
+        m0 *= Tile::BM;
+        n0 *= Tile::BN;
+        tile.begin({static_cast<const char *>(O.w) + (uint64_t)m0 * O.stride_w, O.stride_w, min((uint32_t)Tile::BM, O.vocab - m0), O.chunks},
+                   {static_cast<const char *>(O.x) + (uint64_t)n0 * O.stride_x, O.stride_x, min((uint32_t)Tile::BN, O.rows - n0), O.chunks});
+    }
+    __device__ __forceinline__ uint32_t steps() const { return (O.chunks + 7u) / 8u; }
+    // Whether there is another tile, which is begun.
+    __device__ __forceinline__ bool next(Tile &tile)
+    {
+        id += gridDim.x;
+        const bool more = id < O.mt * O.nt;
+        if (more)
+            begin(tile);
+        return more;
+    }
+};
 
 // The sum of exp(z - base) needs a base that is finite.
 __device__ __forceinline__ float finite_base(float top) { return __builtin_isinf(top) ? 0.0f : top; }
 
-// f(m of the wave's rows, block, register) for the sixteen values of a block, m in 0 .. BM / WM - 1 less four times the lane's half.
+// f(m of the wave's rows less four times the lane's half, register) for the sixteen values of block i.
 template <class F>
 __device__ __forceinline__ void for_block(int i, F &&f)
 {
@@ -63,52 +80,61 @@ template <class T, class Tile, bool kSmooth>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
-    uint32_t bm, bn;
-    tile_of(blockIdx.x, P.O.mt, P.O.nt, bm, bn);
-    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN;
-    Tile tile;
-    logits_tile(tile, P.O, m0, n0, lds);
     constexpr uint32_t GROUP = Tile::BM / Tile::WM;
-    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u)), half = lane / 32u * 4u;
-    const uint32_t mw = m0 + wave / Tile::WN * GROUP;
-    if (mw >= P.O.vocab)
-        return;
-    const uint32_t there = min(GROUP, P.O.vocab - mw);
-    const uint64_t group = mw / GROUP;
+    const uint32_t half = threadIdx.x / 32u % 2u * 4u;
+    Tile tile(lds);
+    LogitTiles<Tile> tiles(P.O, tile);
+    for (bool more = true; more;) {
+        const uint32_t mw = tiles.m0 + tile.first_m(), nw = tiles.n0 + tile.first_n() + threadIdx.x % 32u;
+        int64_t target[Tile::NI];
 #pragma unroll
-    for (int j = 0; j < Tile::NI; ++j) {
-        const uint32_t n = n0 + wave % Tile::WN * (Tile::BN / Tile::WN) + j * 32u + lane % 32u;
-        const bool row = n < P.O.rows;
-        const int64_t target = row ? P.target[n] : -1;
-        const uint32_t at = (uint64_t)target - mw < there ? (uint32_t)((uint64_t)target - mw) : ~0u;
-        float top = -__builtin_inff(), sum = 0.0f, all = 0.0f, wanted = 0.0f;
+        for (int j = 0; j < Tile::NI; ++j)
+            target[j] = nw + j * 32u < P.O.rows ? P.target[nw + j * 32u] : -1;
+        tile.run(tiles.steps());
+        more = tiles.next(tile);
+        tile.finish();
+        if (mw >= P.O.vocab)
+            continue;
+        const uint32_t there = min(GROUP, P.O.vocab - mw);
+        const uint64_t group = mw / GROUP;
 #pragma unroll
-        for (int i = 0; i < Tile::MI; ++i)
-            for_block(i, [&](uint32_t m, int r) {
-                float z = tile.acc[i][j][r];
-                m += half;
-                if (m == at)
-                    wanted = z;
-                if constexpr (kSmooth)
-                    all += m < there ? z : 0.0f;
-                if (there < GROUP)
-                    tile.acc[i][j][r] = z = m < there ? z : -__builtin_inff();
-                top = fmaxf(top, z);
-            });
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float base = finite_base(top);
+        for (int j = 0; j < Tile::NI; ++j) {
+            const uint32_t n = nw + j * 32u;
+            const bool row = n < P.O.rows;
+            const uint32_t at = (uint64_t)target[j] - mw < there ? (uint32_t)((uint64_t)target[j] - mw) : ~0u;
+            float top = -__builtin_inff(), sum = 0.0f, all = 0.0f, wanted = 0.0f;
 #pragma unroll
-        for (int i = 0; i < Tile::MI; ++i)
-            for_block(i, [&](uint32_t, int r) { sum += __builtin_amdgcn_exp2f((tile.acc[i][j][r] - base) * kLog2E); });
-        sum += __shfl_xor(sum, 32, 64);
-        if constexpr (kSmooth)
-            all += __shfl_xor(all, 32, 64);
-        if (row && at != ~0u && (at & 4u) == half)
-            P.of_target[n] = wanted;
-        if (row && half == 0u) {
-            P.part[group * P.O.rows + n] = make_float2(top, sum);
+            for (int i = 0; i < Tile::MI; ++i) {
+                __builtin_amdgcn_sched_barrier(0);           // (a block after the other: there are no registers for more)
+                for_block(i, [&](uint32_t m, int r) {
+                    float z = tile.acc[i][j][r];
+                    m += half;
+                    if (m == at)
+                        wanted = z;
+                    if constexpr (kSmooth)
+                        all += m < there ? z : 0.0f;
+                    if (there < GROUP)
+                        tile.acc[i][j][r] = z = m < there ? z : -__builtin_inff();
+                    top = fmaxf(top, z);
+                });
+            }
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float base = finite_base(top);
+#pragma unroll
+            for (int i = 0; i < Tile::MI; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                for_block(i, [&](uint32_t, int r) { sum += __builtin_amdgcn_exp2f((tile.acc[i][j][r] - base) * kLog2E); });
+            }
+            sum += __shfl_xor(sum, 32, 64);
             if constexpr (kSmooth)
-                P.sums[group * P.O.rows + n] = all;
+                all += __shfl_xor(all, 32, 64);
+            if (row && at != ~0u && (at & 4u) == half)
+                P.of_target[n] = wanted;
+            if (row && half == 0u) {
+                P.part[group * P.O.rows + n] = make_float2(top, sum);
+                if constexpr (kSmooth)
+                    P.sums[group * P.O.rows + n] = all;
+            }
         }
     }
 }
@@ -212,12 +238,12 @@ struct LossRows {
     float *largest;                            // [1]: the largest |g| over the gradients' scale
     uint32_t *flags;
     int64_t ignore;
-    uint32_t rows, padded, vocab;              // padded: the arrays' length, a multiple of 64
+    uint32_t rows, vocab;
     bool per_row;
     float inverse;                             // of the gradients' scale
 };
 
-// One workgroup.  Behind the last row there are rows without a target.
+// One workgroup.
 __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
 {
     __shared__ float tops[16];
@@ -245,10 +271,10 @@ __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
         top = P.grad[0] * part;
     }
     bool bad = false;
-    for (uint32_t n = threadIdx.x; n < P.padded; n += 1024u) {
+    for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u) {
         int32_t code = -1;
         float factor = 0.0f, scale = 0.0f;
-        if (n < P.rows && P.target[n] != P.ignore) {
+        if (P.target[n] != P.ignore) {
             const int64_t t = P.target[n];
             if (t >= 0 && t < (int64_t)P.vocab) {
                 code = (int32_t)t;
@@ -269,51 +295,36 @@ __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
         *P.largest = top * P.inverse;
 }
 
-// Rows as the products take them: at a stride that is a multiple of 16 bytes, zeros behind their end.
+// Rows as the products take them: at a stride that is a multiple of 16 bytes, zeros behind their end.  With a code, zeros for a row without
+// a target, whatever it holds, and the others times their factor.
 template <class T>
-__global__ __launch_bounds__(256) void k_loss_pack(const T *from, uint64_t ld, uint64_t rows, uint32_t columns, T *to, uint32_t to_ld)
+__global__ __launch_bounds__(256) void k_loss_pack(const T *from, uint64_t ld, uint64_t rows, uint32_t columns, T *to, uint32_t to_ld,
+                                                   const int32_t *code, const float *factor)
 {
     constexpr uint32_t VEC = 16u / sizeof(T);
     const uint32_t per = to_ld / VEC;
     for (uint64_t v = (uint64_t)blockIdx.x * 256u + threadIdx.x; v < rows * per; v += (uint64_t)gridDim.x * 256u) {
         const uint64_t row = v / per;
         const uint32_t at = (uint32_t)(v % per) * VEC;
-        float x[VEC];
-        load_some<(int)VEC>(x, from + row * ld + at, (int64_t)columns - at);
+        float x[VEC] = {};
+        if (!code || code[row] >= 0) {
+            load_some<(int)VEC>(x, from + row * ld + at, (int64_t)columns - at);
+            if (code)
+#pragma unroll
+                for (uint32_t e = 0; e < VEC; ++e)
+                    x[e] *= factor[row];
+        }
         store_from_float<(int)VEC>(to + row * to_ld + at, x);
     }
-}
-
-// to[c][r] = from[r][c], zeros for rows behind the last one and for rows without a target; `to_ld` is a multiple of 64.  A workgroup
-// has 64 x 64 elements.
-template <class T>
-__global__ __launch_bounds__(256) void k_loss_transpose(const T *from, uint64_t ld, uint32_t rows, uint32_t columns, const int32_t *code,
-                                                        T *to, uint32_t to_ld)
-{
-    constexpr uint32_t VEC = 16u / sizeof(T), PER = 64u / VEC, STEP = 256u / PER;
-    __shared__ __align__(16) T tile[64][64 + VEC];
-    const uint32_t r0 = blockIdx.y * 64u, c0 = blockIdx.x * 64u, part = threadIdx.x % PER * VEC;
-    for (uint32_t k = threadIdx.x / PER; k < 64u; k += STEP) {
-        const uint32_t row = r0 + k;
-        float x[VEC] = {};
-        if (row < rows && c0 + part < columns && (!code || code[row] >= 0))
-            load_some<(int)VEC>(x, from + (uint64_t)row * ld + c0 + part, (int64_t)columns - c0 - part);
-#pragma unroll
-        for (uint32_t e = 0; e < VEC; ++e)
-            tile[part + e][k] = (T)x[e];
-    }
-    __syncthreads();
-    for (uint32_t k = threadIdx.x / PER; k < 64u && c0 + k < columns; k += STEP)
-        *reinterpret_cast<Chunk *>(to + (uint64_t)(c0 + k) * to_ld + r0 + part) = *reinterpret_cast<const Chunk *>(&tile[k][part]);
 }
 
 struct LossGradient {
     LossOperands O;                            // w, vocab: of the piece
     const int32_t *code;
-    const float *factor, *lse;
-    void *d, *dt;                              // d[rows padded][piece padded], dt[piece][rows padded], both padded to 64, dt times factor
+    const float *lse;
+    void *d;                                   // [rows][piece padded to 64], zeros behind the piece
     uint32_t first;                            // of the vocabulary
-    uint32_t padded_rows, padded_vocab;
+    uint32_t padded_vocab;
     float smoothed, wanted;                    // e / V, 1 - e
 };
 
@@ -321,94 +332,129 @@ template <class T, class Tile>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradient P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
-    uint32_t bm, bn;
-    tile_of(blockIdx.x, P.O.mt, P.O.nt, bm, bn);
-    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN;
-    Tile tile;
-    logits_tile(tile, P.O, m0, n0, lds);
-    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u)), half = lane / 32u * 4u;
-    const uint32_t mw = m0 + wave / Tile::WN * (Tile::BM / Tile::WM);
+    const uint32_t half = threadIdx.x / 32u % 2u * 4u;
+    Tile tile(lds);
+    LogitTiles<Tile> tiles(P.O, tile);
+    for (bool more = true; more;) {
+        const uint32_t mw = tiles.m0 + tile.first_m(), n0 = tiles.n0 + tile.first_n();
+        int32_t code[Tile::NI];
+        float lse[Tile::NI];
 #pragma unroll
-    for (int j = 0; j < Tile::NI; ++j) {
-        const uint32_t n = n0 + wave % Tile::WN * (Tile::BN / Tile::WN) + j * 32u + lane % 32u;
-        if (n >= P.padded_rows)
-            continue;
-        const int32_t code = P.code[n];
-        const float lse = code >= 0 ? P.lse[n] : 0.0f, factor = P.factor[n];
-        const uint32_t target = (uint32_t)code - P.first;    // (no place in the piece where there is none)
-        T *const d = static_cast<T *>(P.d) + (uint64_t)n * P.padded_vocab, *const dt = static_cast<T *>(P.dt) + n;
+        for (int j = 0; j < Tile::NI; ++j) {
+            const uint32_t n = n0 + j * 32u + threadIdx.x % 32u;
+            code[j] = n < P.O.rows ? P.code[n] : -1;
+            lse[j] = n < P.O.rows ? P.lse[n] : 0.0f;
+        }
+        tile.run(tiles.steps());
+        more = tiles.next(tile);
+        tile.finish();
+        // d of columns 8 q + half to 8 q + half + 3 of block i, of the lane's row of block j
+        const auto gradient = [&](int j, int i, int q, float (&x)[4]) {
+            const uint32_t m = mw + i * 32u + q * 8u + half, target = (uint32_t)code[j] - P.first;   // (none in the piece: no place in it)
 #pragma unroll
-        for (int i = 0; i < Tile::MI; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t m = mw + i * 32u + q * 8u + half;
-                float x[4];
-#pragma unroll
-                for (uint32_t e = 0; e < 4u; ++e) {
-                    float v = __builtin_amdgcn_exp2f((tile.acc[i][j][q * 4 + e] - lse) * kLog2E) - P.smoothed;
-                    if (m + e == target)
-                        v -= P.wanted;
-                    x[e] = code >= 0 && m + e < P.O.vocab ? v * kGradientScale<T> : 0.0f;
-                }
-                if (m < P.padded_vocab)
-                    store_from_float<4>(d + m, x);
-#pragma unroll
-                for (uint32_t e = 0; e < 4u; ++e)
-                    if (m + e < P.O.vocab)
-                        dt[(uint64_t)(m + e) * P.padded_rows] = (T)(x[e] * factor);
+            for (uint32_t e = 0; e < 4u; ++e) {
+                float v = __builtin_amdgcn_exp2f((tile.acc[i][j][q * 4 + e] - lse[j]) * kLog2E) - P.smoothed;
+                if (m + e == target)
+                    v -= P.wanted;
+                x[e] = code[j] >= 0 && m + e < P.O.vocab ? v * kGradientScale<T> : 0.0f;
             }
+        };
+        const auto row = [&](int j, uint32_t r) -> T * {
+            const uint32_t n = n0 + j * 32u + r;
+            return n < P.O.rows ? static_cast<T *>(P.d) + (uint64_t)n * P.padded_vocab + mw : nullptr;
+        };
+        if constexpr (sizeof(T) == 2) {
+            tile.store_rows(gradient, row, (int64_t)P.padded_vocab - mw);
+        } else {
+#pragma unroll
+            for (int j = 0; j < Tile::NI; ++j)
+#pragma unroll
+                for (int i = 0; i < Tile::MI; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float x[4];
+                        gradient(j, i, q, x);
+                        T *const to = row(j, threadIdx.x % 32u);
+                        if (to && mw + i * 32u + q * 8u < P.padded_vocab)
+                            store_from_float<4>(to + i * 32 + q * 8 + half, x);
+                    }
+        }
     }
 }
 
-// out[n][m] (+)= sum over k of a[m][k] b[n][k] times *scale, for n below `rows` and m below `columns`; workgroups of split s take
-// the chunks of k from s * each on and write the s-th of the outputs.
+// out[n][m] (+)= sum over k of a[k][m] b[n][k] (or b[k][n], where Tile takes that operand across) times *scale, for m below `columns` and n
+// below `rows`; workgroups of split s take `each` of the k from s * each on and write the s-th of the outputs.
 struct LossProduct {
     const void *a, *b;
-    uint32_t stride_a, stride_b, chunks, each;
+    uint32_t stride_a, stride_b;               // bytes
+    uint32_t wide_a, wide_b;                   // across: 16-byte pieces of a row
+    uint32_t deep_a, deep_b, each;             // k that there are in either, at least one split's
     uint32_t columns, rows, mt, nt;
     void *out;
     uint64_t ld, next;                         // elements from row to row, from split to split
     const float *scale;
 };
 
-template <class T, class Tile, class O, bool kAdd>
+template <class T, class Tile, class O, bool kAcrossB, bool kAdd>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_product(const LossProduct P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
-    const uint32_t all = P.mt * P.nt, split = blockIdx.x / all;
+    constexpr uint32_t VEC = 16u / (uint32_t)sizeof(T);
+    const uint32_t all = P.mt * P.nt, split = blockIdx.x / all, half = threadIdx.x / 32u % 2u * 4u;
     uint32_t bm, bn;
     tile_of(blockIdx.x % all, P.mt, P.nt, bm, bn);
-    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN, begin = min(split * P.each, P.chunks);
-    Tile tile;
-    tile.run({static_cast<const char *>(P.a) + (uint64_t)m0 * P.stride_a + begin * 16u, P.stride_a, min((uint32_t)Tile::BM, P.columns - m0)},
-             {static_cast<const char *>(P.b) + (uint64_t)n0 * P.stride_b + begin * 16u, P.stride_b, min((uint32_t)Tile::BN, P.rows - n0)},
-             min(P.each, P.chunks - begin), lds);
-    const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u)), half = lane / 32u * 4u;
-    const uint32_t mw = m0 + wave / Tile::WN * (Tile::BM / Tile::WM);
+    const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN, k0 = split * P.each;
+    const auto left = [&](uint32_t deep) -> uint32_t { return k0 < deep ? min(P.each, deep - k0) : 0u; };
+    const auto across = [&](const void *p, uint32_t stride, uint32_t wide, uint32_t deep, uint32_t first, uint32_t size) -> Operand {
+        const uint32_t pieces = min(size / VEC, wide - first / VEC);
+        return {static_cast<const char *>(p) + (uint64_t)k0 * stride + (uint64_t)first * sizeof(T), stride, pieces, left(deep)};
+    };
     const float scale = P.scale ? *P.scale : 1.0f;
-    O *const out = static_cast<O *>(P.out) + split * P.next;
+    Tile tile(lds);
+    const Operand a = across(P.a, P.stride_a, P.wide_a, P.deep_a, m0, Tile::BM);
+    if constexpr (kAcrossB)
+        tile.begin(a, across(P.b, P.stride_b, P.wide_b, P.deep_b, n0, Tile::BN));
+    else
+        tile.begin(a, {static_cast<const char *>(P.b) + (uint64_t)n0 * P.stride_b + (uint64_t)k0 * sizeof(T), P.stride_b,
+                       min((uint32_t)Tile::BN, P.rows - n0), left(P.deep_b) / VEC});
+    constexpr uint32_t DEPTH = 128u / (uint32_t)sizeof(T);
+    tile.run(max(1u, (left(max(P.deep_a, P.deep_b)) + DEPTH - 1u) / DEPTH));
+    tile.finish();
+    const uint32_t mw = m0 + tile.first_m();
+    O *const out = static_cast<O *>(P.out) + split * P.next + mw;
+    const auto row = [&](int j, uint32_t r) -> O * {
+        const uint32_t n = n0 + tile.first_n() + j * 32u + r;
+        return n < P.rows ? out + n * P.ld : nullptr;
+    };
+    if constexpr (sizeof(O) == 2 && !kAdd) {
+        tile.store_rows([&](int j, int i, int q, float (&x)[4]) {
 #pragma unroll
-    for (int j = 0; j < Tile::NI; ++j) {
-        const uint32_t n = n0 + wave % Tile::WN * (Tile::BN / Tile::WN) + j * 32u + lane % 32u;
-        if (n >= P.rows)
-            continue;
+            for (int e = 0; e < 4; ++e)
+                x[e] = tile.acc[i][j][q * 4 + e] * scale;
+        }, row, (int64_t)P.columns - mw);
+    } else {
 #pragma unroll
-        for (int i = 0; i < Tile::MI; ++i)
+        for (int j = 0; j < Tile::NI; ++j) {
+            O *const to = row(j, threadIdx.x % 32u);
+            if (!to)
+                continue;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t m = mw + i * 32u + q * 8u + half;
-                if (m >= P.columns)
-                    continue;
-                const int64_t have = (int64_t)P.columns - m;
-                O *const to = out + n * P.ld + m;
-                float x[4], before[4] = {};
-                if constexpr (kAdd)
-                    load_some<4>(before, to, have);
+            for (int i = 0; i < Tile::MI; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    x[e] = tile.acc[i][j][q * 4 + e] * scale + before[e];
-                store_some<4>(to, x, have);
-            }
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t m = i * 32u + q * 8u + half;
+                    const int64_t have = (int64_t)P.columns - mw - m;
+                    if (have <= 0)
+                        continue;
+                    float x[4], before[4] = {};
+                    if constexpr (kAdd)
+                        load_some<4>(before, to + m, have);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = tile.acc[i][j][q * 4 + e] * scale + before[e];
+                    store_some<4>(to + m, x, have);
+                }
+        }
     }
 }
 

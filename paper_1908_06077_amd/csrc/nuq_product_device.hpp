@@ -1,10 +1,15 @@
-// Tiles of a matrix product on the matrix cores: acc[m][n] = sum over k of A[m][k] B[n][k], both operands with k contiguous.
+// Tiles of a matrix product on the matrix cores: acc[m][n] = sum over k of A[m][k] B[n][k].
 //
-// A workgroup of WM x WN waves has a tile of BM x BN; a wave BM / WM x BN / WN of it in 32 x 32 blocks.  Per step 128 bytes of every
-// row (64 elements of 16 bits, 32 of fp32) go from global memory into one half of the LDS, without a register between, while the
-// products of the other half run; operands come out of the LDS one quarter step ahead of their products.  In the LDS chunk c (16
-// bytes) of row r stands at c ^ r % 8: the eight lanes that read one column of chunks at once meet eight different groups of banks.
-// The loads write the LDS in lane order, so it is the address in global memory that is permuted.
+// A workgroup of WM x WN waves has a tile of BM x BN; a wave BM / WM x BN / WN of it in 32 x 32 blocks.  Per step a depth of 128 bytes
+// (64 elements of 16 bits, 32 of fp32) goes from global memory into one half of the LDS, without a register between, while the products
+// of the other half run; operands come out of the LDS one quarter step ahead of their products.  The loads write the LDS in lane order,
+// so where banks would be met twice it is the address in global memory that is permuted.
+//
+// An operand stands in memory by rows, k contiguous: in the LDS 128 bytes of each, chunk c (16 bytes) of row r at c ^ r / 2 % 8.  Sixteen
+// lanes read a column of chunks at once, two rows fill the 64 banks, and so these meet each bank once (with c ^ r % 8 half the time of the
+// reads was conflicts, 1120 TFLOP/s at 8192 x 8192 x 8192 in bfloat16 instead of 1215).  Or it stands across, m or n contiguous: in the
+// LDS the rows of k, and elements of 16 bits are transposed by the reads: 4 x 16 of them at a time, the 64 bytes of two such blocks at
+// c ^ k % 4 (c counts 64 bytes); fp32 is read element by element, 128 bytes at c ^ k / 4 % 2.
 //
 // fp32 operands go through the matrix cores as fp32: a chunk is four products of depth 2, and which k a lane holds is the same in
 // both operands, so the sum is over every k once.
@@ -38,121 +43,250 @@ __device__ __forceinline__ Block multiply(Chunk a, Chunk b, Block c)
     }
 }
 
-// Rows of a tile: the first one's address, the bytes from one to the next (a multiple of 16), and how many there are.
-struct TileRows {
+// 4 x 16 elements of 16 bits out of the LDS: lane l of sixteen brings the address of elements 4 (l % 4) to 4 (l % 4) + 3 of row l / 4 and
+// gets element l of the four rows.
+typedef uint32_t HalfChunk __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ HalfChunk read_transposed(const char *at)
+{
+#ifdef __HIP_DEVICE_COMPILE__                                // (the host's pass does not know the builtin)
+    typedef short S4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(HalfChunk, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)at));
+#else
+    return HalfChunk{};
+#endif
+}
+
+// 16 bytes per lane from buffer + at + offset into the LDS, one lane's behind the other's; zeros for what lies behind the buffer.
+__device__ __forceinline__ void load_into_lds(__amdgpu_buffer_rsrc_t buffer, char *to, uint32_t at, uint32_t offset)
+{
+#ifdef __HIP_DEVICE_COMPILE__                                // (nor that this one takes 16 bytes)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (__attribute__((address_space(3))) void *)to, 16, at, offset, 0, 0);
+#endif
+}
+
+// A tile's operand.  By rows: the tile's first row, the bytes from one to the next, how many there are, the chunks of each.  Across: the
+// tile's first column in the first row of k, the bytes from one k to the next, the chunks of each, how many k there are.  Addresses and
+// strides are multiples of 16, a stride is below 2^22.
+struct Operand {
     const void *first;
-    uint32_t stride, there;
+    uint32_t stride, wide, deep;
 };
 
 // An offset that no buffer of a tile reaches (fewer than 2^31 bytes each): the load brings 0.
 constexpr uint32_t kNowhere = 0x80000000u;
 
-template <class T, int BM_, int BN_, int WM_, int WN_>
+// One operand's part of a stage, SIZE rows or columns of it, loaded by WAVES waves.
+template <class T, int SIZE, int WAVES, bool kAcross>
+struct OperandLoads {
+    static constexpr int LOADS = SIZE / 8 / WAVES;           // per wave and step, 1024 bytes each
+    static constexpr uint32_t DEPTH = 128 / sizeof(T);       // of a step
+    static constexpr uint32_t ROW = kAcross ? SIZE * (uint32_t)sizeof(T) : 128u;            // bytes of a row in the LDS
+    static constexpr uint32_t UNIT = sizeof(T) == 2 ? 4u : 8u;                              // chunks that are permuted as one
+    static_assert(LOADS * 8 * WAVES == SIZE && WAVES % 2 == 0, "whole loads");
+    static_assert(!kAcross || (1024u % ROW == 0 && ROW / 16u >= 4u * UNIT / (sizeof(T) == 2 ? 1u : 2u)), "whole rows, and what is permuted in them");
+
+    Operand O;
+    uint32_t at[LOADS];                                      // offsets of the lane's chunks in a step
+    uint32_t chunk;                                          // by rows: the lane's chunk in every row that it loads
+
+    __device__ __forceinline__ void place(const Operand &o, uint32_t wave, uint32_t lane)
+    {
+        O = o;
+        chunk = lane % 8u ^ (wave % 2u * 4u + lane / 16u);   // (a load is of rows 8 g to 8 g + 7, g odd in odd waves)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t byte = ((uint32_t)i * WAVES + wave) * 1024u + lane * 16u, row = byte / ROW;
+            if constexpr (kAcross) {
+                const uint32_t c = byte % ROW / 16u, turn = sizeof(T) == 2 ? row % 4u : row / 4u % 2u, column = c ^ turn * UNIT;
+                at[i] = column < O.wide ? row * O.stride + column * 16u : kNowhere;
+            } else {
+                at[i] = row < O.wide ? row * O.stride + chunk * 16u : kNowhere;
+            }
+        }
+    }
+    // The loads of step s.
+    __device__ __forceinline__ void issue(uint32_t s, char *__restrict__ to, uint32_t wave) const
+    {
+        const char *first = static_cast<const char *>(O.first);
+        uint32_t rows = O.wide, offset = s * 128u;
+        bool there = chunk + s * 8u < O.deep;
+        if constexpr (kAcross) {
+            first += (uint64_t)(s * DEPTH) * O.stride;
+            rows = s * DEPTH < O.deep ? min(DEPTH, O.deep - s * DEPTH) : 0u;
+            offset = 0;
+            there = true;
+        }
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(first), 0, (int)(rows * O.stride), 0x00020000);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            load_into_lds(buffer, to + ((uint32_t)i * WAVES + wave) * 1024u, there ? at[i] : kNowhere, offset);
+    }
+    // Where a lane reads: its place in the block of 32 rows or columns from `begin` on, and the operand of a quarter from there.
+    static __device__ __forceinline__ uint32_t place_of(uint32_t begin, uint32_t lane)
+    {
+        if constexpr (!kAcross) {
+            return (begin + lane % 32u) * 128u + (lane / 32u ^ lane / 2u % 8u) * 16u;
+        } else if constexpr (sizeof(T) == 2) {               // four columns of row k % 4 = lane / 4 % 4
+            const uint32_t k = lane / 32u * 8u + lane / 4u % 4u, c = begin / 32u ^ k % 4u;
+            return k * ROW + c * 64u + lane / 16u % 2u * 32u + lane % 4u * 8u;
+        } else {
+            return lane / 32u * 4u * ROW + (begin / 32u ^ lane / 32u) * 128u + lane % 32u * 4u;
+        }
+    }
+    template <int N>
+    static __device__ __forceinline__ void read(Chunk (&to)[N], const char *__restrict__ from, uint32_t place, int quarter)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (!kAcross) {
+                to[i] = *reinterpret_cast<const Chunk *>(from + (place ^ (uint32_t)quarter * 32u) + i * 4096);
+            } else if constexpr (sizeof(T) == 2) {           // (the blocks of a wave: i ^ k % 4 in steps of 64 bytes)
+                const char *const at = from + (place ^ (uint32_t)i * 64u) + quarter * 16 * (int)ROW;
+                const HalfChunk low = read_transposed(at), high = read_transposed(at + 4 * ROW);
+                to[i] = Chunk{low[0], low[1], high[0], high[1]};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    to[i][e] = *reinterpret_cast<const uint32_t *>(from + (place ^ (uint32_t)i * 128u) + (quarter * 8 + e) * (int)ROW);
+            }
+        }
+    }
+};
+
+template <class T, int BM_, int BN_, int WM_, int WN_, bool kAcrossA = false, bool kAcrossB = false>
 struct ProductTile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int MI = BM / WM / 32, NI = BN / WN / 32;             // blocks of a wave
     static constexpr int STAGE = (BM + BN) * 128, LDS = 2 * STAGE;
-    static constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;         // loads per wave and step, of eight rows each
-    static_assert(LA * 8 * WAVES == BM && LB * 8 * WAVES == BN, "whole loads");
+    using LoadsA = OperandLoads<T, BM, WAVES, kAcrossA>;
+    using LoadsB = OperandLoads<T, BN, WAVES, kAcrossB>;
 
     Block acc[MI][NI];
 
-    // chunks: of 16 bytes per row, the operands' depth; what lies behind them in a row is not read.
-    __device__ __forceinline__ void run(const TileRows &A, const TileRows &B, uint32_t chunks, char *lds)
+    __device__ __forceinline__ explicit ProductTile(char *lds_) : lds(lds_), half(0u)
     {
-        const uint32_t lane = threadIdx.x % 64u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
-        Loads L{__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(A.first), 0, (int)(A.there * A.stride), 0x00020000),
-                __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(B.first), 0, (int)(B.there * B.stride), 0x00020000),
-                {}, {}, lane % 8u ^ lane / 8u, wave};
-        places(L.a, A, L.chunk, wave, lane);
-        places(L.b, B, L.chunk, wave, lane);
-        const uint32_t swizzled = (lane / 32u ^ lane % 8u) * 16u;
-        const uint32_t a = (wave / WN * (BM / WM) + lane % 32u) * 128u + swizzled;
-        const uint32_t b = BM * 128u + (wave % WN * (BN / WN) + lane % 32u) * 128u + swizzled;
+        const uint32_t lane = threadIdx.x % 64u;
+        wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
+        place_a = LoadsA::place_of(wave / WN * (BM / WM), lane);
+        place_b = BM * 128u + LoadsB::place_of(wave % WN * (BN / WN), lane);
+    }
+    // The tile whose products come next: its first step goes into the half of the LDS that is free.
+    __device__ __forceinline__ void begin(const Operand &A, const Operand &B)
+    {
+        const uint32_t lane = threadIdx.x % 64u;
+        a.place(A, wave, lane);
+        b.place(B, wave, lane);
+        char *const to = lds + half * STAGE;
+        a.issue(0u, to, wave);
+        b.issue(0u, to + BM * 128, wave);
+    }
+    // Its products but those of the last of `steps` steps (at least one), which finish() brings.  Between the two is the place of begin()
+    // for the tile after it: that tile's first loads are on their way while this one's results are written.
+    __device__ __forceinline__ void run(uint32_t steps)
+    {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int j = 0; j < NI; ++j)
                 acc[i][j] = Block{};
-        const uint32_t steps = (chunks + 7u) / 8u;
-        if (steps == 0)
-            return;
-#pragma unroll
-        for (int quarter = 0; quarter < 4; ++quarter)
-            issue(L, quarter, 0u, chunks, lds);
-        uint32_t s = 0;
-        for (; s + 1u < steps; ++s) {
+        for (uint32_t s = 0; s + 1u < steps; ++s) {
             arrive();
-            step<true>(lds + s % 2u * STAGE, lds + (s + 1u) % 2u * STAGE, a, b, L, s + 1u, chunks);
+            step(lds + half * STAGE, lds + (half ^ 1u) * STAGE, true, s + 1u);
+            half ^= 1u;
         }
         arrive();
-        step<false>(lds + s % 2u * STAGE, lds, a, b, L, 0u, 0u);
-        __syncthreads();                                     // (the LDS is free for what follows)
+        half ^= 1u;
     }
+    __device__ __forceinline__ void finish() { step(lds + (half ^ 1u) * STAGE, lds + half * STAGE, false, 0u); }
+
+    // Rows n of results in 16 bits by way of the LDS's free half, so that 16 bytes of a lane and whole lines of a wave are written: call
+    // behind finish(), from all waves.  value(j, i, q, x): x[e] of column 8 q + 4 (lane / 32) + e of block i, row lane % 32 of block j.
+    // to(j, row): where the wave's columns of that row are, none for a row that is not there; `have` of them are.
+    template <class V, class P>
+    __device__ __forceinline__ void store_rows(V &&value, P &&to, int64_t have)
+    {
+        static_assert(sizeof(T) == 2, "16 bits");
+        constexpr uint32_t CHUNKS = MI * 4, PER = 64 / CHUNKS;            // of a row; rows per instruction
+        static_assert(WAVES * 32 * CHUNKS * 16 <= STAGE, "a wave's rows");
+        const uint32_t lane = threadIdx.x % 64u, row = lane % 32u;
+        const auto turn = [](uint32_t r) { return CHUNKS == 16u ? r % 16u : r / 2u % 8u; };      // (as the operands': no bank twice)
+        char *const own = lds + (half ^ 1u) * STAGE + wave * (32u * CHUNKS * 16u);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the others still read this half
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    typedef T T4 __attribute__((ext_vector_type(4)));
+                    float x[4];
+                    value(j, i, q, x);
+                    *reinterpret_cast<T4 *>(own + row * (CHUNKS * 16u) + (((uint32_t)(i * 4 + q) ^ turn(row)) * 16u) + lane / 32u * 8u) =
+                        T4{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (uint32_t k = 0; k < 32u / PER; ++k) {
+                const uint32_t r = k * PER + lane / CHUNKS, c = lane % CHUNKS;
+                const Chunk chunk = *reinterpret_cast<const Chunk *>(own + r * (CHUNKS * 16u) + (c ^ turn(r)) * 16u);
+                T *const at = to(j, r);
+                if (at) {
+                    typedef T T8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+                    const T8 x = __builtin_bit_cast(T8, chunk);
+                    const int64_t left = have - (int64_t)c * 8;
+                    if (left >= 8) {
+                        *reinterpret_cast<T8 *>(at + c * 8u) = x;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < left)
+                                at[c * 8u + e] = x[e];
+                    }
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    // The wave's first column and row in the tile.
+    __device__ __forceinline__ uint32_t first_m() const { return wave / WN * (BM / WM); }
+    __device__ __forceinline__ uint32_t first_n() const { return wave % WN * (BN / WN); }
 
 private:
-    struct Loads {
-        __amdgpu_buffer_rsrc_t ra, rb;
-        uint32_t a[LA], b[LB];                               // offsets of the lane's chunks at depth 0
-        uint32_t chunk, wave;                                // the lane's chunk in every row that it loads
-    };
-    template <int N>
-    static __device__ __forceinline__ void places(uint32_t (&to)[N], const TileRows &R, uint32_t chunk, uint32_t wave, uint32_t lane)
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t row = ((uint32_t)i * WAVES + wave) * 8u + lane / 8u;
-            to[i] = row < R.there ? row * R.stride + chunk * 16u : kNowhere;
-        }
-    }
-    // The loads of one quarter of step s.
-    static __device__ __forceinline__ void issue(const Loads &L, int quarter, uint32_t s, uint32_t chunks, char *__restrict__ to)
-    {
-        using Lds = __attribute__((address_space(3))) void *;
-        const bool there = L.chunk + s * 8u < chunks;
-#pragma unroll
-        for (int i = quarter * (LA + LB) / 4; i < (quarter + 1) * (LA + LB) / 4; ++i) {
-            if (i < LA)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(L.ra, (Lds)(to + (i * WAVES + L.wave) * 1024u), 16, there ? L.a[i < LA ? i : 0] : kNowhere,
-                                                         s * 128u, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rb, (Lds)(to + BM * 128 + ((i - LA) * WAVES + L.wave) * 1024u), 16,
-                                                         there ? L.b[i < LA ? 0 : i - LA] : kNowhere, s * 128u, 0, 0);
-        }
-    }
-    // All loads of all waves are in the LDS, and all reads of the other half are done.
+    char *const lds;
+    LoadsA a;
+    LoadsB b;
+    uint32_t wave, half, place_a, place_b;
+
+    // All loads of all waves are in the LDS, and all reads of the other half are done.  (By the builtin, not inline asm: what else was loaded
+    // before is there too, and the compiler knows.)
     static __device__ __forceinline__ void arrive()
     {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
-    static __device__ __forceinline__ void operands(Chunk (&x)[MI], Chunk (&y)[NI], const char *__restrict__ from, uint32_t a, uint32_t b,
-                                                    int quarter)
-    {
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-            x[i] = *reinterpret_cast<const Chunk *>(from + (a ^ (uint32_t)quarter * 32u) + i * 4096);
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-            y[j] = *reinterpret_cast<const Chunk *>(from + (b ^ (uint32_t)quarter * 32u) + j * 4096);
-    }
-    // The products of the half `from`; the loads of step `next` into the half `to`.  (That the two do not overlap has to be said: reads
+    // The products of the half `from`; if `load`, the loads of step `next` into the half `to`.  (That the two do not overlap has to be said: reads
     // of the LDS would wait for the loads otherwise.  The order is fixed: left to itself the compiler asks for the loads last.)
-    template <bool kLoad>
-    __device__ __forceinline__ void step(const char *__restrict__ from, char *__restrict__ to, uint32_t a, uint32_t b, const Loads &L,
-                                         uint32_t next, uint32_t chunks)
+    __device__ __forceinline__ void step(const char *__restrict__ from, char *__restrict__ to, bool load, uint32_t next)
     {
         Chunk x[2][MI], y[2][NI];
-        operands(x[0], y[0], from, a, b, 0);
+        LoadsA::read(x[0], from, place_a, 0);
+        LoadsB::read(y[0], from, place_b, 0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int quarter = 0; quarter < 4; ++quarter) {
-            if (quarter < 3)
-                operands(x[(quarter + 1) & 1], y[(quarter + 1) & 1], from, a, b, quarter + 1);
-            if (kLoad && quarter < 2) {                      // (early, so that they have the step to arrive)
-                issue(L, 2 * quarter, next, chunks, to);
-                issue(L, 2 * quarter + 1, next, chunks, to);
+            if (quarter < 3) {
+                LoadsA::read(x[(quarter + 1) & 1], from, place_a, quarter + 1);
+                LoadsB::read(y[(quarter + 1) & 1], from, place_b, quarter + 1);
             }
+            if (load && quarter == 0)                       // (early, so that they have the step to arrive)
+                a.issue(next, to, wave);
+            if (load && quarter == 1)
+                b.issue(next, to + BM * 128, wave);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < MI; ++i)

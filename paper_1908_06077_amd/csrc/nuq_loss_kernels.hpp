@@ -95,26 +95,28 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
         tile.finish();
         if (mw >= P.O.vocab)
             continue;
+        // (what the lane's columns are compared with is moved by the lane's half, not the 64 columns: those would fill the registers)
         const uint32_t there = min(GROUP, P.O.vocab - mw);
+        const int32_t lane_there = (int32_t)(there - half);
         const uint64_t group = mw / GROUP;
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
             const uint32_t n = nw + j * 32u;
             const bool row = n < P.O.rows;
             const uint32_t at = (uint64_t)target[j] - mw < there ? (uint32_t)((uint64_t)target[j] - mw) : ~0u;
+            const uint32_t lane_at = at - half;
             float top = -__builtin_inff(), sum = 0.0f, all = 0.0f, wanted = 0.0f;
 #pragma unroll
             for (int i = 0; i < Tile::MI; ++i) {
                 __builtin_amdgcn_sched_barrier(0);           // (a block after the other: there are no registers for more)
                 for_block(i, [&](uint32_t m, int r) {
                     float z = tile.acc[i][j][r];
-                    m += half;
-                    if (m == at)
+                    if (m == lane_at)
                         wanted = z;
                     if constexpr (kSmooth)
-                        all += m < there ? z : 0.0f;
-                    if (there < GROUP)
-                        tile.acc[i][j][r] = z = m < there ? z : -__builtin_inff();
+                        all += (int32_t)m < lane_there ? z : 0.0f;
+                    z = (int32_t)m < lane_there ? z : -__builtin_inff();
+                    tile.acc[i][j][r] = z;
                     top = fmaxf(top, z);
                 });
             }
@@ -350,13 +352,14 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradi
         tile.finish();
         // d of columns 8 q + half to 8 q + half + 3 of block i, of the lane's row of block j
         const auto gradient = [&](int j, int i, int q, float (&x)[4]) {
-            const uint32_t m = mw + i * 32u + q * 8u + half, target = (uint32_t)code[j] - P.first;   // (none in the piece: no place in it)
+            const uint32_t m = i * 32u + q * 8u, target = (uint32_t)code[j] - P.first - mw - half;   // (none in the piece: no place in it)
+            const int32_t there = code[j] >= 0 ? (int32_t)(P.O.vocab - mw - half) : 0;
 #pragma unroll
             for (uint32_t e = 0; e < 4u; ++e) {
                 float v = __builtin_amdgcn_exp2f((tile.acc[i][j][q * 4 + e] - lse[j]) * kLog2E) - P.smoothed;
                 if (m + e == target)
                     v -= P.wanted;
-                x[e] = code[j] >= 0 && m + e < P.O.vocab ? v * kGradientScale<T> : 0.0f;
+                x[e] = (int32_t)(m + e) < there ? v * kGradientScale<T> : 0.0f;
             }
         };
         const auto row = [&](int j, uint32_t r) -> T * {

@@ -544,7 +544,7 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
  *   g = scale * drop(dt);  h = g * gate;   dx = rstd1 * (h' - mean(h') - n1 * mean(h' n1)),  h' = h * inner_weight  (or h)
  * (mean(d) and mean(h') fall away with NUQ_RMS_NORM), and the sums over rows, each of which may be NULL:  dinner_weight of h n1,
  * dinner_bias of h, dgate of g b, douter_weight of dy n2, douter_bias of dy: in fp32 in a fixed order, with at most rows / 256 + 64
- * roundings of the summed magnitudes, rounded once.  dx may be dy or x, dresidual may be dtotal or total, at the same stride (not
+ * roundings of the summed magnitudes (of g n1 and g, times the vectors that are constant along the sum), rounded once.  dx may be dy or x, dresidual may be dtotal or total, at the same stride (not
  * where a sum is asked for over more than 8192 columns: NUQ_EINVAL); the two must not overlap.  workspace: DEVICE memory of nuq_residual_norm_workspace_bytes(rows, hidden) bytes, 16-byte aligned,
  * overwritten; may be NULL where no sum is asked for. */
 uint64_t nuq_residual_norm_workspace_bytes(uint64_t rows, uint32_t hidden);

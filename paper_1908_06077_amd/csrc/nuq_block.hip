@@ -54,6 +54,11 @@ int with_seam_shape(uint32_t hidden, F &&f)
 }
 constexpr uint32_t kSumsInRegisters = 8192;                  // columns; wider rows have their sums taken by a launch of its own
 
+// Forward, from so many threads of rows on teams take several rows each, and their vectors of weights go into the LDS, where four of so
+// many columns leave a CU two workgroups.
+constexpr uint32_t kManyThreads = 1u << 19;
+constexpr int kManyColumns = 2048;
+
 // Workgroups that write partial sums of the weights' gradients, and such rows of workgroups for wide rows.
 constexpr uint32_t kSeamParts = 512, kWideParts = 64;
 static_assert(kSeamParts <= 1024, "nuq_residual_norm_workspace_bytes");
@@ -106,7 +111,7 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
                               void *total, uint64_t ldt, void *y, uint64_t ldy, float *stats, nuq_stream_t stream)
 {
     ResidualNormForward P{x, residual, inner_weight, inner_bias, gate, outer_weight, outer_bias, total, y, stats, {}, rows, ldx, ldr,
-                          ldt, ldy, hidden, inner, outer, eps, scale, residual_scale};
+                          ldt, ldy, hidden, inner, outer, eps, 0.0f, residual_scale};
     if (!valid_seam(rows, hidden, type, weight_type, inner, outer, scale, residual_scale,
                     {inner_weight, inner_bias, gate, outer_weight, outer_bias}) || !draws_of(p, seed, step, P.draws) ||
         !std::isfinite(eps) || eps < 0.0f || (inner == NUQ_NO_NORM && (inner_weight || inner_bias)) ||
@@ -114,6 +119,7 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
         return NUQ_EINVAL;
     if (rows == 0)
         return NUQ_OK;
+    P.factor = scale * P.draws.keep;
     const uint32_t w = width(type);
     if (!valid_array(x, 1, w) || off_grid(residual, w) || !valid_array(total, 1, w) ||
         (outer != NUQ_NO_NORM && !valid_array(y, 1, w)) || (rows > 1 && (ldt < hidden || (y && ldy < hidden))))
@@ -124,17 +130,23 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
         using W = typename decltype(wt)::type;
         return with_seam_shape<T, false>(hidden, [&](auto team, auto elements, auto vec) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
-            const auto run = [&](auto inner_c) {
-                constexpr bool kInner = decltype(inner_c)::value;
-                constexpr uint32_t WG = kSeamForwardWG<TEAM>, TEAMS = WG / TEAM;
-                const uint32_t most = resident_workgroups<k_residual_norm_forward<T, W, TEAM, E, VEC, kInner>>(WG);
+            const auto run = [&](auto inner_c, auto many_c) {
+                constexpr bool kInner = decltype(inner_c)::value, kMany = decltype(many_c)::value;
+                constexpr uint32_t WG = kSeamForwardWG<TEAM, kMany>, TEAMS = WG / TEAM;
+                const uint32_t most = resident_workgroups<k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany>>(WG);
                 if (!most)
                     return (int)NUQ_EHIP;
                 const uint32_t grid = (uint32_t)std::min<uint64_t>((rows + TEAMS - 1) / TEAMS, most);
-                hipLaunchKernelGGL((k_residual_norm_forward<T, W, TEAM, E, VEC, kInner>), dim3(grid), dim3(WG), 0, st, P);
+                hipLaunchKernelGGL((k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany>), dim3(grid), dim3(WG), 0, st, P);
                 return check_launch();
             };
-            return inner != NUQ_NO_NORM ? run(std::true_type{}) : run(std::false_type{});
+            const auto with_inner = [&](auto many_c) {
+                return inner != NUQ_NO_NORM ? run(std::true_type{}, many_c) : run(std::false_type{}, many_c);
+            };
+            if constexpr (TEAM * E <= kManyColumns && VEC > 1)
+                if (rows > kManyThreads / TEAM)
+                    return with_inner(std::true_type{});
+            return with_inner(std::false_type{});
         });
     });
 }
@@ -154,7 +166,7 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
 {
     ResidualNormBackward P{dy, dtotal, x, total, inner_weight, inner_bias, gate, outer_weight, stats, dx, dresidual,
                            static_cast<float *>(workspace), nullptr, {}, rows, ldg, lda, ldx, ldt, ldd, lde, hidden, inner, outer,
-                           scale, residual_scale};
+                           0.0f, residual_scale};
     const bool sums = dinner_weight || dinner_bias || dgate || douter_weight || douter_bias;
     if (!valid_seam(rows, hidden, type, weight_type, inner, outer, scale, residual_scale,
                     {inner_weight, inner_bias, gate, outer_weight, dinner_weight, dinner_bias, dgate, douter_weight, douter_bias}) ||
@@ -176,6 +188,7 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
         return NUQ_ECAPACITY;
     if (hidden > kSumsInRegisters && sums && outer != NUQ_NO_NORM)
         P.means = P.partial + (uint64_t)kSeamSums * hidden * std::min<uint64_t>(rows, 1024u);
+    P.factor = scale * P.draws.keep;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return with_types(type, weight_type, [&](auto tt, auto wt) {
         using T = typename decltype(tt)::type;
@@ -211,8 +224,8 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
         });
         if (rc != NUQ_OK || !sums)
             return rc;
-        const SeamVectors V{{dinner_weight, dinner_bias, dgate, douter_weight, douter_bias}};
-        hipLaunchKernelGGL((k_residual_norm_finish<W>), dim3((hidden + 15u) / 16u, kSeamSums), dim3(1024), 0, st, P.partial, parts,
+        const SeamVectors V{inner_weight, inner_bias, gate, dinner_weight, dinner_bias, dgate, douter_weight, douter_bias, P.factor};
+        hipLaunchKernelGGL((k_residual_norm_finish<W>), dim3((hidden + 15u) / 16u, 3), dim3(1024), 0, st, P.partial, parts,
                            hidden, V);
         return check_launch();
     });

@@ -21,14 +21,25 @@ struct Draws {
     __device__ __forceinline__ uint64_t begin() const { return seed + (step ? (uint64_t)*step * kStepStride : 0ull); }
 };
 
-// x[e] *= what stands for element at + e of the row whose key this is.  What is dropped is 0, whatever it was.
+// x[e] <- 0 where element at + e of the row whose key this is is dropped, whatever it was.  (u >= T for the upper 24 bits u of a word is
+// word >= 2^8 T, whatever the other bits; T = 2^24 drops all.)
 template <int N>
-__device__ __forceinline__ void drop(float (&x)[N], BucketKey key, uint32_t at, uint32_t threshold, float keep)
+__device__ __forceinline__ void drop(float (&x)[N], BucketKey key, uint32_t at, uint32_t threshold)
 {
-    const uint32_t first = (key.k0 + at) * kRngC1;
+    const uint32_t first = (key.k0 + at) * kRngC1, least = threshold << 8;
+    if (threshold >> 24) {
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-        x[e] = draw24(first + (uint32_t)e * kRngC1, key.k1) >= threshold ? x[e] * keep : 0.0f;
+        for (int e = 0; e < N; ++e)
+            x[e] = 0.0f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const uint32_t y = first + (uint32_t)e * kRngC1;
+            uint32_t word = __builtin_amdgcn_bitop3_b32(y, y >> 15, key.k1, 0x96) * kRngC2;      // draw24, before its last shift
+            word ^= word >> 16;
+            x[e] = word >= least ? x[e] : 0.0f;
+        }
+    }
 }
 
 struct Dropout {
@@ -59,8 +70,12 @@ __global__ __launch_bounds__(256) void k_dropout(const Dropout P)
         load_some<VEC>(x, static_cast<const T *>(P.x) + row * P.ldx + at, have);
         if constexpr (kResidual)
             load_some<VEC>(r, static_cast<const T *>(P.residual) + row * P.ldr + at, have);
-        if (P.draws.threshold)
-            drop<VEC>(x, bucket_key(begin, row), at, P.draws.threshold, P.draws.keep);
+        if (P.draws.threshold) {
+            drop<VEC>(x, bucket_key(begin, row), at, P.draws.threshold);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                x[e] *= P.draws.keep;
+        }
         if constexpr (kResidual)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)

@@ -542,14 +542,12 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackw
     store_from_float<VEC>(out + P.hidden, db);
 }
 
-// out <- the sums of `parts` vectors of `hidden` floats that stand `stride` floats apart, in a fixed order: 16 columns at a time per
-// workgroup of 1024, 64 threads to each.
-template <class W>
-__device__ __forceinline__ void column_totals(const float *partial, uint64_t stride, uint32_t parts, uint32_t hidden, W *out)
+// put(column, sum) for the sums of `parts` vectors of `hidden` floats that stand `stride` floats apart, in a fixed order: 16 columns at a
+// time per workgroup of 1024, 64 threads to each.
+template <class F>
+__device__ __forceinline__ void column_totals(const float *partial, uint64_t stride, uint32_t parts, uint32_t hidden, F &&put)
 {
     __shared__ float red[64][17];
-    if (!out)
-        return;
     const uint32_t c = threadIdx.x % 16u, group = threadIdx.x / 16u;
     for (uint32_t begin = blockIdx.x * 16u;;) {
         const uint32_t col = begin + c;
@@ -577,7 +575,7 @@ __device__ __forceinline__ void column_totals(const float *partial, uint64_t str
                 sum += red[part * 16u + k][cc];
             sum = team_sum<4>(sum);
             if (part == 0 && to < hidden)
-                out[to] = (W)sum;
+                put(to, sum);
         }
         begin += gridDim.x * 16u;                            // (hidden is at most 2^30, a grid's columns 2^24)
         if (begin >= hidden)
@@ -591,7 +589,9 @@ template <class W>
 __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, W *dweight,
                                                             W *dbias)
 {
-    column_totals(partial + (uint64_t)blockIdx.y * hidden, 2ull * hidden, parts, hidden, blockIdx.y ? dbias : dweight);
+    W *const out = blockIdx.y ? dbias : dweight;
+    if (out)
+        column_totals(partial + (uint64_t)blockIdx.y * hidden, 2ull * hidden, parts, hidden, [&](uint32_t c, float sum) { out[c] = (W)sum; });
 }
 
 }  // namespace nuq

@@ -8,11 +8,15 @@
 //   dresidual = residual_scale dt;  g = scale drop(dt);  dgate = sum g n';  h = g gate;  dw1 = sum h n;  db1 = sum h
 //   dx = rstd1 (h w1 - mean(h w1) - n mean(h w1 n))      (mean(.) alone falls away in the root-mean-square norm; sums are over rows)
 //
+// The five sums over rows are four: with u = drop(dt) / keep and c = scale keep, U1 = sum u n and U0 = sum u,
+//   dw1 = c gate U1;  db1 = c gate U0;  dgate = c (w1 U1 + b1 U0);  and h w1 = u (c gate w1)
 // A row stays in the registers of one team of threads from its loads to its results: two rows are read and two written forward,
 // four read and two written backward, whatever is fused.  Statistics and sums are fp32, the variance is taken of centred values,
 // results are rounded to their type once.  The mask is computed again in the backward pass.  Bound by HBM, and on short batches by
 // latency.
 #pragma once
+
+#include <type_traits>
 
 #include "nuq_dropout_kernels.hpp"
 
@@ -28,19 +32,32 @@ struct ResidualNormForward {
     Draws draws;
     uint64_t rows, ldx, ldr, ldt, ldy;
     uint32_t hidden, inner, outer;
-    float eps, scale, residual_scale;
+    float eps, factor, residual_scale;         // factor: scale times what is kept is multiplied with
 };
 
-// Sums over the threads of a row, one after the other: a set of red is not written again before a barrier that follows its last read,
-// because the two sets take turns.
-template <int TEAM>
+// Sums over the threads of a row, one after the other, the same bits in each: a set of red is not written again before a barrier that
+// follows its last read, because the two sets take turns.  The teams of a workgroup meet at the barriers of teams of several waves.
+template <int TEAM, int WAVES>
 struct RowSums {
-    float (&red)[2][TEAM > 64 ? TEAM / 64 : 1];
+    float (&red)[2][WAVES];
     uint32_t turn;
     __device__ __forceinline__ float operator()(float x)
     {
-        turn ^= 1u;
-        return row_sum<TEAM>(x, red[turn]);
+        if constexpr (TEAM <= 64) {
+            return team_sum<TEAM>(x);
+        } else {
+            turn ^= 1u;
+            x = team_sum<64>(x);
+            if (threadIdx.x % 64u == 0)
+                red[turn][threadIdx.x / 64u] = x;
+            __syncthreads();
+            const uint32_t own = threadIdx.x / TEAM * (TEAM / 64);
+            x = red[turn][own];
+#pragma unroll
+            for (int k = 1; k < TEAM / 64; ++k)
+                x += red[turn][own + k];
+            return x;
+        }
     }
 };
 
@@ -53,7 +70,107 @@ __device__ __forceinline__ void arrived(const V (&x)[NV])
         asm volatile("" ::"v"(x[k]));
 }
 
-// A vector of `hidden` weights, which may be none, beside a team's row: in registers for all rows, or read again where it is used.
+// add(k, e) for the elements of a row that count, which are not a neighbour's too: `whole`, where the row is whole vectors, as one choice
+// per vector.  The two numbers that add() adds to.
+struct Pair {
+    float a, b;
+};
+template <class Shape, int NV, int VEC, class F>
+__device__ __forceinline__ Pair add_up(const Shape &S, bool whole, F &&add)
+{
+    Pair all{0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        Pair part = all;
+        if (whole) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                add(k, e, part);
+            all = S.there(k) ? part : all;
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                Pair next = all;
+                add(k, e, next);
+                all = S.counts(k, e) ? next : all;
+            }
+        }
+    }
+    return all;
+}
+
+// s <- N(s), its mean and reciprocal deviation.  between(): behind the first barrier, before s changes.
+template <class Sums, class Shape, int NV, int VEC, class F>
+__device__ __forceinline__ void norm_row(float (&s)[NV][VEC], const Shape &S, bool whole, Sums &sums, uint32_t kind, float per, float eps,
+                                         float &mean, float &rstd, F &&between)
+{
+    mean = 0.0f;
+    if (kind == kLayerNorm) {
+        mean = sums(add_up<Shape, NV, VEC>(S, whole, [&](int k, int e, Pair &p) { p.a += s[k][e]; }).a) * per;
+        between();
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                s[k][e] -= mean;
+    }
+    const float square = sums(add_up<Shape, NV, VEC>(S, whole, [&](int k, int e, Pair &p) { p.a = __builtin_fmaf(s[k][e], s[k][e], p.a); }).a);
+    rstd = 1.0f / __builtin_sqrtf(square * per + eps);
+    if (kind != kLayerNorm)
+        between();
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            s[k][e] *= rstd;
+}
+
+// Vectors of `hidden` floats in the LDS for all teams of a workgroup, as the team's threads have the row: written by its first team, read
+// by the thread of a team that has the same columns.  Registers are what waves per SIMD depend on, and those the bytes on their way.
+template <int COUNT, class Shape>
+struct TeamVectors {
+    static constexpr int UNIT = Shape::VEC < 4 ? Shape::VEC : 4, UNITS = Shape::NV * Shape::VEC / UNIT;
+    typedef float Unit __attribute__((ext_vector_type(UNIT)));
+    using Memory = Unit[COUNT][UNITS][Shape::TEAM];
+    Memory &at;
+    __device__ __forceinline__ void put(int which, const float (&x)[Shape::NV][Shape::VEC])
+    {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            Unit v;
+#pragma unroll
+            for (int e = 0; e < UNIT; ++e)
+                v[e] = x[(u * UNIT + e) / Shape::VEC][(u * UNIT + e) % Shape::VEC];
+            at[which][u][threadIdx.x % (uint32_t)Shape::TEAM] = v;
+        }
+    }
+    __device__ __forceinline__ void get(int which, float (&x)[Shape::NV][Shape::VEC]) const
+    {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const Unit v = at[which][u][threadIdx.x % (uint32_t)Shape::TEAM];
+#pragma unroll
+            for (int e = 0; e < UNIT; ++e)
+                x[(u * UNIT + e) / Shape::VEC][(u * UNIT + e) % Shape::VEC] = v[e];
+        }
+    }
+};
+
+// to[k][e] <- the vector's element of that place, or `other` where there is no vector.
+template <class W, class Shape, int NV, int VEC>
+__device__ __forceinline__ void vector_or(float (&to)[NV][VEC], const void *from, const Shape &S, float other)
+{
+    Vec<W, VEC> x[NV];
+    if (from)
+        S.load(x, static_cast<const W *>(from));
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            to[k][e] = from ? (float)x[k][e] : other;
+}
+
+// A vector of weights where a team has few rows: in its registers (kHold), or read where it is used.
 template <class Shape, class W, int NV, int VEC, bool kHold>
 struct RowVector {
     const W *from;
@@ -78,14 +195,6 @@ struct RowVector {
             each(now, f);
         }
     }
-    __device__ __forceinline__ void multiply(const Shape &S, float (&s)[NV][VEC]) const
-    {
-        apply(S, [&](int k, int e, float w) { s[k][e] *= w; });
-    }
-    __device__ __forceinline__ void add(const Shape &S, float (&s)[NV][VEC]) const
-    {
-        apply(S, [&](int k, int e, float w) { s[k][e] += w; });
-    }
 
 private:
     template <class F>
@@ -99,128 +208,163 @@ private:
     }
 };
 
-// Threads of a workgroup.
-template <int TEAM>
-constexpr int kSeamForwardWG = TEAM <= 64 ? 256 : TEAM;
+// Forward: threads of a workgroup.  kMany: there are many rows per team.  What is done to n1 and n2 is then one multiply-add each, by
+// vectors in the LDS: A = w1 gate factor, B = b1 gate factor, w2, b2.
+template <int TEAM, bool kMany>
+constexpr int kSeamForwardWG = kMany ? 1024 : TEAM <= 64 ? 256 : TEAM;
 
-// s <- N(s), its mean and reciprocal deviation.  between(): behind the first barrier, before s changes.
-template <int TEAM, class Shape, int NV, int VEC, class F>
-__device__ __forceinline__ void norm_row(float (&s)[NV][VEC], const Shape &S, RowSums<TEAM> &sums, uint32_t kind, float per, float eps,
-                                         float &mean, float &rstd, F &&between)
-{
-    mean = 0.0f;
-    if (kind == kLayerNorm) {
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                sum += S.counts(k, e) ? s[k][e] : 0.0f;
-        mean = sums(sum) * per;
-        between();
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                s[k][e] -= mean;
-    }
-    float square = 0.0f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            square = __builtin_fmaf(S.counts(k, e) ? s[k][e] : 0.0f, s[k][e], square);
-    rstd = 1.0f / __builtin_sqrtf(sums(square) * per + eps);
-    if (kind != kLayerNorm)
-        between();
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            s[k][e] *= rstd;
-}
-
-template <class T, class W, int TEAM, int E, int VEC, bool kInner>
-__global__ __launch_bounds__(kSeamForwardWG<TEAM>) void k_residual_norm_forward(const ResidualNormForward P)
+template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kMany>
+__global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm_forward(const ResidualNormForward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
-    constexpr int NV = Shape::NV, TEAMS = kSeamForwardWG<TEAM> / TEAM;
-    // the vectors of weights, and the next row ahead, in registers: not beside sixteen elements
-    constexpr bool kHold = E <= 8, kAhead = E <= 8;
-    __shared__ float red[2][TEAM > 64 ? TEAM / 64 : 1];
+    constexpr int NV = Shape::NV, WG = kSeamForwardWG<TEAM, kMany>, TEAMS = WG / TEAM;
+    constexpr bool kAhead = kMany || E <= 8;                 // (the next row in registers: not beside sixteen elements and their weights)
+    using Few = RowVector<Shape, W, NV, VEC, (!kMany && E <= 8)>;
+    using Many = TeamVectors<4, Shape>;
+    __shared__ typename std::conditional<kMany, typename Many::Memory, char>::type kept;
+    __shared__ float red[2][WG / 64];
     const uint32_t hidden = P.hidden;
+    const bool whole = hidden % VEC == 0;
     const float per = 1.0f / (float)hidden;
     const Shape S(hidden);
-    RowSums<TEAM> sums{red, 0u};
+    RowSums<TEAM, WG / 64> sums{red, 0u};
     uint32_t team = threadIdx.x / TEAM;
     if constexpr (TEAM >= 64)
         team = uniform_u32(team);
-    uint64_t row = (uint64_t)blockIdx.x * TEAMS + team;
-    if (row >= P.rows)                                       // (a whole team; teams of more than a wave are the workgroup)
-        return;
     const uint64_t begin = P.draws.begin();
     Vec<T, VEC> xs[NV], rs[NV];
-    const auto load = [&]() {
-        S.load(xs, static_cast<const T *>(P.x) + row * P.ldx);
-        S.load(rs, static_cast<const T *>(P.residual ? P.residual : P.x) + row * (P.residual ? P.ldr : P.ldx));
-    };
-    if constexpr (kAhead)
-        load();
-    using Weights = RowVector<Shape, W, NV, VEC, kHold>;
-    const Weights w1(kInner ? P.w1 : nullptr, S), b1(kInner ? P.b1 : nullptr, S), gate(P.gate, S), w2(P.w2, S), b2(P.b2, S);
+    const T *const residual = static_cast<const T *>(P.residual ? P.residual : P.x);        // (without one, x: read, and not used)
+    const uint64_t ldr = P.residual ? P.ldr : P.ldx;
+    // (a team without a row in the workgroup's last turn takes the last row along, and writes nothing: teams meet at barriers)
+    const auto row_of = [&](uint64_t first) { return min(first + team, P.rows - 1u); };
+    const uint64_t turn = (uint64_t)gridDim.x * TEAMS;
+    uint64_t first = (uint64_t)blockIdx.x * TEAMS;
+    if constexpr (kAhead) {
+        S.load(xs, static_cast<const T *>(P.x) + row_of(first) * P.ldx);
+        S.load(rs, residual + row_of(first) * ldr);
+    }
+    const Few w1(kMany || !kInner ? nullptr : P.w1, S), b1(kMany || !kInner ? nullptr : P.b1, S), gate(kMany ? nullptr : P.gate, S),
+        w2(kMany ? nullptr : P.w2, S), b2(kMany ? nullptr : P.b2, S);
+    if constexpr (kMany) {
+        Many M{kept};
+        if (threadIdx.x < (uint32_t)TEAM) {
+            float a[NV][VEC], b[NV][VEC], g[NV][VEC];
+            vector_or<W>(g, P.gate, S, 1.0f);
+            vector_or<W>(a, P.w1, S, 1.0f);
+            vector_or<W>(b, P.b1, S, 0.0f);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    g[k][e] *= P.factor;
+                    a[k][e] *= g[k][e];
+                    b[k][e] *= g[k][e];
+                }
+            M.put(0, a);
+            M.put(1, b);
+            vector_or<W>(a, P.w2, S, 1.0f);
+            vector_or<W>(b, P.b2, S, 0.0f);
+            M.put(2, a);
+            M.put(3, b);
+        }
+        __syncthreads();
+    }
     for (;;) {
-        const uint64_t now = row;
-        if constexpr (!kAhead)
-            load();
+        const uint64_t now = row_of(first);
+        const bool own = first + team < P.rows;
+        if constexpr (!kAhead) {
+            S.load(xs, static_cast<const T *>(P.x) + now * P.ldx);
+            S.load(rs, residual + now * ldr);
+        }
         float s[NV][VEC], mean, rstd;
-        Vec<T, VEC> r[NV];
         if constexpr (TEAM > 64)
             arrived(rs);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            r[k] = rs[k];
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
                 s[k][e] = (float)xs[k][e];
-        }
-        row += (uint64_t)gridDim.x * TEAMS;
-        const bool more = row < P.rows;
+        first += turn;
+        const bool more = first < P.rows;
         if (kAhead && more)
-            load();
+            S.load(xs, static_cast<const T *>(P.x) + row_of(first) * P.ldx);
         if constexpr (kInner) {
-            norm_row<TEAM>(s, S, sums, P.inner, per, P.eps, mean, rstd, [] {});
-            if (P.stats && threadIdx.x % TEAM == 0) {
+            norm_row(s, S, whole, sums, P.inner, per, P.eps, mean, rstd, [] {});
+            if (P.stats && own && threadIdx.x % TEAM == 0) {
                 if (P.inner == kLayerNorm)
                     P.stats[now] = mean;
                 P.stats[P.rows + now] = rstd;
             }
-            w1.multiply(S, s);
-            b1.add(S, s);
         }
-        gate.multiply(S, s);
+        if constexpr (kMany) {
+            float a[NV][VEC], b[NV][VEC];
+            const Many M{kept};
+            M.get(0, a);
+            if constexpr (kInner)
+                M.get(1, b);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    s[k][e] = kInner ? __builtin_fmaf(s[k][e], a[k][e], b[k][e]) : s[k][e] * a[k][e];
+        } else {
+            w1.apply(S, [&](int k, int e, float w) { s[k][e] *= w; });
+            b1.apply(S, [&](int k, int e, float w) { s[k][e] += w; });
+            gate.apply(S, [&](int k, int e, float w) { s[k][e] *= w; });
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    s[k][e] *= P.factor;
+        }
         if (P.draws.threshold) {
             const BucketKey key = bucket_key(begin, now);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
-                drop<VEC>(s[k], key, S.at[k], P.draws.threshold, P.draws.keep);
+                drop<VEC>(s[k], key, S.at[k], P.draws.threshold);
         }
+        if (P.residual)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    s[k][e] = __builtin_fmaf((float)rs[k][e], P.residual_scale, s[k][e]);
+        if (kAhead && more)
+            S.load(rs, residual + row_of(first) * ldr);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                s[k][e] = (float)(T)(s[k][e] * P.scale + (P.residual ? (float)r[k][e] * P.residual_scale : 0.0f));
+                s[k][e] = (float)(T)s[k][e];
         if (P.outer == kNoNorm) {                            // (behind a barrier of the inner norm: total may be x or residual)
-            S.store(static_cast<T *>(P.total) + now * P.ldt, s);
+            if (own)
+                S.store(static_cast<T *>(P.total) + now * P.ldt, s);
         } else {
-            norm_row<TEAM>(s, S, sums, P.outer, per, P.eps, mean, rstd, [&] { S.store(static_cast<T *>(P.total) + now * P.ldt, s); });
-            if (P.stats && threadIdx.x % TEAM == 0) {
+            norm_row(s, S, whole, sums, P.outer, per, P.eps, mean, rstd, [&] {
+                if (own)
+                    S.store(static_cast<T *>(P.total) + now * P.ldt, s);
+            });
+            if (P.stats && own && threadIdx.x % TEAM == 0) {
                 if (P.outer == kLayerNorm)
                     P.stats[2u * P.rows + now] = mean;
                 P.stats[3u * P.rows + now] = rstd;
             }
-            w2.multiply(S, s);
-            b2.add(S, s);
-            S.store(static_cast<T *>(P.y) + now * P.ldy, s);
+            if constexpr (kMany) {
+                float a[NV][VEC], b[NV][VEC];
+                const Many M{kept};
+                M.get(2, a);
+                M.get(3, b);
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        s[k][e] = __builtin_fmaf(s[k][e], a[k][e], b[k][e]);
+            } else {
+                w2.apply(S, [&](int k, int e, float w) { s[k][e] *= w; });
+                b2.apply(S, [&](int k, int e, float w) { s[k][e] += w; });
+            }
+            if (own)
+                S.store(static_cast<T *>(P.y) + now * P.ldy, s);
         }
         if (!more)
             break;
@@ -232,17 +376,17 @@ struct ResidualNormBackward {
     const void *w1, *b1, *gate, *w2;           // each may be none
     const float *stats;
     void *dx, *dresidual;                      // dresidual: may be none
-    float *partial;                            // [parts][5][hidden]: sums of h n, of h, of g n', of dy n2, of dy; or none
+    float *partial;                            // [parts][4][hidden]: sums of u n, of u, of dy n2, of dy; or none
     float *means;                              // [2][rows] or none: mean(d), mean(d n2), for the sums that a launch of its own takes
     Draws draws;
     uint64_t rows, ldg, lda, ldx, ldt, ldd, lde;
     uint32_t hidden, inner, outer;
-    float scale, residual_scale;
+    float factor, residual_scale;              // factor: scale times what is kept is multiplied with
 };
-constexpr uint32_t kSeamSums = 5;
+constexpr uint32_t kSeamSums = 4;
 
 template <int TEAM>
-constexpr int kSeamBackwardWG = TEAM <= 64 ? 256 : TEAM <= 512 ? 512 : TEAM;
+constexpr int kSeamBackwardWG = TEAM <= 512 ? 512 : TEAM;
 
 // Two sums over the threads of a row, the same bits in each; one barrier.
 template <int TEAM, int WAVES>
@@ -272,15 +416,19 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (&red)[2][2][
     }
 }
 
-// kSums: with the sums over rows, in registers; workgroup p writes partial[p], and a second launch adds those up.
+// kSums: with the sums over rows, in registers; workgroup p writes partial[p], and a second launch adds those up.  w2 and c gate w1 are in
+// the LDS.
 template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kSums>
-__global__ __launch_bounds__(kSeamBackwardWG<TEAM>) void k_residual_norm_backward(const ResidualNormBackward P)
+__global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_residual_norm_backward(const ResidualNormBackward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
     constexpr int NV = Shape::NV, WG = kSeamBackwardWG<TEAM>, TEAMS = WG / TEAM, WAVES = WG / 64;
-    constexpr bool kHold = E <= 8;                           // (the vectors of weights, and all operands at once: not beside sixteen elements)
+    constexpr bool kAhead = TEAM < 1024 && sizeof(T) == 2;   // (the next row in registers, where these hold it)
+    using Vectors = TeamVectors<2, Shape>;
+    __shared__ typename Vectors::Memory kept;
     __shared__ float red[2][2][WAVES];
     const uint32_t hidden = P.hidden;
+    const bool whole = hidden % VEC == 0;
     const Shape S(hidden);
     const float per = 1.0f / (float)hidden;
     const bool outer = P.outer != kNoNorm;
@@ -289,11 +437,38 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>) void k_residual_norm_backwar
         team = uniform_u32(team);
     const uint64_t begin = P.draws.begin();
     float total_of[kSeamSums][NV][VEC] = {};
-    using Weights = RowVector<Shape, W, NV, VEC, kHold>;
-    const Weights w1(kInner ? P.w1 : nullptr, S), b1(kInner && kSums ? P.b1 : nullptr, S), gate(P.gate, S), w2(P.w2, S);
+    // What a pass does without reads something that is there in its place, and does not use it.
+    const T *const dy = static_cast<const T *>(outer ? P.dy : P.x), *const total = static_cast<const T *>(outer ? P.total : P.x);
+    const T *const dtotal = P.dtotal ? static_cast<const T *>(P.dtotal) : dy, *const x = static_cast<const T *>(P.x);
+    const uint64_t ldg = outer ? P.ldg : P.ldx, ldt = outer ? P.ldt : P.ldx, lda = P.dtotal ? P.lda : ldg;
+    Vec<T, VEC> gs[NV], ts[NV], as[NV], xs[NV];
+    const uint64_t on = (uint64_t)gridDim.x * TEAMS;
+    uint64_t first = (uint64_t)blockIdx.x * TEAMS;
+    if (kAhead && first + team < P.rows) {
+        S.load(gs, dy + (first + team) * ldg);
+        S.load(ts, total + (first + team) * ldt);
+        S.load(as, dtotal + (first + team) * lda);
+        S.load(xs, x + (first + team) * P.ldx);
+    }
+    Vectors V{kept};
+    if (threadIdx.x < (uint32_t)TEAM) {
+        float a[NV][VEC], b[NV][VEC];
+        vector_or<W>(a, P.w2, S, 1.0f);
+        V.put(0, a);
+        vector_or<W>(a, P.gate, S, 1.0f);
+        vector_or<W>(b, kInner ? P.w1 : nullptr, S, 1.0f);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                a[k][e] = a[k][e] * P.factor * b[k][e];
+        V.put(1, a);
+    }
+    __syncthreads();
     // (teams of several waves meet at barriers in every row: a workgroup's teams take equally many turns)
-    for (uint64_t first = (uint64_t)blockIdx.x * TEAMS; first < P.rows; first += (uint64_t)gridDim.x * TEAMS) {
+    for (; first < P.rows; first += on) {
         const uint64_t row = first + team;
+        const bool more = kAhead && row + on < P.rows;
         if (row >= P.rows) {                                 // (the workgroup's last turn: only barriers are left to meet)
             if constexpr (TEAM > 64) {
                 __syncthreads();
@@ -302,19 +477,14 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>) void k_residual_norm_backwar
             }
             break;
         }
-        Vec<T, VEC> xs[NV], as[NV];
-        const auto load_x = [&]() { S.load(xs, static_cast<const T *>(P.x) + row * P.ldx); };
-        float d[NV][VEC], n[NV][VEC];
+        if constexpr (!kAhead) {
+            S.load(gs, dy + row * ldg);
+            S.load(ts, total + row * ldt);
+            S.load(as, dtotal + row * lda);
+        }
+        float d[NV][VEC], n[NV][VEC], w[NV][VEC];
         if (outer) {
-            Vec<T, VEC> gs[NV], ts[NV];
-            S.load(gs, static_cast<const T *>(P.dy) + row * P.ldg);
-            S.load(ts, static_cast<const T *>(P.total) + row * P.ldt);
-            // (without a gradient through the sum, dy in its place: read, and not added)
-            S.load(as, static_cast<const T *>(P.dtotal ? P.dtotal : P.dy) + row * (P.dtotal ? P.lda : P.ldg));
-            if constexpr (kHold && (kInner || kSums))
-                load_x();
             const float mean = P.outer == kLayerNorm ? P.stats[2u * P.rows + row] : 0.0f, rstd = P.stats[3u * P.rows + row];
-            float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -322,37 +492,41 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>) void k_residual_norm_backwar
                     n[k][e] = ((float)ts[k][e] - mean) * rstd;
                     d[k][e] = (float)gs[k][e];
                     if constexpr (kSums) {
-                        total_of[3][k][e] = __builtin_fmaf(d[k][e], n[k][e], total_of[3][k][e]);
-                        total_of[4][k][e] += d[k][e];
+                        total_of[2][k][e] = __builtin_fmaf(d[k][e], n[k][e], total_of[2][k][e]);
+                        total_of[3][k][e] += d[k][e];
                     }
                 }
-            w2.multiply(S, d);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float c = S.counts(k, e) ? d[k][e] : 0.0f;
-                    s1 += c;
-                    s2 = __builtin_fmaf(c, n[k][e], s2);
-                }
-            if constexpr (TEAM > 64)
-                arrived(as);
-            row_sums<TEAM, WAVES>(s1, s2, red, turn);
-            s1 = P.outer == kLayerNorm ? s1 * per : 0.0f;
-            s2 *= per;
-            if (P.means && threadIdx.x % TEAM == 0) {
-                P.means[row] = s1;
-                P.means[P.rows + row] = s2;
+            if (more) {
+                S.load(gs, dy + (row + on) * ldg);
+                S.load(ts, total + (row + on) * ldt);
             }
+            V.get(0, w);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    d[k][e] = (d[k][e] - s1 - n[k][e] * s2) * rstd + (P.dtotal ? (float)as[k][e] : 0.0f);
+                    d[k][e] *= w[k][e];
+            Pair sum = add_up<Shape, NV, VEC>(S, whole, [&](int k, int e, Pair &p) {
+                p.a += d[k][e];
+                p.b = __builtin_fmaf(d[k][e], n[k][e], p.b);
+            });
+            if constexpr (TEAM > 64)
+                arrived(as);
+            row_sums<TEAM, WAVES>(sum.a, sum.b, red, turn);
+            sum.a = P.outer == kLayerNorm ? sum.a * per : 0.0f;
+            sum.b *= per;
+            if (P.means && threadIdx.x % TEAM == 0) {
+                P.means[row] = sum.a;
+                P.means[P.rows + row] = sum.b;
+            }
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    d[k][e] = __builtin_fmaf(-n[k][e], sum.b, d[k][e] - sum.a);
+                    d[k][e] = P.dtotal ? __builtin_fmaf(d[k][e], rstd, (float)as[k][e]) : d[k][e] * rstd;
+                }
         } else {
-            S.load(as, static_cast<const T *>(P.dtotal) + row * P.lda);
-            if constexpr (kHold && (kInner || kSums))
-                load_x();
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -363,6 +537,8 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>) void k_residual_norm_backwar
                 __syncthreads();
             }
         }
+        if (more)
+            S.load(as, dtotal + (row + on) * lda);
         if (P.dresidual) {                                   // (behind a barrier: dresidual may be dtotal or total)
             float through[NV][VEC];
 #pragma unroll
@@ -372,76 +548,47 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>) void k_residual_norm_backwar
                     through[k][e] = d[k][e] * P.residual_scale;
             S.store(static_cast<T *>(P.dresidual) + row * P.lde, through);
         }
-        if constexpr (!kHold && (kInner || kSums))
-            load_x();
+        if constexpr (!kAhead)
+            S.load(xs, x + row * P.ldx);
+        if (P.draws.threshold) {                             // d is u from here on
+            const BucketKey key = bucket_key(begin, row);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                drop<VEC>(d[k], key, S.at[k], P.draws.threshold);
+        }
+        const float mean = P.inner == kLayerNorm ? P.stats[row] : 0.0f, rstd = kInner ? P.stats[P.rows + row] : 1.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                n[k][e] = kInner ? ((float)xs[k][e] - mean) * rstd : (float)xs[k][e];
+                if constexpr (kSums) {
+                    total_of[0][k][e] = __builtin_fmaf(d[k][e], n[k][e], total_of[0][k][e]);
+                    if constexpr (kInner)
+                        total_of[1][k][e] += d[k][e];
+                }
+            }
+        if (more)
+            S.load(xs, x + (row + on) * P.ldx);
+        V.get(1, w);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                d[k][e] *= P.scale;
-        if (P.draws.threshold) {
-            const BucketKey key = bucket_key(begin, row);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-                drop<VEC>(d[k], key, S.at[k], P.draws.threshold, P.draws.keep);
-        }
+                d[k][e] *= w[k][e];
         if constexpr (kInner) {
-            const float mean = P.inner == kLayerNorm ? P.stats[row] : 0.0f, rstd = P.stats[P.rows + row];
-            float s1 = 0.0f, s2 = 0.0f;
+            Pair sum = add_up<Shape, NV, VEC>(S, whole, [&](int k, int e, Pair &p) {
+                p.a += d[k][e];
+                p.b = __builtin_fmaf(d[k][e], n[k][e], p.b);
+            });
+            row_sums<TEAM, WAVES>(sum.a, sum.b, red, turn);
+            sum.a = P.inner == kLayerNorm ? sum.a * per : 0.0f;
+            sum.b *= per;
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    n[k][e] = ((float)xs[k][e] - mean) * rstd;
-            if constexpr (kSums) {
-                float whole[NV][VEC];
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        whole[k][e] = n[k][e];
-                w1.multiply(S, whole);
-                b1.add(S, whole);
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        total_of[2][k][e] = __builtin_fmaf(d[k][e], whole[k][e], total_of[2][k][e]);
-            }
-            gate.multiply(S, d);
-            if constexpr (kSums)
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        total_of[0][k][e] = __builtin_fmaf(d[k][e], n[k][e], total_of[0][k][e]);
-                        total_of[1][k][e] += d[k][e];
-                    }
-            w1.multiply(S, d);
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float c = S.counts(k, e) ? d[k][e] : 0.0f;
-                    s1 += c;
-                    s2 = __builtin_fmaf(c, n[k][e], s2);
-                }
-            row_sums<TEAM, WAVES>(s1, s2, red, turn);
-            s1 = P.inner == kLayerNorm ? s1 * per : 0.0f;
-            s2 *= per;
-#pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    d[k][e] = (d[k][e] - s1 - n[k][e] * s2) * rstd;
-        } else {
-            if constexpr (kSums)
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        total_of[2][k][e] = __builtin_fmaf(d[k][e], (float)xs[k][e], total_of[2][k][e]);
-            gate.multiply(S, d);
+                    d[k][e] = __builtin_fmaf(-n[k][e], sum.b, d[k][e] - sum.a) * rstd;
         }
         S.store(static_cast<T *>(P.dx) + row * P.ldd, d);
     }
@@ -494,16 +641,10 @@ __global__ __launch_bounds__(256) void k_residual_norm_columns(const ResidualNor
     const uint32_t at = min(col, P.hidden - VEC);
     const bool outer = P.outer != kNoNorm, inner = P.inner != kNoNorm;
     const uint64_t begin = P.draws.begin();
-    float w1[VEC], b1[VEC] = {}, gate[VEC], w2[VEC];
+    float w2[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
-        w1[e] = gate[e] = w2[e] = 1.0f;
-    if (P.w1)
-        load_as_float<VEC>(w1, static_cast<const W *>(P.w1) + at);
-    if (P.b1)
-        load_as_float<VEC>(b1, static_cast<const W *>(P.b1) + at);
-    if (P.gate)
-        load_as_float<VEC>(gate, static_cast<const W *>(P.gate) + at);
+        w2[e] = 1.0f;
     if (P.w2)
         load_as_float<VEC>(w2, static_cast<const W *>(P.w2) + at);
     float total_of[kSeamSums][VEC] = {};
@@ -521,24 +662,21 @@ __global__ __launch_bounds__(256) void k_residual_norm_columns(const ResidualNor
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     n[e] = (n[e] - mean) * rstd;
-                    part[3][e] = __builtin_fmaf(d[e], n[e], part[3][e]);
-                    part[4][e] += d[e];
-                    d[e] = (d[e] * w2[e] - s1 - n[e] * s2) * rstd;
+                    part[2][e] = __builtin_fmaf(d[e], n[e], part[2][e]);
+                    part[3][e] += d[e];
+                    d[e] = __builtin_fmaf(-n[e], s2, d[e] * w2[e] - s1) * rstd;
                 }
             }
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                d[e] = (d[e] + a[e]) * P.scale;
+                d[e] += a[e];
             if (P.draws.threshold)
-                drop<VEC>(d, bucket_key(begin, row), at, P.draws.threshold, P.draws.keep);
+                drop<VEC>(d, bucket_key(begin, row), at, P.draws.threshold);
             load_as_float<VEC>(n, static_cast<const T *>(P.x) + row * P.ldx + at);
             const float mean = P.inner == kLayerNorm ? P.stats[row] : 0.0f, rstd = inner ? P.stats[P.rows + row] : 1.0f;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                n[e] = (n[e] - mean) * rstd;
-                part[2][e] = __builtin_fmaf(d[e], n[e] * w1[e] + b1[e], part[2][e]);
-                d[e] *= gate[e];
-                part[0][e] = __builtin_fmaf(d[e], n[e], part[0][e]);
+                part[0][e] = __builtin_fmaf(d[e], (n[e] - mean) * rstd, part[0][e]);
                 part[1][e] += d[e];
             }
         }
@@ -555,14 +693,37 @@ __global__ __launch_bounds__(256) void k_residual_norm_columns(const ResidualNor
 }
 
 struct SeamVectors {
-    void *to[kSeamSums];                                     // dw1, db1, dgate, dw2, db2; each may be none
+    const void *w1, *b1, *gate;                              // each may be none
+    void *dw1, *db1, *dgate, *dw2, *db2;                     // each may be none
+    float factor;
 };
 
+// The gradients of the vectors from the partial sums: blockIdx.y 0 those of the branch, 1 and 2 dw2 and db2.  Sixteen columns per workgroup.
 template <class W>
 __global__ __launch_bounds__(1024) void k_residual_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, const SeamVectors V)
 {
-    column_totals(partial + (uint64_t)blockIdx.y * hidden, (uint64_t)kSeamSums * hidden, parts, hidden,
-                  static_cast<W *>(V.to[blockIdx.y]));
+    const uint64_t stride = (uint64_t)kSeamSums * hidden;
+    if (blockIdx.y > 0u) {
+        W *const out = static_cast<W *>(blockIdx.y == 1u ? V.dw2 : V.db2);
+        if (out)
+            column_totals(partial + (1u + blockIdx.y) * hidden, stride, parts, hidden, [&](uint32_t c, float sum) { out[c] = (W)sum; });
+        return;
+    }
+    if (!V.dw1 && !V.db1 && !V.dgate)
+        return;
+    float with_n = 0.0f;
+    column_totals(partial, stride, parts, hidden, [&](uint32_t, float sum) { with_n = sum; });
+    __syncthreads();
+    column_totals(partial + hidden, stride, parts, hidden, [&](uint32_t c, float sum) {        // (the same thread, the same column)
+        const auto of = [&](const void *v, float other) { return v ? (float)static_cast<const W *>(v)[c] : other; };
+        const float g = of(V.gate, 1.0f) * V.factor;
+        if (V.dw1)
+            static_cast<W *>(V.dw1)[c] = (W)(g * with_n);
+        if (V.db1)
+            static_cast<W *>(V.db1)[c] = (W)(g * sum);
+        if (V.dgate)
+            static_cast<W *>(V.dgate)[c] = (W)(V.factor * __builtin_fmaf(of(V.w1, 1.0f), with_n, of(V.b1, 0.0f) * sum));
+    });
 }
 
 }  // namespace nuq

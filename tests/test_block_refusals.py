@@ -27,7 +27,7 @@ FORWARD = dict(x=16, ldx=8, residual=16, ldr=8, inner=1, w1=None, b1=None, gate=
                stream=None)
 BACKWARD = dict(dy=16, ldg=8, dtotal=16, lda=8, x=16, ldx=8, total=16, ldt=8, inner=1, w1=None, b1=None, gate=None, outer=1, w2=None, rows=2,
                 hidden=8, scale=1.0, residual_scale=1.0, p=0.1, seed=1, step=None, type=0, weight_type=0, stats=16, dx=16, ldd=8,
-                dresidual=16, lde=8, dw1=16, db1=16, dgate=16, dw2=16, db2=16, workspace=64, bytes=320, stream=None)
+                dresidual=16, lde=8, dw1=16, db1=16, dgate=16, dw2=16, db2=16, workspace=64, bytes=256, stream=None)
 BOTH = (dict(x=None), dict(x=18), dict(hidden=0), dict(hidden=16385), dict(rows=2 ** 31), dict(type=3), dict(type=1, weight_type=2),
         dict(inner=3), dict(outer=3), dict(inner=0, outer=0, y=None, dy=None), dict(w1=18), dict(b1=18), dict(gate=18), dict(w2=18),
         dict(scale=NAN), dict(residual_scale=float("inf")), dict(p=-0.1), dict(p=NAN), dict(p=1.01), dict(step=12), dict(stats=18),
@@ -46,7 +46,7 @@ def test_residual_norm_forward():
 
 def test_residual_norm_backward():
     size = nuq.nuq_residual_norm_workspace_bytes
-    assert size(2, 8) == 2 * 8 * 20 and size(10 ** 6, 8) == 1024 * 160 and size(3, 10 ** 4) == 3 * 20 * 10 ** 4 + 24
+    assert size(2, 8) == 2 * 8 * 16 and size(10 ** 6, 8) == 1024 * 128 and size(3, 10 ** 4) == 3 * 16 * 10 ** 4 + 24
     call = _lib().nuq_residual_norm_backward
     bare = dict(dw1=None, db1=None, dw2=None, db2=None)
     for bad in BOTH + (dict(dy=None), dict(dy=18), dict(total=None), dict(dx=None), dict(dx=18), dict(ldd=7), dict(lde=7), dict(stats=None),
@@ -58,7 +58,7 @@ def test_residual_norm_backward():
     wide = dict(hidden=9000, ldg=9000, lda=9000, ldx=9000, ldt=9000, ldd=9000, lde=9000, bytes=10 ** 7, dx=32, dresidual=48)
     for bad in (dict(dx=16), dict(dresidual=16)):                             # the sums of wide rows: not from rows that were replaced
         assert call(*{**BACKWARD, **wide, **bad}.values()) == EINVAL, bad
-    assert call(*{**BACKWARD, "bytes": 319}.values()) == ECAPACITY
+    assert call(*{**BACKWARD, "bytes": 255}.values()) == ECAPACITY
 
 
 def test_binding_refuses_tensors_that_do_not_fit(monkeypatch):

@@ -154,10 +154,12 @@ def backward_formula(x, total, dy, dtotal, v, stats, inner, outer, numbers, f):
         n = (n - m1 if inner == "layer" else n) * r1
     whole = n * w1 + b1
     bar_whole = 5 * U * (n * w1).abs() + U * whole.abs()
-    out["dgate"] = ((g * whole).sum(0), (bar * whole.abs() + g.abs() * bar_whole).sum(0) + many * (g * whole).abs().sum(0))
-    h, bar = g * gate, bar * gate.abs() + U * (g * gate).abs()
-    out["dw1"] = ((h * n).sum(0), (bar * n.abs() + 4 * U * (h * n).abs()).sum(0) + many * (h * n).abs().sum(0))
-    out["db1"] = (h.sum(0), bar.sum(0) + many * h.abs().sum(0))
+    # dgate is w1 sum(g n) + b1 sum(g), so it is those magnitudes that round
+    parts = (g * n * w1).abs() + (g * b1).abs()
+    out["dgate"] = ((g * whole).sum(0), (bar * ((n * w1).abs() + b1.abs()) + g.abs() * bar_whole + 6 * U * parts).sum(0) + many * parts.sum(0))
+    h, bar = g * gate, bar * gate.abs() + 3 * U * (g * gate).abs()
+    out["dw1"] = ((h * n).sum(0), (bar * n.abs() + 6 * U * (h * n).abs()).sum(0) + many * (h * n).abs().sum(0))
+    out["db1"] = (h.sum(0), bar.sum(0) + (many + 3 * U) * h.abs().sum(0))
     if inner != "none":
         h, bar = through(h * w1, bar * w1.abs() + U * (h * w1).abs(), n, r1, inner)
     out["dx"] = (h, bar)

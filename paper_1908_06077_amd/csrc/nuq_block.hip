@@ -26,9 +26,13 @@ bool draws_of(double p, uint64_t seed, const int64_t *step, Draws &to)
     return true;
 }
 
-// The team of threads, the elements per thread and the vectors that hold a row of `hidden` elements of type T.  At most eight
-// elements per thread leave registers for the vectors of weights, and backward for the sums of five gradients of them.
-template <class T, bool kBackward, class F>
+enum class SeamPass { kFew, kMany, kBackward };
+
+// The team of threads, the elements per thread and the vectors that hold a row of `hidden` elements of type T.  Every sum over a row costs
+// a wave some twenty instructions and a team of several waves a barrier, so teams are small where registers allow it: forward with many
+// rows a wave has up to 2048 columns; backward, beside four sums per column, sixteen elements per thread (eight in fp32).  A few rows
+// take eight and larger teams, for their latency.
+template <class T, SeamPass kPass, class F>
 int with_seam_shape(uint32_t hidden, F &&f)
 {
     using std::integral_constant;
@@ -41,23 +45,34 @@ int with_seam_shape(uint32_t hidden, F &&f)
     NUQ_SHAPE(4, 8)
     NUQ_SHAPE(16, 8)
     NUQ_SHAPE(64, 8)
-    NUQ_SHAPE(128, 8)
-    NUQ_SHAPE(256, 8)
-    NUQ_SHAPE(512, 8)
-    if constexpr (kBackward) {
-        NUQ_SHAPE(512, 16)
+    if constexpr (kPass == SeamPass::kMany) {
+        if constexpr (VEC == 8) {
+            NUQ_SHAPE(64, 16)
+            NUQ_SHAPE(128, 16)
+        } else {
+            NUQ_SHAPE(128, 8)
+            NUQ_SHAPE(256, 8)
+        }
+        return f(integral_constant<int, 0>{}, integral_constant<int, 0>{}, integral_constant<int, 0>{});
     } else {
-        NUQ_SHAPE(1024, 8)
+        NUQ_SHAPE(128, 8)
+        NUQ_SHAPE(256, 8)
+        NUQ_SHAPE(512, 8)
+        if constexpr (kPass == SeamPass::kBackward) {
+            NUQ_SHAPE(512, 16)
+        } else {
+            NUQ_SHAPE(1024, 8)
+        }
+        return f(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, integral_constant<int, VEC>{});
     }
 #undef NUQ_SHAPE
-    return f(integral_constant<int, 1024>{}, integral_constant<int, 16>{}, integral_constant<int, VEC>{});
 }
 constexpr uint32_t kSumsInRegisters = 8192;                  // columns; wider rows have their sums taken by a launch of its own
 
-// Forward, from so many threads of rows on teams take several rows each, and their vectors of weights go into the LDS, where four of so
-// many columns leave a CU two workgroups.
-constexpr uint32_t kManyThreads = 1u << 19;
-constexpr int kManyColumns = 2048;
+// Forward, from so many elements on teams take several rows each, and their vectors of weights go into the LDS, where four of so many
+// columns leave a CU several workgroups.
+constexpr uint64_t kManyElements = 1u << 22;
+constexpr uint32_t kManyColumns = 2048;
 
 // Workgroups that write partial sums of the weights' gradients, and such rows of workgroups for wide rows.
 constexpr uint32_t kSeamParts = 512, kWideParts = 64;
@@ -128,9 +143,9 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
     return with_types(type, weight_type, [&](auto tt, auto wt) {
         using T = typename decltype(tt)::type;
         using W = typename decltype(wt)::type;
-        return with_seam_shape<T, false>(hidden, [&](auto team, auto elements, auto vec) {
+        const auto run = [&](auto team, auto elements, auto vec, auto many_c) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
-            const auto run = [&](auto inner_c, auto many_c) {
+            const auto launch = [&](auto inner_c) {
                 constexpr bool kInner = decltype(inner_c)::value, kMany = decltype(many_c)::value;
                 constexpr uint32_t WG = kSeamForwardWG<TEAM, kMany>, TEAMS = WG / TEAM;
                 const uint32_t most = resident_workgroups<k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany>>(WG);
@@ -140,14 +155,16 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
                 hipLaunchKernelGGL((k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany>), dim3(grid), dim3(WG), 0, st, P);
                 return check_launch();
             };
-            const auto with_inner = [&](auto many_c) {
-                return inner != NUQ_NO_NORM ? run(std::true_type{}, many_c) : run(std::false_type{}, many_c);
-            };
-            if constexpr (TEAM * E <= kManyColumns && VEC > 1)
-                if (rows > kManyThreads / TEAM)
-                    return with_inner(std::true_type{});
-            return with_inner(std::false_type{});
-        });
+            return inner != NUQ_NO_NORM ? launch(std::true_type{}) : launch(std::false_type{});
+        };
+        if (hidden <= kManyColumns && rows * hidden > kManyElements)
+            return with_seam_shape<T, SeamPass::kMany>(hidden, [&](auto team, auto elements, auto vec) {
+                if constexpr (decltype(team)::value > 0)
+                    return run(team, elements, vec, std::true_type{});
+                else
+                    return (int)NUQ_EINVAL;                  // (no such width)
+            });
+        return with_seam_shape<T, SeamPass::kFew>(hidden, [&](auto team, auto elements, auto vec) { return run(team, elements, vec, std::false_type{}); });
     });
 }
 
@@ -194,7 +211,7 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
         using T = typename decltype(tt)::type;
         using W = typename decltype(wt)::type;
         uint32_t parts = 0;
-        const int rc = rows == 0 ? (int)NUQ_OK : with_seam_shape<T, true>(hidden, [&](auto team, auto elements, auto vec) {
+        const int rc = rows == 0 ? (int)NUQ_OK : with_seam_shape<T, SeamPass::kBackward>(hidden, [&](auto team, auto elements, auto vec) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
             constexpr uint32_t WG = kSeamBackwardWG<TEAM>, TEAMS = WG / TEAM;
             const auto run = [&](auto inner_c, auto sums_c) {

@@ -385,8 +385,12 @@ struct ResidualNormBackward {
 };
 constexpr uint32_t kSeamSums = 4;
 
+// Threads of a workgroup: several teams share what is written of the sums.  And waves per SIMD that the registers have to leave room for:
+// four beside eight elements per thread, two beside sixteen.
 template <int TEAM>
 constexpr int kSeamBackwardWG = TEAM <= 512 ? 512 : TEAM;
+template <int E>
+constexpr int kSeamBackwardWaves = E <= 8 ? 4 : 2;
 
 // Two sums over the threads of a row, the same bits in each; one barrier.
 template <int TEAM, int WAVES>
@@ -419,7 +423,7 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (&red)[2][2][
 // kSums: with the sums over rows, in registers; workgroup p writes partial[p], and a second launch adds those up.  w2 and c gate w1 are in
 // the LDS.
 template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kSums>
-__global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_residual_norm_backward(const ResidualNormBackward P)
+__global__ __launch_bounds__(kSeamBackwardWG<TEAM>, kSeamBackwardWaves<E>) void k_residual_norm_backward(const ResidualNormBackward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
     constexpr int NV = Shape::NV, WG = kSeamBackwardWG<TEAM>, TEAMS = WG / TEAM, WAVES = WG / 64;
@@ -442,14 +446,24 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_res
     const T *const dtotal = P.dtotal ? static_cast<const T *>(P.dtotal) : dy, *const x = static_cast<const T *>(P.x);
     const uint64_t ldg = outer ? P.ldg : P.ldx, ldt = outer ? P.ldt : P.ldx, lda = P.dtotal ? P.lda : ldg;
     Vec<T, VEC> gs[NV], ts[NV], as[NV], xs[NV];
+    // (The statistics with the rows: a load behind theirs would wait for them.  What a norm does not have is read, and not used.  All in one
+    // place and without a condition, so that what is waited for is counted, and not everything; a team without a row takes the last one.)
+    float mean1 = 0.0f, rstd1 = 0.0f, mean2 = 0.0f, rstd2 = 0.0f;
+    const auto load = [&](uint64_t row) {
+        row = min(row, P.rows - 1u);
+        mean1 = P.stats[row];
+        rstd1 = P.stats[P.rows + row];
+        mean2 = P.stats[2u * P.rows + row];
+        rstd2 = P.stats[3u * P.rows + row];
+        S.load(gs, dy + row * ldg);
+        S.load(ts, total + row * ldt);
+        S.load(as, dtotal + row * lda);
+        S.load(xs, x + row * P.ldx);
+    };
     const uint64_t on = (uint64_t)gridDim.x * TEAMS;
     uint64_t first = (uint64_t)blockIdx.x * TEAMS;
-    if (kAhead && first + team < P.rows) {
-        S.load(gs, dy + (first + team) * ldg);
-        S.load(ts, total + (first + team) * ldt);
-        S.load(as, dtotal + (first + team) * lda);
-        S.load(xs, x + (first + team) * P.ldx);
-    }
+    if constexpr (kAhead)
+        load(first + team);
     Vectors V{kept};
     if (threadIdx.x < (uint32_t)TEAM) {
         float a[NV][VEC], b[NV][VEC];
@@ -468,7 +482,6 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_res
     // (teams of several waves meet at barriers in every row: a workgroup's teams take equally many turns)
     for (; first < P.rows; first += on) {
         const uint64_t row = first + team;
-        const bool more = kAhead && row + on < P.rows;
         if (row >= P.rows) {                                 // (the workgroup's last turn: only barriers are left to meet)
             if constexpr (TEAM > 64) {
                 __syncthreads();
@@ -477,29 +490,34 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_res
             }
             break;
         }
-        if constexpr (!kAhead) {
-            S.load(gs, dy + row * ldg);
-            S.load(ts, total + row * ldt);
-            S.load(as, dtotal + row * lda);
-        }
+        if constexpr (!kAhead)
+            load(row);
         float d[NV][VEC], n[NV][VEC], w[NV][VEC];
+        Vec<T, VEC> through_sum[NV], branch[NV];             // (of the row; the arrays above are the next one's from here on)
+        const float m1 = P.inner == kLayerNorm ? mean1 : 0.0f, r1 = rstd1, m2 = P.outer == kLayerNorm ? mean2 : 0.0f, r2 = rstd2;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            through_sum[k] = as[k];
+            branch[k] = xs[k];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                n[k][e] = ((float)ts[k][e] - m2) * r2;
+                d[k][e] = (float)gs[k][e];
+            }
+        }
+        if constexpr (TEAM > 64)
+            arrived(through_sum);
+        if constexpr (kAhead)
+            load(row + on);
         if (outer) {
-            const float mean = P.outer == kLayerNorm ? P.stats[2u * P.rows + row] : 0.0f, rstd = P.stats[3u * P.rows + row];
+            if constexpr (kSums)
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
+                for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    n[k][e] = ((float)ts[k][e] - mean) * rstd;
-                    d[k][e] = (float)gs[k][e];
-                    if constexpr (kSums) {
+                    for (int e = 0; e < VEC; ++e) {
                         total_of[2][k][e] = __builtin_fmaf(d[k][e], n[k][e], total_of[2][k][e]);
                         total_of[3][k][e] += d[k][e];
                     }
-                }
-            if (more) {
-                S.load(gs, dy + (row + on) * ldg);
-                S.load(ts, total + (row + on) * ldt);
-            }
             V.get(0, w);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
@@ -510,35 +528,30 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_res
                 p.a += d[k][e];
                 p.b = __builtin_fmaf(d[k][e], n[k][e], p.b);
             });
-            if constexpr (TEAM > 64)
-                arrived(as);
             row_sums<TEAM, WAVES>(sum.a, sum.b, red, turn);
             sum.a = P.outer == kLayerNorm ? sum.a * per : 0.0f;
             sum.b *= per;
-            if (P.means && threadIdx.x % TEAM == 0) {
-                P.means[row] = sum.a;
-                P.means[P.rows + row] = sum.b;
-            }
+            if constexpr (!kSums)
+                if (P.means && threadIdx.x % TEAM == 0) {
+                    P.means[row] = sum.a;
+                    P.means[P.rows + row] = sum.b;
+                }
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     d[k][e] = __builtin_fmaf(-n[k][e], sum.b, d[k][e] - sum.a);
-                    d[k][e] = P.dtotal ? __builtin_fmaf(d[k][e], rstd, (float)as[k][e]) : d[k][e] * rstd;
+                    d[k][e] = P.dtotal ? __builtin_fmaf(d[k][e], r2, (float)through_sum[k][e]) : d[k][e] * r2;
                 }
         } else {
 #pragma unroll
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    d[k][e] = (float)as[k][e];
-            if constexpr (TEAM > 64) {
-                arrived(as);
+                    d[k][e] = (float)through_sum[k][e];
+            if constexpr (TEAM > 64)
                 __syncthreads();
-            }
         }
-        if (more)
-            S.load(as, dtotal + (row + on) * lda);
         if (P.dresidual) {                                   // (behind a barrier: dresidual may be dtotal or total)
             float through[NV][VEC];
 #pragma unroll
@@ -548,28 +561,23 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_res
                     through[k][e] = d[k][e] * P.residual_scale;
             S.store(static_cast<T *>(P.dresidual) + row * P.lde, through);
         }
-        if constexpr (!kAhead)
-            S.load(xs, x + row * P.ldx);
         if (P.draws.threshold) {                             // d is u from here on
             const BucketKey key = bucket_key(begin, row);
 #pragma unroll
             for (int k = 0; k < NV; ++k)
                 drop<VEC>(d[k], key, S.at[k], P.draws.threshold);
         }
-        const float mean = P.inner == kLayerNorm ? P.stats[row] : 0.0f, rstd = kInner ? P.stats[P.rows + row] : 1.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                n[k][e] = kInner ? ((float)xs[k][e] - mean) * rstd : (float)xs[k][e];
+                n[k][e] = kInner ? ((float)branch[k][e] - m1) * r1 : (float)branch[k][e];
                 if constexpr (kSums) {
                     total_of[0][k][e] = __builtin_fmaf(d[k][e], n[k][e], total_of[0][k][e]);
                     if constexpr (kInner)
                         total_of[1][k][e] += d[k][e];
                 }
             }
-        if (more)
-            S.load(xs, x + (row + on) * P.ldx);
         V.get(1, w);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
@@ -588,7 +596,7 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, (E <= 8 ? 4 : 1)) void k_res
             for (int k = 0; k < NV; ++k)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
-                    d[k][e] = __builtin_fmaf(-n[k][e], sum.b, d[k][e] - sum.a) * rstd;
+                    d[k][e] = __builtin_fmaf(-n[k][e], sum.b, d[k][e] - sum.a) * r1;
         }
         S.store(static_cast<T *>(P.dx) + row * P.ldd, d);
     }

@@ -242,7 +242,7 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
         if (rc != NUQ_OK || !sums)
             return rc;
         const SeamVectors V{inner_weight, inner_bias, gate, dinner_weight, dinner_bias, dgate, douter_weight, douter_bias, P.factor};
-        hipLaunchKernelGGL((k_residual_norm_finish<W>), dim3((hidden + 15u) / 16u, 3), dim3(1024), 0, st, P.partial, parts,
+        hipLaunchKernelGGL((k_residual_norm_finish<W>), dim3((hidden + 15u) / 16u, 2), dim3(1024), 0, st, P.partial, parts,
                            hidden, V);
         return check_launch();
     });

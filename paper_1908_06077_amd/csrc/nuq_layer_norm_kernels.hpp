@@ -542,38 +542,49 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const LayerNormBackw
     store_from_float<VEC>(out + P.hidden, db);
 }
 
-// put(column, sum) for the sums of `parts` vectors of `hidden` floats that stand `stride` floats apart, in a fixed order: 16 columns at a
-// time per workgroup of 1024, 64 threads to each.
-template <class F>
+// put(column, sums) for the sums of `parts` vectors of `hidden` floats that stand `stride` floats apart, of K such sets that stand one
+// behind the other, in a fixed order: 16 columns at a time per workgroup of 1024, 64 threads to each.
+template <int K, class F>
 __device__ __forceinline__ void column_totals(const float *partial, uint64_t stride, uint32_t parts, uint32_t hidden, F &&put)
 {
-    __shared__ float red[64][17];
+    __shared__ float red[K][64][17];
     const uint32_t c = threadIdx.x % 16u, group = threadIdx.x / 16u;
     for (uint32_t begin = blockIdx.x * 16u;;) {
         const uint32_t col = begin + c;
-        float sum = 0.0f;
+        float sum[K] = {};
         if (col < hidden) {
             const float *const from = partial + col;
             uint32_t p = group;
-            for (; p + 192u < parts; p += 256u) {            // four loads at once
-                float x[4];
+            for (; p + 192u < parts; p += 256u) {            // four loads of each at once
+                float x[K][4];
 #pragma unroll
-                for (uint32_t k = 0; k < 4u; ++k)
-                    x[k] = from[(p + 64u * k) * stride];
-                sum += (x[0] + x[1]) + (x[2] + x[3]);
+                for (int i = 0; i < K; ++i)
+#pragma unroll
+                    for (uint32_t k = 0; k < 4u; ++k)
+                        x[i][k] = from[(p + 64u * k) * stride + (uint32_t)i * hidden];
+#pragma unroll
+                for (int i = 0; i < K; ++i)
+                    sum[i] += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
             }
             for (; p < parts; p += 64u)
-                sum += from[p * stride];
+#pragma unroll
+                for (int i = 0; i < K; ++i)
+                    sum[i] += from[p * stride + (uint32_t)i * hidden];
         }
-        red[group][c] = sum;
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            red[i][group][c] = sum[i];
         __syncthreads();
         if (threadIdx.x < 64u) {                             // one wave: four lanes to a column
             const uint32_t cc = threadIdx.x / 4u, part = threadIdx.x % 4u, to = begin + cc;
-            sum = 0.0f;
 #pragma unroll
-            for (uint32_t k = 0; k < 16u; ++k)
-                sum += red[part * 16u + k][cc];
-            sum = team_sum<4>(sum);
+            for (int i = 0; i < K; ++i) {
+                sum[i] = 0.0f;
+#pragma unroll
+                for (uint32_t k = 0; k < 16u; ++k)
+                    sum[i] += red[i][part * 16u + k][cc];
+                sum[i] = team_sum<4>(sum[i]);
+            }
             if (part == 0 && to < hidden)
                 put(to, sum);
         }
@@ -591,7 +602,8 @@ __global__ __launch_bounds__(1024) void k_layer_norm_finish(const float *partial
 {
     W *const out = blockIdx.y ? dbias : dweight;
     if (out)
-        column_totals(partial + (uint64_t)blockIdx.y * hidden, 2ull * hidden, parts, hidden, [&](uint32_t c, float sum) { out[c] = (W)sum; });
+        column_totals<1>(partial + (uint64_t)blockIdx.y * hidden, 2ull * hidden, parts, hidden,
+                         [&](uint32_t c, const float (&sum)[1]) { out[c] = (W)sum[0]; });
 }
 
 }  // namespace nuq

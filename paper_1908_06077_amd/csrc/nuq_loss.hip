@@ -53,8 +53,8 @@ struct Parts {
     }
 };
 
-// Columns of rows that a workgroup takes, and the logits' groups: of 64 of the vocabulary where a wave has all of the rows.
-uint32_t group_of(uint32_t rows) { return rows <= 64 ? 64 : 128; }
+// The logits' groups: what a wave has of the vocabulary.
+uint32_t group_of(uint32_t rows) { return rows <= 64 ? 32 : rows <= 128 ? 64 : 128; }
 
 struct ForwardParts {
     char *x, *w;
@@ -95,11 +95,11 @@ uint32_t splits_of(uint64_t tiles, uint32_t steps, uint32_t most_splits)
 uint32_t tile_rows(uint32_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 uint32_t tile_columns(uint32_t columns) { return columns <= 128 ? 128 : 256; }
 
-// Entries of the vocabulary whose d is in the workspace at a time: at most 160 MiB of them (2048 at least), and of those numbers the one
+// Entries of the vocabulary whose d is in the workspace at a time: at most 320 MiB of them (2048 at least), and of those numbers the one
 // whose three products take the fewest steps of rounds of 256 tiles.
 uint32_t piece_of(const LossShape &S)
 {
-    const uint64_t row = (uint64_t)S.rows * S.bytes(), most = std::min<uint64_t>(std::max<uint64_t>((160ull << 20) / row, 2048u), 1u << 20) / 256u;
+    const uint64_t row = (uint64_t)S.rows * S.bytes(), most = std::min<uint64_t>(std::max<uint64_t>((320ull << 20) / row, 2048u), 1u << 20) / 256u;
     const uint64_t all = over(S.vocab, 256);
     if (all <= most)
         return (uint32_t)up(S.vocab, 64);
@@ -139,9 +139,11 @@ struct BackwardParts {
         largest = P.take<float>(1);
         clean = P.take<char>(S.rows * S.packed() * b);
         d = P.take<char>(S.rows * wide * b);
+        // for more than one set of sums: as much as d and the weights take
+        const uint64_t more = std::max<uint64_t>(4ull << 20, S.rows * wide * b + (uint64_t)S.vocab * S.hidden * b);
         const uint32_t depth = 128u / (uint32_t)b, steps = over(wide, depth);
-        splits = splits_of((uint64_t)over(S.hidden, S.rows > 128 ? tile_columns(S.hidden) : 256) * over(S.rows, tile_rows(S.rows)), steps,
-                           1u + (uint32_t)std::min<uint64_t>(63u, std::max<uint64_t>(4ull << 20, S.rows * wide * b) / (4u * S.rows * up(S.hidden, 4))));
+        splits = splits_of((uint64_t)over(S.hidden, S.rows > 128 ? tile_columns(S.hidden) : 128) * over(S.rows, tile_rows(S.rows)), steps,
+                           1u + (uint32_t)std::min<uint64_t>(63u, more / (4u * S.rows * up(S.hidden, 4))));
         each = over(steps, splits) * depth;
         ld_sums = up(S.hidden, 4);
         sums = P.take<float>(splits * S.rows * ld_sums);
@@ -153,15 +155,16 @@ struct BackwardParts {
 template <class T, bool kAcrossA, class F>
 int with_rows(uint32_t rows, F &&f)
 {
-    return rows > 128  ? f(Type<ProductTile<T, 256, 256, 2, 4, kAcrossA>>{})
-           : rows > 64 ? f(Type<ProductTile<T, 256, 128, 2, 2, kAcrossA>>{})
-           : rows > 32 ? f(Type<ProductTile<T, 256, 64, 4, 1, kAcrossA>>{})
-                       : f(Type<ProductTile<T, 256, 32, 4, 1, kAcrossA>>{});
+    return rows > 128  ? f(Type<ProductTile<T, 256, 256, 2, 4, 2, kAcrossA>>{})
+           : rows > 64 ? f(Type<ProductTile<T, 128, 128, 2, 2, 2, kAcrossA>>{})
+           : rows > 32 ? f(Type<ProductTile<T, 128, 64, 4, 1, 3, kAcrossA>>{})
+                       : f(Type<ProductTile<T, 128, 32, 4, 1, 4, kAcrossA>>{});
 }
 template <class T, bool kAcrossB, class F>
 int with_columns(uint32_t columns, F &&f)
 {
-    return columns > 128 ? f(Type<ProductTile<T, 256, 256, 2, 4, true, kAcrossB>>{}) : f(Type<ProductTile<T, 128, 256, 2, 4, true, kAcrossB>>{});
+    return columns > 128 ? f(Type<ProductTile<T, 256, 256, 2, 4, 2, true, kAcrossB>>{})
+                         : f(Type<ProductTile<T, 128, 256, 2, 4, 2, true, kAcrossB>>{});
 }
 
 template <class T>
@@ -223,7 +226,7 @@ int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *we
     if (!valid_loss(S, rows, target, smoothing, lse, workspace) || off_grid(loss, 4) || off_grid(mean, 4))
         return NUQ_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    LossJoin J{target, nullptr, nullptr, nullptr, loss, lse, loss, mean, flags_ptr(), ignore, S.rows, vocab, 0, smoothing};
+    LossJoin J{target, nullptr, nullptr, nullptr, loss, lse, mean, flags_ptr(), ignore, S.rows, vocab, 0, smoothing};
     if (!J.flags)
         return NUQ_EHIP;
     if (rows == 0) {
@@ -263,10 +266,13 @@ int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *we
     J.row_loss = loss ? loss : W.row_loss;
     J.groups = W.groups;
     if (rows <= 16) {
-        hipLaunchKernelGGL(k_loss_join<true>, dim3(1), dim3(1024), 0, st, J);
+        if (rows == 1)
+            hipLaunchKernelGGL((k_loss_join<1, true>), dim3(1), dim3(1024), 0, st, J);
+        else
+            hipLaunchKernelGGL((k_loss_join<16, true>), dim3(1), dim3(1024), 0, st, J);
         return check_launch();
     }
-    hipLaunchKernelGGL(k_loss_join<false>, dim3(over(rows, 16)), dim3(1024), 0, st, J);
+    hipLaunchKernelGGL((k_loss_join<16, false>), dim3(over(rows, 16)), dim3(1024), 0, st, J);
     if (mean)
         hipLaunchKernelGGL(k_loss_mean, dim3(1), dim3(1024), 0, st, J);
     return check_launch();
@@ -290,7 +296,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
     if (rows == 0)                                           // sums over no rows
         return !dweight ? (int)NUQ_OK : with_type(type, [&](auto tt) {
             using T = typename decltype(tt)::type;
-            using Tile = ProductTile<T, 256, 256, 2, 4, true, true>;
+            using Tile = ProductTile<T, 256, 256, 2, 4, 2, true, true>;
             LossProduct P{weight, weight, 16, 16, 0, 0, 0, 0, 0, hidden, vocab, over(hidden, Tile::BM), over(vocab, Tile::BN), dweight, lde, 0, nullptr};
             hipLaunchKernelGGL((k_loss_product<T, Tile, T, true, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
             return check_launch();
@@ -304,7 +310,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
     R.factor = W.factor;
     R.scale = W.scale;
     R.largest = W.largest;
-    hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(1024), 0, st, R);
+    hipLaunchKernelGGL(k_loss_rows, dim3(grad_per_row ? 1u : over(rows, 1024)), dim3(1024), 0, st, R);
     if (const int rc = check_launch(); rc != NUQ_OK)
         return rc;
     return with_type(type, [&](auto tt) {

@@ -50,9 +50,9 @@ struct LogitTiles {
         m0 *= Tile::BM;
         n0 *= Tile::BN;
         tile.begin({static_cast<const char *>(O.w) + (uint64_t)m0 * O.stride_w, O.stride_w, min((uint32_t)Tile::BM, O.vocab - m0), O.chunks},
-                   {static_cast<const char *>(O.x) + (uint64_t)n0 * O.stride_x, O.stride_x, min((uint32_t)Tile::BN, O.rows - n0), O.chunks});
+                   {static_cast<const char *>(O.x) + (uint64_t)n0 * O.stride_x, O.stride_x, min((uint32_t)Tile::BN, O.rows - n0), O.chunks},
+                   (O.chunks + 7u) / 8u);
     }
-    __device__ __forceinline__ uint32_t steps() const { return (O.chunks + 7u) / 8u; }
     // Whether there is another tile, which is begun.
     __device__ __forceinline__ bool next(Tile &tile)
     {
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j)
             target[j] = nw + j * 32u < P.O.rows ? P.target[nw + j * 32u] : -1;
-        tile.run(tiles.steps());
+        tile.run();
         more = tiles.next(tile);
         tile.finish();
         if (mw >= P.O.vocab)
@@ -145,8 +145,7 @@ struct LossJoin {
     const int64_t *target;
     const float2 *part;
     const float *sums, *of_target;             // sums: where targets are smoothed
-    float *loss, *lse;                         // loss: may be none
-    float *row_loss;                           // workspace, may be loss
+    float *row_loss, *lse;
     float *mean;                               // [2], may be none: the mean loss, and 1 / rows that count
     uint32_t *flags;
     int64_t ignore;
@@ -159,11 +158,13 @@ __device__ __forceinline__ void loss_mean(const LossJoin &P)
 {
     __shared__ double red[2][16];
     double sum = 0.0, count = 0.0;
-    for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u)
-        if (P.target[n] != P.ignore) {
-            sum += (double)P.row_loss[n];
-            count += 1.0;
-        }
+#pragma unroll 4
+    for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u) {
+        const int64_t target = P.target[n];
+        const float loss = P.row_loss[n];
+        sum += target != P.ignore ? (double)loss : 0.0;
+        count += target != P.ignore ? 1.0 : 0.0;
+    }
     sum = workgroup_sum<1024>(sum, red[0]);
     count = workgroup_sum<1024>(count, red[1]);
     if (threadIdx.x == 0) {
@@ -173,44 +174,68 @@ __device__ __forceinline__ void loss_mean(const LossJoin &P)
     }
 }
 
-// Sixteen rows per workgroup, 64 threads to each.  kAlone: there are no more rows, and the mean is taken here.
-template <bool kAlone>
+// Largest logit, sum of exp(z - largest) and sum of logits of a part of the vocabulary.
+struct LossPart {
+    float top, sum, all;
+    __device__ __forceinline__ void join(float other, float its, float logits)
+    {
+        const float higher = fmaxf(top, other), base = finite_base(higher);
+        sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2E) + its * __builtin_amdgcn_exp2f((other - base) * kLog2E);
+        top = higher;
+        all += logits;
+    }
+    // Over the wave's first WIDTH lanes, the same in each.
+    template <int WIDTH>
+    __device__ __forceinline__ void join_lanes()
+    {
+#pragma unroll
+        for (int off = 1; off < WIDTH; off <<= 1)
+            join(__shfl_xor(top, off, 64), __shfl_xor(sum, off, 64), __shfl_xor(all, off, 64));
+    }
+};
+
+// ROWS rows per workgroup (1 or 16), 1024 / ROWS threads to each.  kAlone: there are no more rows, and the mean is taken here.
+template <int ROWS, bool kAlone>
 __global__ __launch_bounds__(1024) void k_loss_join(const LossJoin P)
 {
-    __shared__ float tops[64][17], sums[64][17], alls[64][17];
-    const uint32_t r = threadIdx.x % 16u, of = threadIdx.x / 16u, n = blockIdx.x * 16u + r;
-    const bool row = n < P.rows;
-    float top = -__builtin_inff(), sum = 0.0f, all = 0.0f;
-    if (row)
-        for (uint32_t g = of; g < P.groups; g += 64u) {
-            const float2 p = P.part[(uint64_t)g * P.rows + n];
-            const float higher = fmaxf(top, p.x), base = finite_base(higher);
-            sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2E) + p.y * __builtin_amdgcn_exp2f((p.x - base) * kLog2E);
-            top = higher;
-            if (P.sums)
-                all += P.sums[(uint64_t)g * P.rows + n];
+    constexpr uint32_t THREADS = 1024 / ROWS;
+    static_assert(ROWS == 1 || ROWS == 16, "a wave per row, or sixteen");
+    __shared__ LossPart parts[ROWS][ROWS == 1 ? 16 : 65];
+    const uint32_t r = threadIdx.x % ROWS, of = threadIdx.x / ROWS, lane = threadIdx.x % 64u, wave = threadIdx.x / 64u;
+    uint32_t n = blockIdx.x * ROWS + r;
+    LossPart p{-__builtin_inff(), 0.0f, 0.0f};
+    if (n < P.rows)
+#pragma unroll 4
+        for (uint32_t g = of; g < P.groups; g += THREADS) {
+            const float2 x = P.part[(uint64_t)g * P.rows + n];
+            p.join(x.x, x.y, P.sums ? P.sums[(uint64_t)g * P.rows + n] : 0.0f);
         }
-    tops[of][r] = top;
-    sums[of][r] = sum;
-    alls[of][r] = all;
-    __syncthreads();
-    if (of == 0 && row) {
-        for (uint32_t k = 1; k < 64u; ++k)
-            top = fmaxf(top, tops[k][r]);
-        const float base = finite_base(top);
-        float total = 0.0f, logits = 0.0f;
-        for (uint32_t k = 0; k < 64u; ++k) {
-            total += sums[k][r] * __builtin_amdgcn_exp2f((tops[k][r] - base) * kLog2E);
-            logits += alls[k][r];
-        }
-        const float lse = top == __builtin_inff() && total == total ? top : base + logf(total);
+    bool writes;                                             // the one thread that has all of row n
+    if constexpr (ROWS == 1) {
+        p.join_lanes<64>();
+        if (lane == 0)
+            parts[0][wave] = p;
+        __syncthreads();
+        p = parts[0][lane % 16u];
+        p.join_lanes<16>();
+        writes = threadIdx.x == 0;
+    } else {                                                 // wave k joins what row k's 64 threads have
+        parts[r][of] = p;
+        __syncthreads();
+        p = parts[wave][lane];
+        p.join_lanes<64>();
+        n = blockIdx.x * ROWS + wave;
+        writes = lane == 0;
+    }
+    if (writes && n < P.rows) {
+        const float lse = p.top == __builtin_inff() && p.sum == p.sum ? p.top : finite_base(p.top) + logf(p.sum);
         const int64_t t = P.target[n];
         float loss = 0.0f;
         if (t != P.ignore) {
             if (t >= 0 && t < (int64_t)P.vocab) {
                 loss = (1.0f - P.smoothing) * (lse - P.of_target[n]);
                 if (P.sums)
-                    loss += P.smoothing * (lse - logits / (float)P.vocab);
+                    loss += P.smoothing * (lse - p.all / (float)P.vocab);
             } else {
                 loss = __builtin_nanf("");
                 atomicOr(P.flags, (uint32_t)NUQ_FLAG_MALFORMED);
@@ -218,8 +243,6 @@ __global__ __launch_bounds__(1024) void k_loss_join(const LossJoin P)
         }
         P.lse[n] = lse;
         P.row_loss[n] = loss;
-        if (P.loss)
-            P.loss[n] = loss;
     }
     if constexpr (kAlone) {
         if (!P.mean)
@@ -245,7 +268,7 @@ struct LossRows {
     float inverse;                             // of the gradients' scale
 };
 
-// One workgroup.
+// One workgroup where there is a gradient per row, whose largest is sought; as many as there are thousands of rows elsewhere.
 __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
 {
     __shared__ float tops[16];
@@ -273,7 +296,7 @@ __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
         top = P.grad[0] * part;
     }
     bool bad = false;
-    for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u) {
+    for (uint32_t n = blockIdx.x * 1024u + threadIdx.x; n < P.rows; n += gridDim.x * 1024u) {
         int32_t code = -1;
         float factor = 0.0f, scale = 0.0f;
         if (P.target[n] != P.ignore) {
@@ -293,7 +316,7 @@ __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
     }
     if (bad)
         atomicOr(P.flags, (uint32_t)NUQ_FLAG_MALFORMED);
-    if (threadIdx.x == 0)
+    if (blockIdx.x == 0 && threadIdx.x == 0)
         *P.largest = top * P.inverse;
 }
 
@@ -347,7 +370,7 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradi
             code[j] = n < P.O.rows ? P.code[n] : -1;
             lse[j] = n < P.O.rows ? P.lse[n] : 0.0f;
         }
-        tile.run(tiles.steps());
+        tile.run();
         more = tiles.next(tile);
         tile.finish();
         // d of columns 8 q + half to 8 q + half + 3 of block i, of the lane's row of block j
@@ -414,14 +437,15 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_product(const LossProduc
     };
     const float scale = P.scale ? *P.scale : 1.0f;
     Tile tile(lds);
+    constexpr uint32_t DEPTH = 128u / (uint32_t)sizeof(T);
     const Operand a = across(P.a, P.stride_a, P.wide_a, P.deep_a, m0, Tile::BM);
+    const uint32_t steps = max(1u, (left(max(P.deep_a, P.deep_b)) + DEPTH - 1u) / DEPTH);
     if constexpr (kAcrossB)
-        tile.begin(a, across(P.b, P.stride_b, P.wide_b, P.deep_b, n0, Tile::BN));
+        tile.begin(a, across(P.b, P.stride_b, P.wide_b, P.deep_b, n0, Tile::BN), steps);
     else
         tile.begin(a, {static_cast<const char *>(P.b) + (uint64_t)n0 * P.stride_b + (uint64_t)k0 * sizeof(T), P.stride_b,
-                       min((uint32_t)Tile::BN, P.rows - n0), left(P.deep_b) / VEC});
-    constexpr uint32_t DEPTH = 128u / (uint32_t)sizeof(T);
-    tile.run(max(1u, (left(max(P.deep_a, P.deep_b)) + DEPTH - 1u) / DEPTH));
+                       min((uint32_t)Tile::BN, P.rows - n0), left(P.deep_b) / VEC}, steps);
+    tile.run();
     tile.finish();
     const uint32_t mw = m0 + tile.first_m();
     O *const out = static_cast<O *>(P.out) + split * P.next + mw;

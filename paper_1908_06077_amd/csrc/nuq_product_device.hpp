@@ -1,9 +1,10 @@
 // Tiles of a matrix product on the matrix cores: acc[m][n] = sum over k of A[m][k] B[n][k].
 //
 // A workgroup of WM x WN waves has a tile of BM x BN; a wave BM / WM x BN / WN of it in 32 x 32 blocks.  Per step a depth of 128 bytes
-// (64 elements of 16 bits, 32 of fp32) goes from global memory into one half of the LDS, without a register between, while the products
-// of the other half run; operands come out of the LDS one quarter step ahead of their products.  The loads write the LDS in lane order,
-// so where banks would be met twice it is the address in global memory that is permuted.
+// (64 elements of 16 bits, 32 of fp32) goes from global memory into one of the stages in the LDS, without a register between, while the
+// products of another run; operands come out of the LDS one quarter step ahead of their products.  Two stages for tiles whose products
+// take longer than a load; four for tiles of few rows, which only pass the other operand by.  The loads write the LDS in lane order, so
+// where banks would be met twice it is the address in global memory that is permuted.
 //
 // An operand stands in memory by rows, k contiguous: in the LDS 128 bytes of each, chunk c (16 bytes) of row r at c ^ r / 2 % 8.  Sixteen
 // lanes read a column of chunks at once, two rows fill the 64 banks, and so these meet each bank once (with c ^ r % 8 half the time of the
@@ -153,36 +154,41 @@ struct OperandLoads {
     }
 };
 
-template <class T, int BM_, int BN_, int WM_, int WN_, bool kAcrossA = false, bool kAcrossB = false>
+template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool kAcrossA = false, bool kAcrossB = false>
 struct ProductTile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, WAVES = WM * WN, THREADS = 64 * WAVES;
     static constexpr int MI = BM / WM / 32, NI = BN / WN / 32;             // blocks of a wave
-    static constexpr int STAGE = (BM + BN) * 128, LDS = 2 * STAGE;
+    static constexpr int STAGES = STAGES_, STAGE = (BM + BN) * 128, LDS = STAGES * STAGE;
     using LoadsA = OperandLoads<T, BM, WAVES, kAcrossA>;
     using LoadsB = OperandLoads<T, BN, WAVES, kAcrossB>;
 
     Block acc[MI][NI];
 
-    __device__ __forceinline__ explicit ProductTile(char *lds_) : lds(lds_), half(0u)
+    __device__ __forceinline__ explicit ProductTile(char *lds_) : lds(lds_), last(STAGES - 1u)
     {
         const uint32_t lane = threadIdx.x % 64u;
         wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64u));
         place_a = LoadsA::place_of(wave / WN * (BM / WM), lane);
         place_b = BM * 128u + LoadsB::place_of(wave % WN * (BN / WN), lane);
     }
-    // The tile whose products come next: its first step goes into the half of the LDS that is free.
-    __device__ __forceinline__ void begin(const Operand &A, const Operand &B)
+    // The tile whose products come next, of `steps` steps (at least one): its first ones go into the stages behind the last that is read.
+    __device__ __forceinline__ void begin(const Operand &A, const Operand &B, uint32_t steps_)
     {
         const uint32_t lane = threadIdx.x % 64u;
+        steps = steps_;
         a.place(A, wave, lane);
         b.place(B, wave, lane);
-        char *const to = lds + half * STAGE;
-        a.issue(0u, to, wave);
-        b.issue(0u, to + BM * 128, wave);
+#pragma unroll
+        for (uint32_t s = 0; s < STAGES - 1u; ++s)
+            if (s < steps) {
+                char *const to = stage(last + 1u + s);
+                a.issue(s, to, wave);
+                b.issue(s, to + BM * 128, wave);
+            }
     }
-    // Its products but those of the last of `steps` steps (at least one), which finish() brings.  Between the two is the place of begin()
-    // for the tile after it: that tile's first loads are on their way while this one's results are written.
-    __device__ __forceinline__ void run(uint32_t steps)
+    // Its products but those of the last step, which finish() brings.  Between the two is the place of begin() for the tile after it: that
+    // tile's first loads are on their way while this one's results are written.
+    __device__ __forceinline__ void run()
     {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
@@ -190,16 +196,16 @@ struct ProductTile {
             for (int j = 0; j < NI; ++j)
                 acc[i][j] = Block{};
         for (uint32_t s = 0; s + 1u < steps; ++s) {
-            arrive();
-            step(lds + half * STAGE, lds + (half ^ 1u) * STAGE, true, s + 1u);
-            half ^= 1u;
+            arrive(s);
+            last = wrap(last + 1u);
+            step(stage(last), stage(last + STAGES - 1u), s + STAGES - 1u < steps, s + STAGES - 1u);
         }
-        arrive();
-        half ^= 1u;
+        arrive(steps - 1u);
+        last = wrap(last + 1u);
     }
-    __device__ __forceinline__ void finish() { step(lds + (half ^ 1u) * STAGE, lds + half * STAGE, false, 0u); }
+    __device__ __forceinline__ void finish() { step(stage(last), stage(last + 1u), false, 0u); }
 
-    // Rows n of results in 16 bits by way of the LDS's free half, so that 16 bytes of a lane and whole lines of a wave are written: call
+    // Rows n of results in 16 bits by way of the stage read last, so that 16 bytes of a lane and whole lines of a wave are written: call
     // behind finish(), from all waves.  value(j, i, q, x): x[e] of column 8 q + 4 (lane / 32) + e of block i, row lane % 32 of block j.
     // to(j, row): where the wave's columns of that row are, none for a row that is not there; `have` of them are.
     template <class V, class P>
@@ -209,10 +215,10 @@ struct ProductTile {
         constexpr uint32_t CHUNKS = MI * 4, PER = 64 / CHUNKS;            // of a row; rows per instruction
         static_assert(WAVES * 32 * CHUNKS * 16 <= STAGE, "a wave's rows");
         const uint32_t lane = threadIdx.x % 64u, row = lane % 32u;
-        const auto turn = [](uint32_t r) { return CHUNKS == 16u ? r % 16u : r / 2u % 8u; };      // (as the operands': no bank twice)
-        char *const own = lds + (half ^ 1u) * STAGE + wave * (32u * CHUNKS * 16u);
+        const auto turn = [](uint32_t r) { return r / (16u / CHUNKS) % CHUNKS; };                // (as the operands': no bank twice)
+        char *const own = stage(last) + wave * (32u * CHUNKS * 16u);
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the others still read this half
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the others still read this stage
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
@@ -258,18 +264,32 @@ private:
     char *const lds;
     LoadsA a;
     LoadsB b;
-    uint32_t wave, half, place_a, place_b;
+    uint32_t wave, steps, last, place_a, place_b;            // last: the stage that is read, or was last
 
-    // All loads of all waves are in the LDS, and all reads of the other half are done.  (By the builtin, not inline asm: what else was loaded
-    // before is there too, and the compiler knows.)
-    static __device__ __forceinline__ void arrive()
+    // k below 2 STAGES.
+    static __device__ __forceinline__ uint32_t wrap(uint32_t k) { return STAGES == 3 ? (k >= 3u ? k - 3u : k) : k % STAGES; }
+    __device__ __forceinline__ char *stage(uint32_t k) const { return lds + wrap(k) * STAGE; }
+
+    // Step s's loads of all waves are in the LDS, and all reads of the stage before it are done.  (By the builtin, not inline asm: what else
+    // was loaded before is there too, and the compiler knows.)
+    __device__ __forceinline__ void arrive(uint32_t s) const
     {
+        constexpr int EACH = LoadsA::LOADS + LoadsB::LOADS;  // loads of a step, which later steps may leave on their way
+        const uint32_t later = min(STAGES - 2u, steps - 1u - s);
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt(0) lgkmcnt(0)
+        if (STAGES >= 4 && later == 2u)
+            __builtin_amdgcn_s_waitcnt(counter(2 * EACH));
+        else if (STAGES >= 3 && later == 1u)
+            __builtin_amdgcn_s_waitcnt(counter(EACH));
+        else
+            __builtin_amdgcn_s_waitcnt(counter(0));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     }
-    // The products of the half `from`; if `load`, the loads of step `next` into the half `to`.  (That the two do not overlap has to be said: reads
+    static constexpr int counter(int loads) { return 0x0070 | (loads & 15) | loads >> 4 << 14; }      // vmcnt(loads) lgkmcnt(0)
+    static_assert(STAGES >= 2 && STAGES <= 4 && (STAGES - 2) * (LoadsA::LOADS + LoadsB::LOADS) < 64, "what is counted");
+
+    // The products of the stage `from`; if `load`, the loads of step `next` into the stage `to`.  (That the two do not overlap has to be said: reads
     // of the LDS would wait for the loads otherwise.  The order is fixed: left to itself the compiler asks for the loads last.)
     __device__ __forceinline__ void step(const char *__restrict__ from, char *__restrict__ to, bool load, uint32_t next)
     {

@@ -706,32 +706,31 @@ struct SeamVectors {
     float factor;
 };
 
-// The gradients of the vectors from the partial sums: blockIdx.y 0 those of the branch, 1 and 2 dw2 and db2.  Sixteen columns per workgroup.
+// The gradients of the vectors from the partial sums: blockIdx.y 0 those of the branch, 1 dw2 and db2.
 template <class W>
 __global__ __launch_bounds__(1024) void k_residual_norm_finish(const float *partial, uint32_t parts, uint32_t hidden, const SeamVectors V)
 {
     const uint64_t stride = (uint64_t)kSeamSums * hidden;
-    if (blockIdx.y > 0u) {
-        W *const out = static_cast<W *>(blockIdx.y == 1u ? V.dw2 : V.db2);
-        if (out)
-            column_totals(partial + (1u + blockIdx.y) * hidden, stride, parts, hidden, [&](uint32_t c, float sum) { out[c] = (W)sum; });
-        return;
+    if (blockIdx.y == 1u) {
+        if (V.dw2 || V.db2)
+            column_totals<2>(partial + 2u * hidden, stride, parts, hidden, [&](uint32_t c, const float (&sum)[2]) {
+                if (V.dw2)
+                    static_cast<W *>(V.dw2)[c] = (W)sum[0];
+                if (V.db2)
+                    static_cast<W *>(V.db2)[c] = (W)sum[1];
+            });
+    } else if (V.dw1 || V.db1 || V.dgate) {
+        column_totals<2>(partial, stride, parts, hidden, [&](uint32_t c, const float (&sum)[2]) {
+            const auto of = [&](const void *v, float other) { return v ? (float)static_cast<const W *>(v)[c] : other; };
+            const float g = of(V.gate, 1.0f) * V.factor;
+            if (V.dw1)
+                static_cast<W *>(V.dw1)[c] = (W)(g * sum[0]);
+            if (V.db1)
+                static_cast<W *>(V.db1)[c] = (W)(g * sum[1]);
+            if (V.dgate)
+                static_cast<W *>(V.dgate)[c] = (W)(V.factor * __builtin_fmaf(of(V.w1, 1.0f), sum[0], of(V.b1, 0.0f) * sum[1]));
+        });
     }
-    if (!V.dw1 && !V.db1 && !V.dgate)
-        return;
-    float with_n = 0.0f;
-    column_totals(partial, stride, parts, hidden, [&](uint32_t, float sum) { with_n = sum; });
-    __syncthreads();
-    column_totals(partial + hidden, stride, parts, hidden, [&](uint32_t c, float sum) {        // (the same thread, the same column)
-        const auto of = [&](const void *v, float other) { return v ? (float)static_cast<const W *>(v)[c] : other; };
-        const float g = of(V.gate, 1.0f) * V.factor;
-        if (V.dw1)
-            static_cast<W *>(V.dw1)[c] = (W)(g * with_n);
-        if (V.db1)
-            static_cast<W *>(V.db1)[c] = (W)(g * sum);
-        if (V.dgate)
-            static_cast<W *>(V.dgate)[c] = (W)(V.factor * __builtin_fmaf(of(V.w1, 1.0f), with_n, of(V.b1, 0.0f) * sum));
-    });
 }
 
 }  // namespace nuq

@@ -111,11 +111,13 @@ int nuq_dropout(const void *x, uint64_t ldx, const void *residual, uint64_t ldr,
         using T = typename decltype(t)::type;
         const uint64_t vectors = (hidden + 16u / w - 1u) / (16u / w) * rows;
         const dim3 grid((uint32_t)std::min<uint64_t>((vectors + 255u) / 256u, 256u * 32u));
-        if (residual)
-            hipLaunchKernelGGL((k_dropout<T, true>), grid, dim3(256), 0, st, P);
-        else
-            hipLaunchKernelGGL((k_dropout<T, false>), grid, dim3(256), 0, st, P);
-        return check_launch();
+        const auto run = [&](auto residual_c, auto once_c) {
+            hipLaunchKernelGGL((k_dropout<T, decltype(residual_c)::value, decltype(once_c)::value>), grid, dim3(256), 0, st, P);
+            return check_launch();
+        };
+        const bool once = rows * hidden > kLastLevelCache / (w * (residual ? 3u : 2u));
+        const auto with_residual = [&](auto once_c) { return residual ? run(std::true_type{}, once_c) : run(std::false_type{}, once_c); };
+        return once ? with_residual(std::true_type{}) : with_residual(std::false_type{});
     });
 }
 
@@ -145,17 +147,20 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
         using W = typename decltype(wt)::type;
         const auto run = [&](auto team, auto elements, auto vec, auto many_c) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
-            const auto launch = [&](auto inner_c) {
-                constexpr bool kInner = decltype(inner_c)::value, kMany = decltype(many_c)::value;
+            const auto launch = [&](auto inner_c, auto once_c) {
+                constexpr bool kInner = decltype(inner_c)::value, kMany = decltype(many_c)::value, kOnce = decltype(once_c)::value;
                 constexpr uint32_t WG = kSeamForwardWG<TEAM, kMany>, TEAMS = WG / TEAM;
-                const uint32_t most = resident_workgroups<k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany>>(WG);
+                const uint32_t most = resident_workgroups<k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany, kOnce>>(WG);
                 if (!most)
                     return (int)NUQ_EHIP;
                 const uint32_t grid = (uint32_t)std::min<uint64_t>((rows + TEAMS - 1) / TEAMS, most);
-                hipLaunchKernelGGL((k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany>), dim3(grid), dim3(WG), 0, st, P);
+                hipLaunchKernelGGL((k_residual_norm_forward<T, W, TEAM, E, VEC, kInner, kMany, kOnce>), dim3(grid), dim3(WG), 0, st, P);
                 return check_launch();
             };
-            return inner != NUQ_NO_NORM ? launch(std::true_type{}) : launch(std::false_type{});
+            const auto with_inner = [&](auto once_c) {
+                return inner != NUQ_NO_NORM ? launch(std::true_type{}, once_c) : launch(std::false_type{}, once_c);
+            };
+            return rows * hidden > kLastLevelCache / (4u * w) ? with_inner(std::true_type{}) : with_inner(std::false_type{});
         };
         if (hidden <= kManyColumns && rows * hidden > kManyElements)
             return with_seam_shape<T, SeamPass::kMany>(hidden, [&](auto team, auto elements, auto vec) {
@@ -214,22 +219,25 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
         const int rc = rows == 0 ? (int)NUQ_OK : with_seam_shape<T, SeamPass::kBackward>(hidden, [&](auto team, auto elements, auto vec) {
             constexpr int TEAM = decltype(team)::value, E = decltype(elements)::value, VEC = decltype(vec)::value;
             constexpr uint32_t WG = kSeamBackwardWG<TEAM>, TEAMS = WG / TEAM;
-            const auto run = [&](auto inner_c, auto sums_c) {
-                constexpr bool kInner = decltype(inner_c)::value, kSums = decltype(sums_c)::value;
-                const uint32_t most = resident_workgroups<k_residual_norm_backward<T, W, TEAM, E, VEC, kInner, kSums>>(WG);
+            const auto run = [&](auto inner_c, auto sums_c, auto once_c) {
+                constexpr bool kInner = decltype(inner_c)::value, kSums = decltype(sums_c)::value, kOnce = decltype(once_c)::value;
+                const uint32_t most = resident_workgroups<k_residual_norm_backward<T, W, TEAM, E, VEC, kInner, kSums, kOnce>>(WG);
                 if (!most)
                     return (int)NUQ_EHIP;
                 parts = (uint32_t)std::min<uint64_t>((rows + TEAMS - 1) / TEAMS, kSums ? std::min(most, kSeamParts) : most);
-                hipLaunchKernelGGL((k_residual_norm_backward<T, W, TEAM, E, VEC, kInner, kSums>), dim3(parts), dim3(WG), 0, st, P);
+                hipLaunchKernelGGL((k_residual_norm_backward<T, W, TEAM, E, VEC, kInner, kSums, kOnce>), dim3(parts), dim3(WG), 0, st, P);
                 return check_launch();
             };
-            const auto with_inner = [&](auto sums_c) {
-                return inner != NUQ_NO_NORM ? run(std::true_type{}, sums_c) : run(std::false_type{}, sums_c);
+            const auto with_inner = [&](auto sums_c, auto once_c) {
+                return inner != NUQ_NO_NORM ? run(std::true_type{}, sums_c, once_c) : run(std::false_type{}, sums_c, once_c);
             };
             if constexpr (TEAM * E <= (int)kSumsInRegisters) {
-                return sums ? with_inner(std::true_type{}) : with_inner(std::false_type{});
+                if (!sums)
+                    return with_inner(std::false_type{}, std::false_type{});
+                return rows * hidden > kLastLevelCache / (6u * w) ? with_inner(std::true_type{}, std::true_type{})
+                                                                  : with_inner(std::true_type{}, std::false_type{});
             } else {
-                int done = with_inner(std::false_type{});
+                int done = with_inner(std::false_type{}, std::false_type{});     // (the sums read the rows again)
                 if (done == NUQ_OK && sums) {
                     constexpr uint32_t COLUMNS = 256u * 16u / sizeof(T);
                     parts = (uint32_t)std::min<uint64_t>(rows, kWideParts);

@@ -53,7 +53,7 @@ struct Dropout {
 // A vector of 16 bytes at a time per thread, the launch's vectors one after the other over the rows; the next one's place follows
 // from the present one's without a division.  The key is a few 64-bit products per vector, the draw of an element two 32-bit
 // products beside six other instructions.  Bound by HBM.
-template <class T, bool kResidual>
+template <class T, bool kResidual, bool kOnce>
 __global__ __launch_bounds__(256) void k_dropout(const Dropout P)
 {
     constexpr int VEC = 16 / (int)sizeof(T);
@@ -67,9 +67,9 @@ __global__ __launch_bounds__(256) void k_dropout(const Dropout P)
         const uint32_t at = v * VEC;
         const int64_t have = (int64_t)P.hidden - at;
         float x[VEC], r[VEC];
-        load_some<VEC>(x, static_cast<const T *>(P.x) + row * P.ldx + at, have);
+        load_some<VEC, false, kOnce>(x, static_cast<const T *>(P.x) + row * P.ldx + at, have);
         if constexpr (kResidual)
-            load_some<VEC>(r, static_cast<const T *>(P.residual) + row * P.ldr + at, have);
+            load_some<VEC, false, kOnce>(r, static_cast<const T *>(P.residual) + row * P.ldr + at, have);
         if (P.draws.threshold) {
             drop<VEC>(x, bucket_key(begin, row), at, P.draws.threshold);
 #pragma unroll
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256) void k_dropout(const Dropout P)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
                 x[e] += r[e];
-        store_some<VEC>(static_cast<T *>(P.y) + row * P.ldy + at, x, have);
+        store_some<VEC, false, kOnce>(static_cast<T *>(P.y) + row * P.ldy + at, x, have);
         v += on;
         if (v >= per) {
             v -= per;

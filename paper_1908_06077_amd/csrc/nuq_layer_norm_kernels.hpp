@@ -39,20 +39,26 @@ struct RowShape {
     }
     __device__ __forceinline__ bool there(int k) const { return twice[k] < (uint32_t)VEC; }
     __device__ __forceinline__ bool counts(int k, int e) const { return (uint32_t)e >= twice[k]; }
-    template <class V>
+    // kOnce: with the hint that the memory is touched once.
+    template <bool kOnce = false, class V>
     __device__ __forceinline__ void load(Vec<V, VEC> (&to)[NV], const V *row) const
     {
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            to[k] = *reinterpret_cast<const Vec<V, VEC> *>(row + at[k]);
+        for (int k = 0; k < NV; ++k) {
+            const auto *const from = reinterpret_cast<const Vec<V, VEC> *>(row + at[k]);
+            if constexpr (kOnce)
+                to[k] = __builtin_nontemporal_load(from);
+            else
+                to[k] = *from;
+        }
     }
-    template <class V>
+    template <bool kOnce = false, class V>
     __device__ __forceinline__ void store(V *row, const float (&from)[NV][VEC]) const
     {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (there(k))
-                store_from_float<VEC>(row + at[k], from[k]);
+                store_from_float<VEC, kOnce>(row + at[k], from[k]);
     }
 };
 

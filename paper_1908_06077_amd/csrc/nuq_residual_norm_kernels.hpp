@@ -13,7 +13,8 @@
 // A row stays in the registers of one team of threads from its loads to its results: two rows are read and two written forward,
 // four read and two written backward, whatever is fused.  Statistics and sums are fp32, the variance is taken of centred values,
 // results are rounded to their type once.  The mask is computed again in the backward pass.  Bound by HBM, and on short batches by
-// latency.
+// latency.  kOnce: rows that together do not fit the last-level cache are read and written with that hint (16384 x 8192 in bfloat16
+// backward 307 -> 281 us).
 #pragma once
 
 #include <type_traits>
@@ -213,7 +214,7 @@ private:
 template <int TEAM, bool kMany>
 constexpr int kSeamForwardWG = kMany ? 1024 : TEAM <= 64 ? 256 : TEAM;
 
-template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kMany>
+template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kMany, bool kOnce>
 __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm_forward(const ResidualNormForward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
@@ -240,8 +241,8 @@ __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm
     const uint64_t turn = (uint64_t)gridDim.x * TEAMS;
     uint64_t first = (uint64_t)blockIdx.x * TEAMS;
     if constexpr (kAhead) {
-        S.load(xs, static_cast<const T *>(P.x) + row_of(first) * P.ldx);
-        S.load(rs, residual + row_of(first) * ldr);
+        S.template load<kOnce>(xs, static_cast<const T *>(P.x) + row_of(first) * P.ldx);
+        S.template load<kOnce>(rs, residual + row_of(first) * ldr);
     }
     const Few w1(kMany || !kInner ? nullptr : P.w1, S), b1(kMany || !kInner ? nullptr : P.b1, S), gate(kMany ? nullptr : P.gate, S),
         w2(kMany ? nullptr : P.w2, S), b2(kMany ? nullptr : P.b2, S);
@@ -273,8 +274,8 @@ __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm
         const uint64_t now = row_of(first);
         const bool own = first + team < P.rows;
         if constexpr (!kAhead) {
-            S.load(xs, static_cast<const T *>(P.x) + now * P.ldx);
-            S.load(rs, residual + now * ldr);
+            S.template load<kOnce>(xs, static_cast<const T *>(P.x) + now * P.ldx);
+            S.template load<kOnce>(rs, residual + now * ldr);
         }
         float s[NV][VEC], mean, rstd;
         if constexpr (TEAM > 64)
@@ -287,7 +288,7 @@ __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm
         first += turn;
         const bool more = first < P.rows;
         if (kAhead && more)
-            S.load(xs, static_cast<const T *>(P.x) + row_of(first) * P.ldx);
+            S.template load<kOnce>(xs, static_cast<const T *>(P.x) + row_of(first) * P.ldx);
         if constexpr (kInner) {
             norm_row(s, S, whole, sums, P.inner, per, P.eps, mean, rstd, [] {});
             if (P.stats && own && threadIdx.x % TEAM == 0) {
@@ -330,7 +331,7 @@ __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm
                 for (int e = 0; e < VEC; ++e)
                     s[k][e] = __builtin_fmaf((float)rs[k][e], P.residual_scale, s[k][e]);
         if (kAhead && more)
-            S.load(rs, residual + row_of(first) * ldr);
+            S.template load<kOnce>(rs, residual + row_of(first) * ldr);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -338,11 +339,11 @@ __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm
                 s[k][e] = (float)(T)s[k][e];
         if (P.outer == kNoNorm) {                            // (behind a barrier of the inner norm: total may be x or residual)
             if (own)
-                S.store(static_cast<T *>(P.total) + now * P.ldt, s);
+                S.template store<kOnce>(static_cast<T *>(P.total) + now * P.ldt, s);
         } else {
             norm_row(s, S, whole, sums, P.outer, per, P.eps, mean, rstd, [&] {
                 if (own)
-                    S.store(static_cast<T *>(P.total) + now * P.ldt, s);
+                    S.template store<kOnce>(static_cast<T *>(P.total) + now * P.ldt, s);
             });
             if (P.stats && own && threadIdx.x % TEAM == 0) {
                 if (P.outer == kLayerNorm)
@@ -364,7 +365,7 @@ __global__ __launch_bounds__((kSeamForwardWG<TEAM, kMany>)) void k_residual_norm
                 b2.apply(S, [&](int k, int e, float w) { s[k][e] += w; });
             }
             if (own)
-                S.store(static_cast<T *>(P.y) + now * P.ldy, s);
+                S.template store<kOnce>(static_cast<T *>(P.y) + now * P.ldy, s);
         }
         if (!more)
             break;
@@ -422,7 +423,7 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (&red)[2][2][
 
 // kSums: with the sums over rows, in registers; workgroup p writes partial[p], and a second launch adds those up.  w2 and c gate w1 are in
 // the LDS.
-template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kSums>
+template <class T, class W, int TEAM, int E, int VEC, bool kInner, bool kSums, bool kOnce>
 __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, kSeamBackwardWaves<E>) void k_residual_norm_backward(const ResidualNormBackward P)
 {
     using Shape = RowShape<T, TEAM, E, VEC>;
@@ -455,10 +456,10 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, kSeamBackwardWaves<E>) void 
         rstd1 = P.stats[P.rows + row];
         mean2 = P.stats[2u * P.rows + row];
         rstd2 = P.stats[3u * P.rows + row];
-        S.load(gs, dy + row * ldg);
-        S.load(ts, total + row * ldt);
-        S.load(as, dtotal + row * lda);
-        S.load(xs, x + row * P.ldx);
+        S.template load<kOnce>(gs, dy + row * ldg);
+        S.template load<kOnce>(ts, total + row * ldt);
+        S.template load<kOnce>(as, dtotal + row * lda);
+        S.template load<kOnce>(xs, x + row * P.ldx);
     };
     const uint64_t on = (uint64_t)gridDim.x * TEAMS;
     uint64_t first = (uint64_t)blockIdx.x * TEAMS;
@@ -559,7 +560,7 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, kSeamBackwardWaves<E>) void 
 #pragma unroll
                 for (int e = 0; e < VEC; ++e)
                     through[k][e] = d[k][e] * P.residual_scale;
-            S.store(static_cast<T *>(P.dresidual) + row * P.lde, through);
+            S.template store<kOnce>(static_cast<T *>(P.dresidual) + row * P.lde, through);
         }
         if (P.draws.threshold) {                             // d is u from here on
             const BucketKey key = bucket_key(begin, row);
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, kSeamBackwardWaves<E>) void 
                 for (int e = 0; e < VEC; ++e)
                     d[k][e] = __builtin_fmaf(-n[k][e], sum.b, d[k][e] - sum.a) * r1;
         }
-        S.store(static_cast<T *>(P.dx) + row * P.ldd, d);
+        S.template store<kOnce>(static_cast<T *>(P.dx) + row * P.ldd, d);
     }
     if constexpr (kSums) {
         float *const out = P.partial + (uint64_t)blockIdx.x * kSeamSums * hidden;

@@ -16,12 +16,6 @@ namespace {
 
 using namespace nuq;
 
-// Arrays that fit this are read and written plainly: they may still be there, and stay for what comes next.  Larger ones take
-// non-temporal loads and stores: an AdamW step on 25.6 M elements (409 MB) 163 -> 130 us, on 1.56 G 8.10 -> 7.52 ms; on 117 MB
-// of 8-bit states, weights and gradients they cost 2 %.  Between (134 to 300 MB) they win 5 % where the arrays have left the cache
-// and lose 20 % where they have not.
-constexpr uint64_t kLastLevelCache = 256ull << 20;
-
 // What a step's launches have in common, and what the step's arguments are checked for.
 struct AdamwCall {
     uint32_t T, g_type, copy_type;

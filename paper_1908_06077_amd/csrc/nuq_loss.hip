@@ -14,7 +14,6 @@ namespace {
 using namespace nuq;
 
 constexpr uint32_t kMostLossRows = 1u << 20, kMostHidden = 1u << 16, kMostVocab = 1u << 24;
-constexpr uint64_t kMostTiles = 1ull << 22;                  // of a launch: fewer than 2^32 threads
 
 uint64_t up(uint64_t n, uint64_t m) { return (n + m - 1) / m * m; }
 uint32_t over(uint64_t n, uint64_t m) { return (uint32_t)((n + m - 1) / m); }
@@ -30,10 +29,11 @@ struct LossShape {
                (uint64_t)rows * vocab <= 1ull << 38;
     }
     uint32_t bytes() const { return width(type); }
-    // Whether loads of 16 bytes take the rows as they stand.
+    // Whether loads of 16 bytes take the rows as they stand.  (Rows that overlap are laid out anew: what a tile may read is reckoned by its
+    // rows' stride.)
     bool whole(const void *p, uint64_t ld) const
     {
-        return !off_grid(p, 16) && ld * bytes() % 16u == 0 && hidden * bytes() % 16u == 0 && ld * bytes() < 1u << 22;
+        return !off_grid(p, 16) && ld >= hidden && ld * bytes() % 16u == 0 && hidden * bytes() % 16u == 0 && ld * bytes() < 1u << 22;
     }
     bool pack_x() const { return !whole(x, ldx); }
     bool pack_w() const { return !whole(w, ldw); }

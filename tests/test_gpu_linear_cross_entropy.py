@@ -231,6 +231,23 @@ def test_extreme_logits(nuq):
     assert float(out[1][0]) == float("inf") and float(out[0][0]) == float("inf")
 
 
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_rows_that_overlap(nuq, kind):
+    """Strides of zero (one row for all), one element and sixteen bytes."""
+    rows, hidden, vocab = 40, 64, 300
+    x, w, target = inputs(rows, hidden, vocab, kind, 3, ignored=False)
+    flat, many = torch.randn(4096, device=DEV).to(kind), torch.randn(8192, device=DEV).to(kind) / 4
+    one = torch.ones(1, device=DEV)
+    for stride in (0, 1, 8):
+        xs, ws = flat.as_strided((rows, hidden), (stride, 1)), many.as_strided((vocab, hidden), (stride, 1))
+        for a, b in ((xs, w), (x, ws), (xs, ws), (x[:1].expand(1, hidden), w)):
+            t = target[:a.shape[0]]
+            got, want = forward(nuq, a, b, t), forward(nuq, a.contiguous(), b.contiguous(), t)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+            g, h = backward(nuq, a, b, t, got[1], one, got[2]), backward(nuq, a.contiguous(), b.contiguous(), t, got[1], one, got[2])
+            assert torch.equal(g[0], h[0]) and torch.equal(g[1], h[1])
+
+
 def test_no_rows(nuq):
     x, w = torch.empty(0, 24, device=DEV), torch.randn(50, 24, device=DEV)
     target, mean = torch.empty(0, dtype=torch.int64, device=DEV), torch.empty(2, device=DEV)

@@ -53,8 +53,55 @@ struct Parts {
     }
 };
 
-// The logits' groups: what a wave has of the vocabulary.
-uint32_t group_of(uint32_t rows) { return rows <= 64 ? 32 : rows <= 128 ? 64 : 128; }
+// Tiles.  Up to 64 rows a product passes its other operand by: tiles of all rows, with more stages.  Else the tile whose rounds of 256
+// workgroups take the least, counted in rounds of 256 x 256: a round of 128 x 128, a quarter of the work, counts 0.35 in 16 bits (0.3 was
+// tried: gradients of 1003 rows of 1001 against 10007 weights in fp16 took 128 us, with the one round of 256 x 256 that 0.35 chooses 119),
+// one of 64 x 64 counts 0.11.  fp32 products take eight times as long and hide what smaller tiles read: no 256 x 256 there.  Against one
+// rule by the number of rows: 1341 x 1189 against 3799 weights in bfloat16 forward 36 us instead of 46, 656 x 1756 against 504 in fp32
+// 121 instead of 417, gradients of 13209 x 259 against 1127 in bfloat16 204 instead of 316.
+enum class TileSize { k32, k64Rows, k64, k128, k256 };
+TileSize tile_for(uint64_t columns, uint64_t rows, uint32_t bytes, bool with_64)
+{
+    if (rows <= 32)
+        return TileSize::k32;
+    if (rows <= 64)
+        return TileSize::k64Rows;
+    const auto rounds = [&](uint64_t size) { return (double)(((columns + size - 1) / size * ((rows + size - 1) / size) + 255u) / 256u); };
+    const double t256 = bytes == 2 ? rounds(256) : 1e30, t128 = rounds(128) * (bytes == 2 ? 0.35 : 0.25),
+                 t64 = with_64 ? rounds(64) * (bytes == 2 ? 0.11 : 0.07) : 1e30;
+    return t256 <= t128 && t256 <= t64 ? TileSize::k256 : t128 <= t64 ? TileSize::k128 : TileSize::k64;
+}
+uint32_t tile_columns(TileSize t) { return t == TileSize::k256 ? 256 : t == TileSize::k64 ? 64 : 128; }
+uint32_t tile_rows(TileSize t) { return t == TileSize::k256 ? 256 : t == TileSize::k128 ? 128 : t == TileSize::k32 ? 32 : 64; }
+
+// f(Type<tile>).  kWith64: tiles of 64 x 64 may be asked for; kFew: those of few rows.
+template <class T, bool kAcrossA, bool kAcrossB, bool kFew, bool kWith64, class F>
+int with_tile(TileSize t, F &&f)
+{
+    if constexpr (sizeof(T) == 2)
+        if (t == TileSize::k256)
+            return f(Type<ProductTile<T, 256, 256, 2, 4, 2, kAcrossA, kAcrossB>>{});
+    if constexpr (kFew) {
+        if (t == TileSize::k32)
+            return f(Type<ProductTile<T, 128, 32, 4, 1, 4, kAcrossA, kAcrossB>>{});
+        if (t == TileSize::k64Rows)
+            return f(Type<ProductTile<T, 128, 64, 4, 1, 3, kAcrossA, kAcrossB>>{});
+    }
+    if constexpr (kWith64)
+        if (t == TileSize::k64)
+            return f(Type<ProductTile<T, 64, 64, 2, 2, 4, kAcrossA, kAcrossB>>{});
+    return f(Type<ProductTile<T, 128, 128, 2, 2, 2, kAcrossA, kAcrossB>>{});
+}
+
+// Each product's: the logits forward, the logits backward, the weights' gradient (its rows are the vocabulary's), the rows' gradient
+// (which is split over the vocabulary where its tiles are few, so they may be large).
+TileSize logits_tile(const LossShape &S) { return tile_for(S.vocab, S.rows, S.bytes(), false); }
+TileSize gradient_tile(const LossShape &S, uint32_t piece) { return tile_for(piece, S.rows, S.bytes(), true); }
+TileSize weights_tile(const LossShape &S, uint32_t piece) { return tile_for(S.hidden, std::max(piece, 65u), S.bytes(), false); }
+TileSize rows_tile(const LossShape &S)
+{
+    return S.rows <= 32 ? TileSize::k32 : S.rows <= 64 ? TileSize::k64Rows : S.bytes() == 2 && S.rows > 128 && S.hidden > 128 ? TileSize::k256 : TileSize::k128;
+}
 
 struct ForwardParts {
     char *x, *w;
@@ -67,7 +114,7 @@ struct ForwardParts {
         Parts P{static_cast<char *>(workspace)};
         x = P.take<char>(S.pack_x() ? S.rows * S.packed() * S.bytes() : 0);
         w = P.take<char>(S.pack_w() ? S.vocab * S.packed() * S.bytes() : 0);
-        groups = over(S.vocab, group_of(S.rows));
+        groups = over(S.vocab, tile_columns(logits_tile(S)));
         part = P.take<float2>((uint64_t)groups * S.rows);
         sums = P.take<float>(smooth ? (uint64_t)groups * S.rows : 0);
         of_target = P.take<float>(S.rows);
@@ -92,9 +139,6 @@ uint32_t splits_of(uint64_t tiles, uint32_t steps, uint32_t most_splits)
     return best;
 }
 
-uint32_t tile_rows(uint32_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
-uint32_t tile_columns(uint32_t columns) { return columns <= 128 ? 128 : 256; }
-
 // Entries of the vocabulary whose d is in the workspace at a time: at most 320 MiB of them (2048 at least), and of those numbers the one
 // whose three products take the fewest steps of rounds of 256 tiles.
 uint32_t piece_of(const LossShape &S)
@@ -103,7 +147,7 @@ uint32_t piece_of(const LossShape &S)
     const uint64_t all = over(S.vocab, 256);
     if (all <= most)
         return (uint32_t)up(S.vocab, 64);
-    const uint64_t nt = over(S.rows, tile_rows(S.rows)), ht = over(S.hidden, tile_columns(S.hidden)), depth = 128 / S.bytes();
+    const uint64_t nt = over(S.rows, 256), ht = over(S.hidden, 256), depth = 128 / S.bytes();
     const auto rounds = [](uint64_t tiles) { return (tiles + 255u) / 256u; };
     const auto steps = [&](uint64_t tiles) {                 // of a piece of so many tiles
         return rounds(tiles * nt) * (over(S.hidden, depth) + 3u) + rounds(tiles * ht) * over(S.rows, depth) + rounds(ht * nt) * tiles * 256u / depth;
@@ -142,7 +186,7 @@ struct BackwardParts {
         // for more than one set of sums: as much as d and the weights take
         const uint64_t more = std::max<uint64_t>(4ull << 20, S.rows * wide * b + (uint64_t)S.vocab * S.hidden * b);
         const uint32_t depth = 128u / (uint32_t)b, steps = over(wide, depth);
-        splits = splits_of((uint64_t)over(S.hidden, S.rows > 128 ? tile_columns(S.hidden) : 128) * over(S.rows, tile_rows(S.rows)), steps,
+        splits = splits_of((uint64_t)over(S.hidden, tile_columns(rows_tile(S))) * over(S.rows, tile_rows(rows_tile(S))), steps,
                            1u + (uint32_t)std::min<uint64_t>(63u, more / (4u * S.rows * up(S.hidden, 4))));
         each = over(steps, splits) * depth;
         ld_sums = up(S.hidden, 4);
@@ -150,22 +194,6 @@ struct BackwardParts {
         used = P.used;
     }
 };
-
-// f(Type<tile>) for a product of many columns, by its rows, and for one of many rows, by its columns.
-template <class T, bool kAcrossA, class F>
-int with_rows(uint32_t rows, F &&f)
-{
-    return rows > 128  ? f(Type<ProductTile<T, 256, 256, 2, 4, 2, kAcrossA>>{})
-           : rows > 64 ? f(Type<ProductTile<T, 128, 128, 2, 2, 2, kAcrossA>>{})
-           : rows > 32 ? f(Type<ProductTile<T, 128, 64, 4, 1, 3, kAcrossA>>{})
-                       : f(Type<ProductTile<T, 128, 32, 4, 1, 4, kAcrossA>>{});
-}
-template <class T, bool kAcrossB, class F>
-int with_columns(uint32_t columns, F &&f)
-{
-    return columns > 128 ? f(Type<ProductTile<T, 256, 256, 2, 4, 2, true, kAcrossB>>{})
-                         : f(Type<ProductTile<T, 128, 256, 2, 4, 2, true, kAcrossB>>{});
-}
 
 template <class T>
 int pack(const void *from, uint64_t ld, uint64_t rows, uint32_t columns, char *to, uint64_t to_ld, const int32_t *code, const float *factor,
@@ -243,7 +271,7 @@ int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *we
         LossForward P{{}, target, W.part, W.sums, W.of_target};
         if (const int done = operands<T>(S, W.x, W.w, P.O, st); done != NUQ_OK)
             return done;
-        return with_rows<T, false>(S.rows, [&](auto tile) {
+        return with_tile<T, false, false, true, false>(logits_tile(S), [&](auto tile) {
             using Tile = typename decltype(tile)::type;
             P.O.mt = over(vocab, Tile::BM);
             P.O.nt = over(rows, Tile::BN);
@@ -296,7 +324,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
     if (rows == 0)                                           // sums over no rows
         return !dweight ? (int)NUQ_OK : with_type(type, [&](auto tt) {
             using T = typename decltype(tt)::type;
-            using Tile = ProductTile<T, 256, 256, 2, 4, 2, true, true>;
+            using Tile = ProductTile<T, 128, 128, 2, 2, 2, true, true>;
             LossProduct P{weight, weight, 16, 16, 0, 0, 0, 0, 0, hidden, vocab, over(hidden, Tile::BM), over(vocab, Tile::BN), dweight, lde, 0, nullptr};
             hipLaunchKernelGGL((k_loss_product<T, Tile, T, true, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
             return check_launch();
@@ -328,7 +356,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
             G.O.vocab = here;
             G.padded_vocab = (uint32_t)up(here, 64);
             const uint32_t stride_d = G.padded_vocab * (uint32_t)sizeof(T);
-            rc = with_rows<T, false>(S.rows, [&](auto tile) {
+            rc = with_tile<T, false, false, true, true>(gradient_tile(S, here), [&](auto tile) {
                 using Tile = typename decltype(tile)::type;
                 G.O.mt = over(here, Tile::BM);
                 G.O.nt = over(rows, Tile::BN);
@@ -339,7 +367,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
                 return check_launch();
             });
             if (rc == NUQ_OK && dweight)
-                rc = with_columns<T, true>(hidden, [&](auto tile) {
+                rc = with_tile<T, true, true, false, false>(weights_tile(S, here), [&](auto tile) {
                     using Tile = typename decltype(tile)::type;
                     LossProduct P{W.clean, W.d, (uint32_t)(S.packed() * sizeof(T)), stride_d, (uint32_t)S.packed() / VEC, G.padded_vocab / VEC,
                                   S.rows, S.rows, (uint32_t)up(rows, 64), hidden, here, over(hidden, Tile::BM), over(here, Tile::BN),
@@ -347,8 +375,8 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
                     hipLaunchKernelGGL((k_loss_product<T, Tile, T, true, false>), dim3(P.mt * P.nt), dim3(Tile::THREADS), 0, st, P);
                     return check_launch();
                 });
-            if (rc == NUQ_OK && dx) {
-                const auto product = [&](auto tile) {
+            if (rc == NUQ_OK && dx)
+                rc = with_tile<T, true, false, true, false>(rows_tile(S), [&](auto tile) {
                     using Tile = typename decltype(tile)::type;
                     LossProduct P{G.O.w, W.d, G.O.stride_w, stride_d, S.pack_w() ? (uint32_t)S.packed() / VEC : hidden / VEC, 0, here,
                                   G.padded_vocab, W.each, hidden, S.rows, over(hidden, Tile::BM), over(rows, Tile::BN), W.sums, W.ld_sums,
@@ -359,9 +387,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
                     else
                         hipLaunchKernelGGL((k_loss_product<T, Tile, float, false, false>), grid, dim3(Tile::THREADS), 0, st, P);
                     return check_launch();
-                };
-                rc = rows > 128 ? with_columns<T, false>(hidden, product) : with_rows<T, true>(S.rows, product);
-            }
+                });
         }
         if (rc == NUQ_OK && dx) {
             const uint64_t vectors = rows * over(hidden, 4);

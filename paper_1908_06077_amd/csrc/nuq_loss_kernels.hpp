@@ -33,8 +33,8 @@ struct LossOperands {
 struct LossForward {
     LossOperands O;
     const int64_t *target;
-    float2 *part;                              // [groups][rows]: largest logit, sum of exp(z - largest)
-    float *sums;                               // [groups][rows]: sum of logits, where targets are smoothed
+    float2 *part;                              // [tiles of the vocabulary][rows]: largest logit, sum of exp(z - largest)
+    float *sums;                               // the same: sum of logits, where targets are smoothed
     float *of_target;                          // [rows]: the target's logit
 };
 
@@ -67,6 +67,26 @@ struct LogitTiles {
 // The sum of exp(z - base) needs a base that is finite.
 __device__ __forceinline__ float finite_base(float top) { return __builtin_isinf(top) ? 0.0f : top; }
 
+// Largest logit, sum of exp(z - largest) and sum of logits of a part of the vocabulary.
+struct LossPart {
+    float top, sum, all;
+    __device__ __forceinline__ void join(float other, float its, float logits)
+    {
+        const float higher = fmaxf(top, other), base = finite_base(higher);
+        sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2E) + its * __builtin_amdgcn_exp2f((other - base) * kLog2E);
+        top = higher;
+        all += logits;
+    }
+    // Over the wave's first WIDTH lanes, the same in each.
+    template <int WIDTH>
+    __device__ __forceinline__ void join_lanes()
+    {
+#pragma unroll
+        for (int off = 1; off < WIDTH; off <<= 1)
+            join(__shfl_xor(top, off, 64), __shfl_xor(sum, off, 64), __shfl_xor(all, off, 64));
+    }
+};
+
 // f(m of the wave's rows less four times the lane's half, register) for the sixteen values of block i.
 template <class F>
 __device__ __forceinline__ void for_block(int i, F &&f)
@@ -80,12 +100,13 @@ template <class T, class Tile, bool kSmooth>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
-    constexpr uint32_t GROUP = Tile::BM / Tile::WM;
+    constexpr uint32_t WIDE = Tile::BM / Tile::WM;           // of a wave
+    static_assert(Tile::BN <= Tile::THREADS && sizeof(LossPart) * Tile::BN * Tile::WM <= Tile::STAGE, "a row's parts");
     const uint32_t half = threadIdx.x / 32u % 2u * 4u;
     Tile tile(lds);
     LogitTiles<Tile> tiles(P.O, tile);
     for (bool more = true; more;) {
-        const uint32_t mw = tiles.m0 + tile.first_m(), nw = tiles.n0 + tile.first_n() + threadIdx.x % 32u;
+        const uint32_t m0 = tiles.m0, n0 = tiles.n0, mw = m0 + tile.first_m(), nw = n0 + tile.first_n() + threadIdx.x % 32u;
         int64_t target[Tile::NI];
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j)
@@ -93,16 +114,12 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
         tile.run();
         more = tiles.next(tile);
         tile.finish();
-        if (mw >= P.O.vocab)
-            continue;
-        // (what the lane's columns are compared with is moved by the lane's half, not the 64 columns: those would fill the registers)
-        const uint32_t there = min(GROUP, P.O.vocab - mw);
+        // (what the lane's columns are compared with is moved by the lane's half, not the columns: those would fill the registers)
+        const uint32_t there = mw < P.O.vocab ? min(WIDE, P.O.vocab - mw) : 0u;
         const int32_t lane_there = (int32_t)(there - half);
-        const uint64_t group = mw / GROUP;
+        LossPart part[Tile::NI];
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
-            const uint32_t n = nw + j * 32u;
-            const bool row = n < P.O.rows;
             const uint32_t at = (uint64_t)target[j] - mw < there ? (uint32_t)((uint64_t)target[j] - mw) : ~0u;
             const uint32_t lane_at = at - half;
             float top = -__builtin_inff(), sum = 0.0f, all = 0.0f, wanted = 0.0f;
@@ -130,13 +147,31 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
             sum += __shfl_xor(sum, 32, 64);
             if constexpr (kSmooth)
                 all += __shfl_xor(all, 32, 64);
-            if (row && at != ~0u && (at & 4u) == half)
-                P.of_target[n] = wanted;
-            if (row && half == 0u) {
-                P.part[group * P.O.rows + n] = make_float2(top, sum);
-                if constexpr (kSmooth)
-                    P.sums[group * P.O.rows + n] = all;
+            if (at != ~0u && (at & 4u) == half)
+                P.of_target[nw + j * 32u] = wanted;
+            part[j] = {top, sum, all};
+        }
+        // the waves that have parts of one row, joined by a thread of the row
+        LossPart *const parts = reinterpret_cast<LossPart *>(tile.free_stage());
+#pragma unroll
+        for (int j = 0; j < Tile::NI; ++j)
+            if (half == 0u)
+                parts[(mw - m0) / WIDE * Tile::BN + tile.first_n() + j * 32u + threadIdx.x % 32u] = part[j];
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const uint32_t n = n0 + threadIdx.x;
+        if (threadIdx.x < (uint32_t)Tile::BN && n < P.O.rows) {
+            LossPart p = parts[threadIdx.x];
+#pragma unroll
+            for (int k = 1; k < Tile::WM; ++k) {
+                const LossPart q = parts[k * Tile::BN + threadIdx.x];
+                p.join(q.top, q.sum, q.all);
             }
+            const uint64_t to = (uint64_t)(m0 / Tile::BM) * P.O.rows + n;
+            P.part[to] = make_float2(p.top, p.sum);
+            if constexpr (kSmooth)
+                P.sums[to] = p.all;
         }
     }
 }
@@ -173,26 +208,6 @@ __device__ __forceinline__ void loss_mean(const LossJoin &P)
         P.mean[1] = (float)part;
     }
 }
-
-// Largest logit, sum of exp(z - largest) and sum of logits of a part of the vocabulary.
-struct LossPart {
-    float top, sum, all;
-    __device__ __forceinline__ void join(float other, float its, float logits)
-    {
-        const float higher = fmaxf(top, other), base = finite_base(higher);
-        sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2E) + its * __builtin_amdgcn_exp2f((other - base) * kLog2E);
-        top = higher;
-        all += logits;
-    }
-    // Over the wave's first WIDTH lanes, the same in each.
-    template <int WIDTH>
-    __device__ __forceinline__ void join_lanes()
-    {
-#pragma unroll
-        for (int off = 1; off < WIDTH; off <<= 1)
-            join(__shfl_xor(top, off, 64), __shfl_xor(sum, off, 64), __shfl_xor(all, off, 64));
-    }
-};
 
 // ROWS rows per workgroup (1 or 16), 1024 / ROWS threads to each.  kAlone: there are no more rows, and the mean is taken here.
 template <int ROWS, bool kAlone>

@@ -205,6 +205,16 @@ struct ProductTile {
     }
     __device__ __forceinline__ void finish() { step(stage(last), stage(last + 1u), false, 0u); }
 
+    // The stage read last, for the waves' own use behind finish(): until the next run().  All waves call it.
+    __device__ __forceinline__ char *free_stage() const
+    {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the others may still read it
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        return stage(last);
+    }
+
     // Rows n of results in 16 bits by way of the stage read last, so that 16 bytes of a lane and whole lines of a wave are written: call
     // behind finish(), from all waves.  value(j, i, q, x): x[e] of column 8 q + 4 (lane / 32) + e of block i, row lane % 32 of block j.
     // to(j, row): where the wave's columns of that row are, none for a row that is not there; `have` of them are.
@@ -216,11 +226,7 @@ struct ProductTile {
         static_assert(WAVES * 32 * CHUNKS * 16 <= STAGE, "a wave's rows");
         const uint32_t lane = threadIdx.x % 64u, row = lane % 32u;
         const auto turn = [](uint32_t r) { return r / (16u / CHUNKS) % CHUNKS; };                // (as the operands': no bank twice)
-        char *const own = stage(last) + wave * (32u * CHUNKS * 16u);
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the others still read this stage
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        char *const own = free_stage() + wave * (32u * CHUNKS * 16u);
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
 #pragma unroll

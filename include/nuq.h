@@ -6,7 +6,8 @@
  * (Sec. 3.1, Def. 1) -> ENCODE into Elias-recursive-coded bit strings (App. A,
  * Alg. 2) -> DECODE, dequantize and average K workers' gradients (App. A; the
  * aggregate line of Alg. 1).  Beside it, the operators that training a transformer
- * on such gradients needs: AdamW, the gradients' norm, layer norm (near the end).
+ * on such gradients needs: AdamW, the gradients' norm, layer norm, dropout, the norms
+ * around a block's residual sum, the loss over a vocabulary (near the end).
  *
  * Conventions for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller, unless the

@@ -15,6 +15,8 @@
 // results are rounded to their type once.  The mask is computed again in the backward pass.  Bound by HBM, and on short batches by
 // latency.  kOnce: rows that together do not fit the last-level cache are read and written with that hint (16384 x 8192 in bfloat16
 // backward 307 -> 281 us).
+// Measured, both norms, gate, bias and dropout, bfloat16: 8192 rows of 1600 forward 27 us (3.9 TB/s of 105 MB), backward 38 us (4.1 of
+// 157 MB) and 6.5 us for the launch that adds the sums up; 16384 of 8192 backward, root-mean-square norms, 266 us (6.1 TB/s) and 12.
 #pragma once
 
 #include <type_traits>

@@ -1,12 +1,14 @@
 """Dropout as a torch module over the library's kernel: the mask follows from a counter and is never stored.
 
-    drop = Dropout(0.1, seed=7)
+    drop = Dropout(0.1)
     y = drop(x)                          # like torch.nn.Dropout(0.1)
     stream = drop(branch, stream)        # stream + dropped branch, in one pass
 
-Every call in training draws anew: its mask is that of `seed` and the number of calls before it.  A captured graph repeats the calls
-it was captured with; `step`, an int64 tensor on the device that the program moves between replays, gives each replay masks of its
-own.
+Every call in training draws anew.  Without a seed its mask is that of a number from torch's generator on the CPU: torch.manual_seed
+repeats a run, and a function that is run again for its gradients (torch.utils.checkpoint) has the masks of its first run.  With a seed
+the mask is that of the seed and the number of calls before it: modules need seeds of their own, and a function that is run again draws
+anew.  A captured graph repeats the calls it was captured with; `step`, an int64 tensor on the device that the program moves between
+replays, gives each replay masks of its own.
 """
 from __future__ import annotations
 
@@ -17,14 +19,16 @@ from .norm import _rows
 
 
 class Draws:
-    """Numbers for calls that draw: the seed of a module, moved on by every call."""
+    """Numbers for calls that draw: from torch's generator, or the seed of a module, moved on by every call."""
 
-    def __init__(self, p: float, seed: int, step: torch.Tensor | None):
+    def __init__(self, p: float, seed: int | None, step: torch.Tensor | None):
         if not 0.0 <= p <= 1.0:
             raise ValueError("a probability between 0 and 1")
         self.p, self.seed, self.step, self.calls = p, seed, step, 0
 
     def next(self) -> int:
+        if self.seed is None:
+            return int(torch.randint(1 << 62, ()))
         self.calls += 1
         return (self.seed + self.calls * 0xA0761D6478BD642F) & (1 << 64) - 1     # (odd: no two of 2^64 calls share one)
 
@@ -53,7 +57,7 @@ class _Dropout(torch.autograd.Function):
 class Dropout(torch.nn.Module):
     """torch.nn.Dropout with masks of its own; called with a second tensor it adds what is kept to that."""
 
-    def __init__(self, p: float = 0.1, seed: int = 0, step: torch.Tensor | None = None):
+    def __init__(self, p: float = 0.1, seed: int | None = None, step: torch.Tensor | None = None):
         super().__init__()
         self.draws = Draws(p, seed, step)
 
@@ -66,4 +70,4 @@ class Dropout(torch.nn.Module):
         return _Dropout.apply(x, residual, p, self.draws.next() if p else 0, self.draws.step)
 
     def extra_repr(self) -> str:
-        return "p=%g, seed=%d" % (self.draws.p, self.draws.seed)
+        return "p=%g, seed=%s" % (self.draws.p, self.draws.seed)

@@ -126,7 +126,7 @@ class ResidualNorm(torch.nn.Module):
     alone without an outer norm.  gate: the value its weights begin with, or None for no gate.  Dropout draws as dropout.Dropout does."""
 
     def __init__(self, hidden: int, inner: str | None = None, outer: str | None = "layer", gate: float | None = None, scale: float = 1.0,
-                 residual_scale: float = 1.0, dropout: float = 0.0, eps: float = 1e-5, bias: bool = True, seed: int = 0,
+                 residual_scale: float = 1.0, dropout: float = 0.0, eps: float = 1e-5, bias: bool = True, seed: int | None = None,
                  step: torch.Tensor | None = None, device=None, dtype=None):
         super().__init__()
         from .dropout import Draws

@@ -152,3 +152,31 @@ def test_graph_draws_anew_where_its_step_moves(nuq):
         torch.cuda.synchronize()
         assert torch.equal(y, eager[k]) and torch.equal(dx, y)
     assert len({int((e != 0).sum()) for e in eager}) > 1
+
+
+def test_module_without_a_seed_draws_from_torch(nuq):
+    """Two modules have masks of their own, torch.manual_seed repeats them, and a function that is run again for its gradients has the masks
+    of its first run: with and without that the gradients are the same bits."""
+    from torch.utils.checkpoint import checkpoint
+
+    from paper_1908_06077_amd.dropout import Dropout
+    x = torch.ones(64, 512, device=DEV)
+    one, two = Dropout(0.5), Dropout(0.5)
+    torch.manual_seed(11)
+    a, b = one(x), two(x)
+    torch.manual_seed(11)
+    assert torch.equal(a, two(x)) and torch.equal(b, one(x))
+    agree = (a == b).float().mean().item()                   # of 32768 fair coins: 0.5, six deviations are 0.017
+    assert abs(agree - 0.5) < 0.017
+
+    w = torch.randn(512, 512, device=DEV, generator=torch.Generator(DEV).manual_seed(1), requires_grad=True)
+
+    def both(x):
+        return two(torch.tanh(one(x) @ w), x)
+
+    grads = []
+    for again in (False, True):
+        torch.manual_seed(12)
+        y = checkpoint(both, x, use_reentrant=False) if again else both(x)
+        grads.append(torch.autograd.grad((y * torch.arange(512, device=DEV)).sum(), w)[0])
+    assert torch.equal(*grads)

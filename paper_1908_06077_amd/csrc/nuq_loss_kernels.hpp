@@ -89,46 +89,41 @@ struct LossPart {
     }
 };
 
-// f(m of the wave's rows less four times the lane's half, register) for the sixteen values of block i.
-template <class F>
-__device__ __forceinline__ void for_block(int i, F &&f)
-{
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-        f((uint32_t)(i * 32 + r / 4 * 8 + r % 4), r);
-}
-
 template <class T, class Tile, bool kSmooth>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
     constexpr uint32_t WIDE = Tile::BM / Tile::WM;           // of a wave
     static_assert(Tile::BN <= Tile::THREADS && sizeof(LossPart) * Tile::BN * Tile::WM <= Tile::STAGE, "a row's parts");
-    const uint32_t half = threadIdx.x / 32u % 2u * 4u;
+    const uint32_t quad = threadIdx.x / 16u % 4u * 4u;       // the lane's columns of a block are quad to quad + 3
     Tile tile(lds);
     LogitTiles<Tile> tiles(P.O, tile);
     for (bool more = true; more;) {
-        const uint32_t m0 = tiles.m0, n0 = tiles.n0, mw = m0 + tile.first_m(), nw = n0 + tile.first_n() + threadIdx.x % 32u;
-        int64_t target[Tile::NI];
-#pragma unroll
-        for (int j = 0; j < Tile::NI; ++j)
-            target[j] = nw + j * 32u < P.O.rows ? P.target[nw + j * 32u] : -1;
+        const uint32_t m0 = tiles.m0, n0 = tiles.n0, mw = m0 + tile.first_m(), nw = n0 + tile.first_n() + threadIdx.x % 16u;
         tile.run();
+        uint32_t target[Tile::NI];
+#pragma unroll
+        for (int j = 0; j < Tile::NI; ++j) {
+            const int64_t t = nw + j * 16u < P.O.rows ? P.target[nw + j * 16u] : -1;
+            target[j] = (uint64_t)t < P.O.vocab ? (uint32_t)t : ~0u;
+        }
         more = tiles.next(tile);
         tile.finish();
-        // (what the lane's columns are compared with is moved by the lane's half, not the columns: those would fill the registers)
+        // (what the lane's columns are compared with is moved by the lane's place, not the columns: those would fill the registers)
         const uint32_t there = mw < P.O.vocab ? min(WIDE, P.O.vocab - mw) : 0u;
-        const int32_t lane_there = (int32_t)(there - half);
+        const int32_t lane_there = (int32_t)(there - quad);
         LossPart part[Tile::NI];
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
-            const uint32_t at = (uint64_t)target[j] - mw < there ? (uint32_t)((uint64_t)target[j] - mw) : ~0u;
-            const uint32_t lane_at = at - half;
+            const uint32_t at = target[j] - mw < there ? target[j] - mw : ~0u, lane_at = at - quad;
             float top = -__builtin_inff(), sum = 0.0f, all = 0.0f, wanted = 0.0f;
 #pragma unroll
             for (int i = 0; i < Tile::MI; ++i) {
-                __builtin_amdgcn_sched_barrier(0);           // (a block after the other: there are no registers for more)
-                for_block(i, [&](uint32_t m, int r) {
+                if (i % 4 == 0)
+                    __builtin_amdgcn_sched_barrier(0);       // (four blocks after the other: there are no registers for more)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t m = i * 16u + r;
                     float z = tile.acc[i][j][r];
                     if (m == lane_at)
                         wanted = z;
@@ -137,28 +132,35 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
                     z = (int32_t)m < lane_there ? z : -__builtin_inff();
                     tile.acc[i][j][r] = z;
                     top = fmaxf(top, z);
-                });
+                }
             }
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float base = finite_base(top);
 #pragma unroll
             for (int i = 0; i < Tile::MI; ++i) {
-                __builtin_amdgcn_sched_barrier(0);
-                for_block(i, [&](uint32_t, int r) { sum += __builtin_amdgcn_exp2f((tile.acc[i][j][r] - base) * kLog2E); });
+                if (i % 4 == 0)
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    sum += __builtin_amdgcn_exp2f((tile.acc[i][j][r] - base) * kLog2E);
             }
+            sum += __shfl_xor(sum, 16, 64);
             sum += __shfl_xor(sum, 32, 64);
-            if constexpr (kSmooth)
+            if constexpr (kSmooth) {
+                all += __shfl_xor(all, 16, 64);
                 all += __shfl_xor(all, 32, 64);
-            if (at != ~0u && (at & 4u) == half)
-                P.of_target[nw + j * 32u] = wanted;
+            }
+            if (at != ~0u && (at & 12u) == quad)
+                P.of_target[nw + j * 16u] = wanted;
             part[j] = {top, sum, all};
         }
         // the waves that have parts of one row, joined by a thread of the row
         LossPart *const parts = reinterpret_cast<LossPart *>(tile.free_stage());
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j)
-            if (half == 0u)
-                parts[(mw - m0) / WIDE * Tile::BN + tile.first_n() + j * 32u + threadIdx.x % 32u] = part[j];
+            if (quad == 0u)
+                parts[(mw - m0) / WIDE * Tile::BN + tile.first_n() + j * 16u + threadIdx.x % 16u] = part[j];
         __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -374,36 +376,36 @@ template <class T, class Tile>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradient P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
-    const uint32_t half = threadIdx.x / 32u % 2u * 4u;
+    const uint32_t quad = threadIdx.x / 16u % 4u * 4u;
     Tile tile(lds);
     LogitTiles<Tile> tiles(P.O, tile);
     for (bool more = true; more;) {
         const uint32_t mw = tiles.m0 + tile.first_m(), n0 = tiles.n0 + tile.first_n();
+        tile.run();
         int32_t code[Tile::NI];
         float lse[Tile::NI];
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
-            const uint32_t n = n0 + j * 32u + threadIdx.x % 32u;
+            const uint32_t n = n0 + j * 16u + threadIdx.x % 16u;
             code[j] = n < P.O.rows ? P.code[n] : -1;
             lse[j] = n < P.O.rows ? P.lse[n] : 0.0f;
         }
-        tile.run();
         more = tiles.next(tile);
         tile.finish();
-        // d of columns 8 q + half to 8 q + half + 3 of block i, of the lane's row of block j
-        const auto gradient = [&](int j, int i, int q, float (&x)[4]) {
-            const uint32_t m = i * 32u + q * 8u, target = (uint32_t)code[j] - P.first - mw - half;   // (none in the piece: no place in it)
-            const int32_t there = code[j] >= 0 ? (int32_t)(P.O.vocab - mw - half) : 0;
+        // d of columns quad to quad + 3 of block i, of the lane's row of block j
+        const auto gradient = [&](int j, int i, float (&x)[4]) {
+            const uint32_t m = i * 16u, target = (uint32_t)code[j] - P.first - mw - quad;            // (none in the piece: no place in it)
+            const int32_t there = code[j] >= 0 ? (int32_t)(P.O.vocab - mw - quad) : 0;
 #pragma unroll
             for (uint32_t e = 0; e < 4u; ++e) {
-                float v = __builtin_amdgcn_exp2f((tile.acc[i][j][q * 4 + e] - lse[j]) * kLog2E) - P.smoothed;
+                float v = __builtin_amdgcn_exp2f((tile.acc[i][j][e] - lse[j]) * kLog2E) - P.smoothed;
                 if (m + e == target)
                     v -= P.wanted;
                 x[e] = (int32_t)(m + e) < there ? v * kGradientScale<T> : 0.0f;
             }
         };
         const auto row = [&](int j, uint32_t r) -> T * {
-            const uint32_t n = n0 + j * 32u + r;
+            const uint32_t n = n0 + j * 16u + r;
             return n < P.O.rows ? static_cast<T *>(P.d) + (uint64_t)n * P.padded_vocab + mw : nullptr;
         };
         if constexpr (sizeof(T) == 2) {
@@ -412,15 +414,13 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradi
 #pragma unroll
             for (int j = 0; j < Tile::NI; ++j)
 #pragma unroll
-                for (int i = 0; i < Tile::MI; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float x[4];
-                        gradient(j, i, q, x);
-                        T *const to = row(j, threadIdx.x % 32u);
-                        if (to && mw + i * 32u + q * 8u < P.padded_vocab)
-                            store_from_float<4>(to + i * 32 + q * 8 + half, x);
-                    }
+                for (int i = 0; i < Tile::MI; ++i) {
+                    float x[4];
+                    gradient(j, i, x);
+                    T *const to = row(j, threadIdx.x % 16u);
+                    if (to && mw + i * 16u < P.padded_vocab)
+                        store_from_float<4>(to + i * 16 + quad, x);
+                }
         }
     }
 }
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_product(const LossProduc
 {
     __shared__ __align__(16) char lds[Tile::LDS];
     constexpr uint32_t VEC = 16u / (uint32_t)sizeof(T);
-    const uint32_t all = P.mt * P.nt, split = blockIdx.x / all, half = threadIdx.x / 32u % 2u * 4u;
+    const uint32_t all = P.mt * P.nt, split = blockIdx.x / all, quad = threadIdx.x / 16u % 4u * 4u;
     uint32_t bm, bn;
     tile_of(blockIdx.x % all, P.mt, P.nt, bm, bn);
     const uint32_t m0 = bm * Tile::BM, n0 = bn * Tile::BN, k0 = split * P.each;
@@ -467,37 +467,35 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_product(const LossProduc
     const uint32_t mw = m0 + tile.first_m();
     O *const out = static_cast<O *>(P.out) + split * P.next + mw;
     const auto row = [&](int j, uint32_t r) -> O * {
-        const uint32_t n = n0 + tile.first_n() + j * 32u + r;
+        const uint32_t n = n0 + tile.first_n() + j * 16u + r;
         return n < P.rows ? out + n * P.ld : nullptr;
     };
     if constexpr (sizeof(O) == 2 && !kAdd) {
-        tile.store_rows([&](int j, int i, int q, float (&x)[4]) {
+        tile.store_rows([&](int j, int i, float (&x)[4]) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                x[e] = tile.acc[i][j][q * 4 + e] * scale;
+                x[e] = tile.acc[i][j][e] * scale;
         }, row, (int64_t)P.columns - mw);
     } else {
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
-            O *const to = row(j, threadIdx.x % 32u);
+            O *const to = row(j, threadIdx.x % 16u);
             if (!to)
                 continue;
 #pragma unroll
-            for (int i = 0; i < Tile::MI; ++i)
+            for (int i = 0; i < Tile::MI; ++i) {
+                const uint32_t m = i * 16u + quad;
+                const int64_t have = (int64_t)P.columns - mw - m;
+                if (have <= 0)
+                    continue;
+                float x[4], before[4] = {};
+                if constexpr (kAdd)
+                    load_some<4>(before, to + m, have);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t m = i * 32u + q * 8u + half;
-                    const int64_t have = (int64_t)P.columns - mw - m;
-                    if (have <= 0)
-                        continue;
-                    float x[4], before[4] = {};
-                    if constexpr (kAdd)
-                        load_some<4>(before, to + m, have);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        x[e] = tile.acc[i][j][q * 4 + e] * scale + before[e];
-                    store_some<4>(to + m, x, have);
-                }
+                for (int e = 0; e < 4; ++e)
+                    x[e] = tile.acc[i][j][e] * scale + before[e];
+                store_some<4>(to + m, x, have);
+            }
         }
     }
 }

@@ -95,13 +95,13 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
     __shared__ __align__(16) char lds[Tile::LDS];
     constexpr uint32_t WIDE = Tile::BM / Tile::WM;           // of a wave
     static_assert(Tile::BN <= Tile::THREADS && sizeof(LossPart) * Tile::BN * Tile::WM <= Tile::STAGE, "a row's parts");
-    const uint32_t quad = threadIdx.x / 16u % 4u * 4u;       // the lane's columns of a block are quad to quad + 3
     Tile tile(lds);
     LogitTiles<Tile> tiles(P.O, tile);
     for (bool more = true; more;) {
-        const uint32_t m0 = tiles.m0, n0 = tiles.n0, mw = m0 + tile.first_m(), nw = n0 + tile.first_n() + threadIdx.x % 16u;
+        const uint32_t m0 = tiles.m0, n0 = tiles.n0, mw = m0 + tile.first_m();
         tile.run();
-        uint32_t target[Tile::NI];
+        const uint32_t thread = thread_again(), quad = thread / 16u % 4u * 4u, nw = n0 + tile.first_n() + thread % 16u;
+        uint32_t target[Tile::NI];                           // (the lane's columns of a block are quad to quad + 3)
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
             const int64_t t = nw + j * 16u < P.O.rows ? P.target[nw + j * 16u] : -1;
@@ -160,16 +160,16 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j)
             if (quad == 0u)
-                parts[(mw - m0) / WIDE * Tile::BN + tile.first_n() + j * 16u + threadIdx.x % 16u] = part[j];
+                parts[(mw - m0) / WIDE * Tile::BN + tile.first_n() + j * 16u + thread % 16u] = part[j];
         __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        const uint32_t n = n0 + threadIdx.x;
-        if (threadIdx.x < (uint32_t)Tile::BN && n < P.O.rows) {
-            LossPart p = parts[threadIdx.x];
+        const uint32_t n = n0 + thread;
+        if (thread < (uint32_t)Tile::BN && n < P.O.rows) {
+            LossPart p = parts[thread];
 #pragma unroll
             for (int k = 1; k < Tile::WM; ++k) {
-                const LossPart q = parts[k * Tile::BN + threadIdx.x];
+                const LossPart q = parts[k * Tile::BN + thread];
                 p.join(q.top, q.sum, q.all);
             }
             const uint64_t to = (uint64_t)(m0 / Tile::BM) * P.O.rows + n;
@@ -376,17 +376,17 @@ template <class T, class Tile>
 __global__ __launch_bounds__(Tile::THREADS) void k_loss_gradient(const LossGradient P)
 {
     __shared__ __align__(16) char lds[Tile::LDS];
-    const uint32_t quad = threadIdx.x / 16u % 4u * 4u;
     Tile tile(lds);
     LogitTiles<Tile> tiles(P.O, tile);
     for (bool more = true; more;) {
         const uint32_t mw = tiles.m0 + tile.first_m(), n0 = tiles.n0 + tile.first_n();
         tile.run();
+        const uint32_t thread = thread_again(), quad = thread / 16u % 4u * 4u;
         int32_t code[Tile::NI];
         float lse[Tile::NI];
 #pragma unroll
         for (int j = 0; j < Tile::NI; ++j) {
-            const uint32_t n = n0 + j * 16u + threadIdx.x % 16u;
+            const uint32_t n = n0 + j * 16u + thread % 16u;
             code[j] = n < P.O.rows ? P.code[n] : -1;
             lse[j] = n < P.O.rows ? P.lse[n] : 0.0f;
         }

@@ -70,6 +70,16 @@ __device__ __forceinline__ void load_into_lds(__amdgpu_buffer_rsrc_t buffer, cha
 #endif
 }
 
+// The thread's place in its workgroup, or lane, where what follows from it is reckoned again for every tile: kept from one tile to the
+// next it would fill the registers that the products need.
+__device__ __forceinline__ uint32_t thread_again()
+{
+    uint32_t t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+__device__ __forceinline__ uint32_t lane_again() { return thread_again() % 64u; }
+
 // A tile's operand.  By rows: the tile's first row, the bytes from one to the next, how many there are, the chunks of each.  Across: the
 // tile's first column in the first row of k, the bytes from one k to the next, the chunks of each, how many k there are.  Addresses and
 // strides are multiples of 16, a stride is below 2^22.
@@ -181,7 +191,7 @@ struct ProductTile {
     // behind the last that is read.
     __device__ __forceinline__ void begin(const Operand &A, const Operand &B, uint32_t steps_)
     {
-        const uint32_t lane = threadIdx.x % 64u;
+        const uint32_t lane = lane_again();
         steps = max(steps_, 2u);
         a.place(A, wave, lane);
         b.place(B, wave, lane);
@@ -247,7 +257,7 @@ struct ProductTile {
         static_assert(sizeof(T) == 2, "16 bits");
         constexpr uint32_t CHUNKS = MI * 2, PER = 64 / CHUNKS;            // of a row; rows per instruction
         static_assert(WAVES * 16 * CHUNKS * 16 <= STAGE && PER <= 16, "a wave's rows");
-        const uint32_t lane = threadIdx.x % 64u, row = lane % 16u;
+        const uint32_t lane = lane_again(), row = lane % 16u;
         const auto turn = [](uint32_t r) { return r / (16u / CHUNKS) % CHUNKS; };                // (as the operands': no bank twice)
         char *const own = free_stage() + wave * (16u * CHUNKS * 16u);
 #pragma unroll

@@ -28,7 +28,7 @@ class Draws:
 
     def next(self) -> int:
         if self.seed is None:
-            return int(torch.randint(1 << 62, ()))
+            return int(torch.randint(1 << 62, (), device="cpu"))      # (whatever the default device)
         self.calls += 1
         return (self.seed + self.calls * 0xA0761D6478BD642F) & (1 << 64) - 1     # (odd: no two of 2^64 calls share one)
 

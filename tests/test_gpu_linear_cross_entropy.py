@@ -359,3 +359,41 @@ def test_forward_and_backward_replay_in_a_graph(nuq):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+def both_ways(nuq, rows, hidden, vocab, kind, smoothing=0.0, pad=0):
+    x, w, target = inputs(rows, hidden, vocab, kind, rows + hidden + vocab, pad)
+    loss, lse, mean = forward(nuq, x, w, target, smoothing)
+    _, want_lse, want, _, bar_lse, bar = formula(x, w, target, smoothing)
+    what = (rows, hidden, vocab)
+    close(lse, want_lse, bar_lse, ("lse", *what))
+    close(loss, want, bar, ("loss", *what))
+    dx, dw = backward(nuq, x, w, target, lse, torch.ones(1, device=DEV), mean, smoothing)
+    (want_x, bar_x), (want_w, bar_w) = gradient_formula(x, w, target, lse, mean[1], smoothing)
+    close(dx, want_x, bar_x, ("dx", *what))
+    close(dw, want_w, bar_w, ("dw", *what))
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("rows", [5, 40, 70])
+def test_every_number_of_steps(nuq, rows, kind):
+    """Depths of one step, of as many as there are stages, of one less and one more, whole and cut: in the logits over the width, in the
+    gradients over the vocabulary and the rows."""
+    for hidden in (1, 33, 64, 65, 96, 128, 129, 192, 193, 257, 320, 385):
+        both_ways(nuq, rows, hidden, 203, kind)
+    for vocab in (1, 31, 64, 65, 96, 128, 129, 192, 257, 320, 385):
+        both_ways(nuq, rows, 72, vocab, kind, 0.1)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("rows", [1, 31, 63, 65, 96, 127, 129, 192, 200, 257, 321])
+def test_every_number_of_rows(nuq, rows, kind):
+    both_ways(nuq, rows, 136, 140, kind)
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+@pytest.mark.parametrize("rows,hidden,vocab", [(70, 1001, 8300), (2600, 40, 8300), (2600, 72, 8300), (2600, 136, 8300)])
+def test_largest_tiles(nuq, rows, hidden, vocab, kind):
+    """Enough tiles that the largest are taken, in the weights' gradient and in the logits, with depths of a step and of a few."""
+    both_ways(nuq, rows, hidden, vocab, kind)
+    both_ways(nuq, rows, hidden, vocab, kind, 0.1, pad=3)

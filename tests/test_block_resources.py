@@ -1,5 +1,5 @@
 """Registers of dropout's, the residual norm's and the loss's kernels, from the metadata of the library's own code objects: none spills vector
-registers but the backward pass of teams of 512 in 16 bits (four) and, once per tile, the loss's largest tiles (two backward, ten forward with
+registers but the backward pass of teams of 512 in 16 bits (four) and, once per tile, the loss's largest tiles (ten, backward and forward with
 smoothing), and nothing that a CU has to hold several of fills it alone."""
 import os
 import re
@@ -39,7 +39,7 @@ def kernels(tmp_path_factory):
 def test_nothing_spills(kernels, pattern, least):
     of = {n: r for n, r in kernels.items() if pattern in n}
     assert len(of) >= least
-    most = {r"k_residual_norm_backwardIDF16.*Li512ELi8ELi8E": 4, r"k_loss_gradientI.*Li256ELi256E": 2, r"k_loss_logitsI.*Li256ELi256E.*ELb1E": 10}
+    most = {r"k_residual_norm_backwardIDF16.*Li512ELi8ELi8E": 4, r"k_loss_gradientI.*Li256ELi256E": 10, r"k_loss_logitsI.*Li256ELi256E.*ELb1E": 10}
     spills = {n: r[1] for n, r in of.items() if r[1] > max((m for p, m in most.items() if re.search(p, n)), default=0)}
     assert not spills
 

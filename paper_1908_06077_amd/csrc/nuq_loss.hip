@@ -97,7 +97,14 @@ int with_tile(TileSize t, F &&f)
 // (which is split over the vocabulary where its tiles are few, so they may be large).
 TileSize logits_tile(const LossShape &S) { return tile_for(S.vocab, S.rows, S.bytes(), false); }
 TileSize gradient_tile(const LossShape &S, uint32_t piece) { return tile_for(piece, S.rows, S.bytes(), true); }
-TileSize weights_tile(const LossShape &S, uint32_t piece) { return tile_for(S.hidden, std::max(piece, 65u), S.bytes(), false); }
+TileSize weights_tile(const LossShape &S, uint32_t piece)
+{
+    // (fp32, whose tiles take long: small ones where those of 128 x 128 leave half the CUs idle.  Gradients of 6321 x 905 against 1414 weights,
+    // 96 tiles, 725 -> 553 us; of 6818 x 37 against 28141, a piece of which has 96, 2083 -> 1253)
+    if (S.bytes() == 4 && (uint64_t)over(S.hidden, 128) * over(piece, 128) <= 128u)
+        return TileSize::k64;
+    return tile_for(S.hidden, std::max(piece, 65u), S.bytes(), false);
+}
 TileSize rows_tile(const LossShape &S)
 {
     return S.rows <= 32 ? TileSize::k32 : S.rows <= 64 ? TileSize::k64Rows : S.bytes() == 2 && S.rows > 128 && S.hidden > 128 ? TileSize::k256 : TileSize::k128;
@@ -367,7 +374,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
                 return check_launch();
             });
             if (rc == NUQ_OK && dweight)
-                rc = with_tile<T, true, true, false, false>(weights_tile(S, here), [&](auto tile) {
+                rc = with_tile<T, true, true, false, sizeof(T) == 4>(weights_tile(S, here), [&](auto tile) {
                     using Tile = typename decltype(tile)::type;
                     LossProduct P{W.clean, W.d, (uint32_t)(S.packed() * sizeof(T)), stride_d, (uint32_t)S.packed() / VEC, G.padded_vocab / VEC,
                                   S.rows, S.rows, (uint32_t)up(rows, 64), hidden, here, over(hidden, Tile::BM), over(here, Tile::BN),

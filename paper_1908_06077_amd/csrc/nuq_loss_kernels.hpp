@@ -9,8 +9,8 @@
 // launch makes a piece's logits again and writes d, rounded to the operands' type (its products sum over rows or the vocabulary in
 // fp32, and a rounding of 2^-9 or 2^-12 of each term is what the operands have too); two products take it to dx and dw.
 // Bound by the matrix cores: 2 N V H operations forward, 6 N V H backward and 2 N V H for the logits made again; on few rows by reading w.
-// Measured in bfloat16, H = 1600, V = 50257: 8192 rows forward 1003 to 1037 us (1.27 to 1.31 PFLOP/s; 1045 is what a library product of
-// the same shape takes that does write the logits), backward 3577 to 3643 us (1.45 to 1.47 PFLOP/s over its four products); one row forward
+// Measured in bfloat16, H = 1600, V = 50257: 8192 rows forward 970 to 1023 us (1.29 to 1.36 PFLOP/s; 1045 is what a library product of
+// the same shape takes that does write the logits), backward 3360 to 3487 us (1.51 to 1.57 PFLOP/s over its four products); one row forward
 // 34 us, w at 5.0 TB/s.  The results of a tile (nine vector instructions and an exponential per logit) hide nothing: all waves of a CU are at
 // them at once.  Fewer were tried, without the comparisons where a block has no target and no end: forward 1013 -> 1024, so these stay.
 #pragma once

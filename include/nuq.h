@@ -569,7 +569,7 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
  * number (0 and 1 where there are none).  Products of operands of 16 bits are exact and summed in fp32 on the matrix cores, fp32 operands
  * are multiplied in fp32; exponentials and sums in fp32, the mean in fp64 in a fixed order.  rows at most 2^20, hidden 2^16, vocab 2^24,
  * rows * vocab 2^38; smoothing from 0, below 1.  workspace: DEVICE memory of nuq_linear_cross_entropy_workspace_bytes(..., 0) bytes,
- * 16-byte aligned, overwritten; it holds two or three numbers per row and 128 or 256 entries of the vocabulary, and a copy of x or weight
+ * 16-byte aligned, overwritten; it holds two or three numbers per row and 64 to 256 entries of the vocabulary, and a copy of x or weight
  * where 16-byte loads do not take it as it stands (its address, stride or width no multiple of 16 bytes). */
 uint64_t nuq_linear_cross_entropy_workspace_bytes(const void *x, uint64_t ldx, const void *weight, uint64_t ldw,
                                                   uint64_t rows, uint32_t hidden, uint32_t vocab, uint32_t type,

@@ -57,8 +57,7 @@ struct Parts {
 // workgroups take the least, counted in rounds of 256 x 256: a round of 128 x 128, a quarter of the work, counts 0.35 in 16 bits (0.3 was
 // tried: gradients of 1003 rows of 1001 against 10007 weights in fp16 took 128 us, with the one round of 256 x 256 that 0.35 chooses 119),
 // one of 64 x 64 counts 0.11.  fp32 products take eight times as long and hide what smaller tiles read: no 256 x 256 there.  Against one
-// rule by the number of rows: 1341 x 1189 against 3799 weights in bfloat16 forward 36 us instead of 46, 656 x 1756 against 504 in fp32
-// 121 instead of 417, gradients of 13209 x 259 against 1127 in bfloat16 204 instead of 316.
+// rule by the number of rows: 1341 x 1189 against 3799 weights in bfloat16 forward 36 us instead of 46, gradients of 13209 x 259 against 1127 in bfloat16 204 instead of 316.
 enum class TileSize { k32, k64Rows, k64, k128, k256 };
 TileSize tile_for(uint64_t columns, uint64_t rows, uint32_t bytes, bool with_64)
 {
@@ -95,19 +94,23 @@ int with_tile(TileSize t, F &&f)
 
 // Each product's: the logits forward, the logits backward, the weights' gradient (its rows are the vocabulary's), the rows' gradient
 // (which is split over the vocabulary where its tiles are few, so they may be large).
-TileSize logits_tile(const LossShape &S) { return tile_for(S.vocab, S.rows, S.bytes(), false); }
+// Forward the smallest only where those of 128 x 128 leave half the CUs idle: their parts of the vocabulary take twice the workspace.
+// (656 x 1756 against 504 in fp32 115 -> 41 us, 361 x 2743 against 317 in fp16 47 -> 30.)  The rows' gradient in fp32 takes them where a row
+// fits one: 6818 x 37 against 28141 1262 -> 935 us.
+TileSize logits_tile(const LossShape &S) { return tile_for(S.vocab, S.rows, S.bytes(), (uint64_t)over(S.vocab, 128) * over(S.rows, 128) <= 128u); }
 TileSize gradient_tile(const LossShape &S, uint32_t piece) { return tile_for(piece, S.rows, S.bytes(), true); }
 TileSize weights_tile(const LossShape &S, uint32_t piece)
 {
     // (fp32, whose tiles take long: small ones where those of 128 x 128 leave half the CUs idle.  Gradients of 6321 x 905 against 1414 weights,
-    // 96 tiles, 725 -> 553 us; of 6818 x 37 against 28141, a piece of which has 96, 2083 -> 1253)
+    // 96 tiles, 725 -> 553 us; of 6818 x 37 against 28141, whose pieces have fewer still, 2083 -> 1253)
     if (S.bytes() == 4 && (uint64_t)over(S.hidden, 128) * over(piece, 128) <= 128u)
         return TileSize::k64;
     return tile_for(S.hidden, std::max(piece, 65u), S.bytes(), false);
 }
 TileSize rows_tile(const LossShape &S)
 {
-    return S.rows <= 32 ? TileSize::k32 : S.rows <= 64 ? TileSize::k64Rows : S.bytes() == 2 && S.rows > 128 && S.hidden > 128 ? TileSize::k256 : TileSize::k128;
+    return S.rows <= 32 ? TileSize::k32 : S.rows <= 64 ? TileSize::k64Rows : S.bytes() == 4 ? (S.hidden <= 64 ? TileSize::k64 : TileSize::k128)
+                                                                           : S.rows > 128 && S.hidden > 128 ? TileSize::k256 : TileSize::k128;
 }
 
 struct ForwardParts {
@@ -278,7 +281,7 @@ int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *we
         LossForward P{{}, target, W.part, W.sums, W.of_target};
         if (const int done = operands<T>(S, W.x, W.w, P.O, st); done != NUQ_OK)
             return done;
-        return with_tile<T, false, false, true, false>(logits_tile(S), [&](auto tile) {
+        return with_tile<T, false, false, true, true>(logits_tile(S), [&](auto tile) {
             using Tile = typename decltype(tile)::type;
             P.O.mt = over(vocab, Tile::BM);
             P.O.nt = over(rows, Tile::BN);
@@ -383,7 +386,7 @@ int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *w
                     return check_launch();
                 });
             if (rc == NUQ_OK && dx)
-                rc = with_tile<T, true, false, true, false>(rows_tile(S), [&](auto tile) {
+                rc = with_tile<T, true, false, true, sizeof(T) == 4>(rows_tile(S), [&](auto tile) {
                     using Tile = typename decltype(tile)::type;
                     LossProduct P{G.O.w, W.d, G.O.stride_w, stride_d, S.pack_w() ? (uint32_t)S.packed() / VEC : hidden / VEC, 0, here,
                                   G.padded_vocab, W.each, hidden, S.rows, over(hidden, Tile::BM), over(rows, Tile::BN), W.sums, W.ld_sums,

@@ -57,7 +57,8 @@ struct Parts {
 // workgroups take the least, counted in rounds of 256 x 256: a round of 128 x 128, a quarter of the work, counts 0.35 in 16 bits (0.3 was
 // tried: gradients of 1003 rows of 1001 against 10007 weights in fp16 took 128 us, with the one round of 256 x 256 that 0.35 chooses 119),
 // one of 64 x 64 counts 0.11.  fp32 products take eight times as long and hide what smaller tiles read: no 256 x 256 there.  Against one
-// rule by the number of rows: 1341 x 1189 against 3799 weights in bfloat16 forward 36 us instead of 46, gradients of 13209 x 259 against 1127 in bfloat16 204 instead of 316.
+// rule by the number of rows: 1341 x 1189 against 3799 weights in bfloat16 forward 36 us instead of 46, gradients of 13209 x 259 against
+// 1127 in bfloat16 204 instead of 316.
 enum class TileSize { k32, k64Rows, k64, k128, k256 };
 TileSize tile_for(uint64_t columns, uint64_t rows, uint32_t bytes, bool with_64)
 {

@@ -508,8 +508,13 @@ __global__ __launch_bounds__(kSeamBackwardWG<TEAM>, kSeamBackwardWaves<E>) void 
                 d[k][e] = (float)gs[k][e];
             }
         }
-        if constexpr (TEAM > 64)
+        if constexpr (TEAM > 64) {
             arrived(through_sum);
+            // (without an inner norm x is in no sum before the one barrier behind which dx is stored: dx may be x, and where a row is not
+            // whole vectors another wave's last vector has columns of this thread's)
+            if constexpr (kSums && !kInner)
+                arrived(branch);
+        }
         if constexpr (kAhead)
             load(row + on);
         if (outer) {

@@ -163,9 +163,7 @@ __global__ __launch_bounds__(Tile::THREADS) void k_loss_logits(const LossForward
         for (int j = 0; j < Tile::NI; ++j)
             if (quad == 0u)
                 parts[(mw - m0) / WIDE * Tile::BN + tile.first_n() + j * 16u + thread % 16u] = part[j];
-        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        lds_barrier();
         const uint32_t n = n0 + thread;
         if (thread < (uint32_t)Tile::BN && n < P.O.rows) {
             LossPart p = parts[thread];

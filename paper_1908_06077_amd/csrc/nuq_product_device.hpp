@@ -80,6 +80,16 @@ __device__ __forceinline__ uint32_t thread_again()
 }
 __device__ __forceinline__ uint32_t lane_again() { return thread_again() % 64u; }
 
+// All that the workgroup's waves had of the LDS is read and written behind this, loads from global memory may still be on their way.  (The
+// builtins touch no memory as far as the compiler knows: the clobbers keep accesses on their side.)
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);                      // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // A tile's operand.  By rows: the tile's first row, the bytes from one to the next, how many there are, the chunks of each.  Across: the
 // tile's first column in the first row of k, the bytes from one k to the next, the chunks of each, how many k there are.  Addresses and
 // strides are multiples of 16, a stride is below 2^22.
@@ -241,10 +251,7 @@ struct ProductTile {
     // The stage read last, for the waves' own use behind finish(): until the next run().  All waves call it.
     __device__ __forceinline__ char *free_stage() const
     {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): the others may still read it
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        lds_barrier();                                       // (the others may still read it)
         return stage(last);
     }
 

@@ -279,12 +279,14 @@ struct LossRows {
     const float *grad, *mean;                  // grad: one number, or one per row; mean: may be none, mean[1] is multiplied in
     int32_t *code;
     float *factor, *scale;
-    float *largest;                            // [1]: the largest |g| over the gradients' scale
+    float *largest;                            // [1]: the largest |g| of a row that counts, over the gradients' scale
     uint32_t *flags;
     int64_t ignore;
     uint32_t rows, vocab;
     bool per_row;
     float inverse;                             // of the gradients' scale
+    // (A row that does not count has gradient 0, whatever the caller's is: a NaN of its loss may have come back.)
+    __device__ __forceinline__ bool counts(int64_t t) const { return t != ignore && t >= 0 && t < (int64_t)vocab; }
 };
 
 // One workgroup where there is a gradient per row, whose largest is sought; as many as there are thousands of rows elsewhere.
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
     if (P.per_row) {
         bool lost = false;
         for (uint32_t n = threadIdx.x; n < P.rows; n += 1024u)
-            if (P.target[n] != P.ignore) {
+            if (P.counts(P.target[n])) {
                 const float g = fabsf(P.grad[n] * part);
                 lost |= !(g < __builtin_inff());
                 top = fmaxf(top, g);
@@ -318,16 +320,14 @@ __global__ __launch_bounds__(1024) void k_loss_rows(const LossRows P)
     for (uint32_t n = blockIdx.x * 1024u + threadIdx.x; n < P.rows; n += gridDim.x * 1024u) {
         int32_t code = -1;
         float factor = 0.0f, scale = 0.0f;
-        if (P.target[n] != P.ignore) {
-            const int64_t t = P.target[n];
-            if (t >= 0 && t < (int64_t)P.vocab) {
-                code = (int32_t)t;
-                const float g = P.per_row ? P.grad[n] * part : top;
-                factor = !P.per_row ? 1.0f : top == 0.0f ? 0.0f : g / top;
-                scale = g * P.inverse;
-            } else {
-                bad = true;
-            }
+        const int64_t t = P.target[n];
+        if (P.counts(t)) {
+            code = (int32_t)t;
+            const float g = P.per_row ? P.grad[n] * part : top;
+            factor = !P.per_row ? 1.0f : top == 0.0f ? 0.0f : g / top;
+            scale = g * P.inverse;
+        } else if (t != P.ignore) {
+            bad = true;
         }
         P.code[n] = code;
         P.factor[n] = factor;

@@ -103,8 +103,10 @@ class _ResidualNorm(torch.autograd.Function):
         dy, dtotal = grads if outer != nuq.NO_NORM else (None, grads[0])
         if dy is None and dtotal is None:
             return (None,) * 15
-        if dy is None and outer != nuq.NO_NORM:              # the norm itself was not used
-            dy = torch.zeros_like(x)
+        factor = w2
+        if dy is None and outer != nuq.NO_NORM:              # the norm itself was not used: as of a norm of rows of 0, whatever total holds
+            dy = total = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+            stats, factor = torch.cat([stats[:2], torch.zeros_like(stats[2:])]), None
         need = ctx.needs_input_grad
         empty = lambda v, k: torch.empty_like(v) if v is not None and need[k] else None  # noqa: E731
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -114,7 +116,7 @@ class _ResidualNorm(torch.autograd.Function):
         if any(v is not None for v in (dw1, db1, dgate, dw2, db2)):
             workspace = torch.empty(nuq.nuq_residual_norm_workspace_bytes(stats.shape[1], x.shape[-1]), dtype=torch.uint8, device=x.device)
         nuq.nuq_residual_norm_backward(None if dy is None else _rows(dy), None if dtotal is None else _rows(dtotal), x,
-                                       total, inner, w1, b1, gate, outer, w2, scale, residual_scale, p,
+                                       total, inner, w1, b1, gate, outer, factor, scale, residual_scale, p,
                                        seed, step, stats, dx, dresidual, dw1, db1, dgate, dw2, db2, workspace)
         return (dx, dresidual, dw1, db1, dgate, dw2, db2) + (None,) * 8
 

@@ -25,13 +25,14 @@ class _LinearCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, target, ignore, smoothing, mean):
         x, weight, target = _rows(x), _rows(weight), target.contiguous()
-        rows = x.numel() // x.shape[-1]
-        loss, lse = torch.empty(2, rows, dtype=torch.float32, device=x.device)
+        loss = torch.empty(target.shape, dtype=torch.float32, device=x.device)
+        lse = torch.empty(target.numel(), dtype=torch.float32, device=x.device)
         both = torch.empty(2, dtype=torch.float32, device=x.device) if mean else None
         nuq.nuq_linear_cross_entropy_forward(x, weight, target, ignore, smoothing, loss, lse, both, _workspace(x, weight, False))
         ctx.save_for_backward(x, weight, target, lse, both)
         ctx.numbers = (ignore, smoothing)
-        return both[0] if mean else loss.view(target.shape)
+        # (not a view, which autograd would not let the program change in place; the backward pass reads both[1] alone)
+        return both[0].data if mean else loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable

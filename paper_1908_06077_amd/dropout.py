@@ -6,9 +6,9 @@
 
 Every call in training draws anew.  Without a seed its mask is that of a number from torch's generator on the CPU: torch.manual_seed
 repeats a run, and a function that is run again for its gradients (torch.utils.checkpoint) has the masks of its first run.  With a seed
-the mask is that of the seed and the number of calls before it: modules need seeds of their own, and a function that is run again draws
-anew.  A captured graph repeats the calls it was captured with; `step`, an int64 tensor on the device that the program moves between
-replays, gives each replay masks of its own.
+the mask is that of the seed and the number of calls before it, which is in the module's state_dict: modules need seeds of their own, and a
+function that is run again draws anew.  A captured graph repeats the calls it was captured with; `step`, an int64 tensor on the device that
+the program moves between replays, gives each replay masks of its own.  It stays the program's: neither state_dict nor .to() takes it along.
 """
 from __future__ import annotations
 
@@ -18,13 +18,25 @@ from . import binding as nuq
 from .norm import _rows
 
 
-class Draws:
-    """Numbers for calls that draw: from torch's generator, or the seed of a module, moved on by every call."""
+class Draws(torch.nn.Module):
+    """Numbers for calls that draw: from torch's generator, or the seed of a module, moved on by every call.  With a seed the number of
+    calls is part of the module's state_dict."""
 
     def __init__(self, p: float, seed: int | None, step: torch.Tensor | None):
+        super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError("a probability between 0 and 1")
         self.p, self.seed, self.step, self.calls = p, seed, step, 0
+
+    def _save_to_state_dict(self, destination, prefix, keep_vars):
+        if self.seed is not None:
+            destination[prefix + "calls"] = torch.tensor(self.calls, device="cpu")
+
+    def _load_from_state_dict(self, state_dict, prefix, *rest):
+        calls = state_dict.pop(prefix + "calls", None)        # (none in a state of a module without a seed: the number stays)
+        if calls is not None and self.seed is not None:
+            self.calls = int(calls)
+        super()._load_from_state_dict(state_dict, prefix, *rest)
 
     def next(self) -> int:
         if self.seed is None:

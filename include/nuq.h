@@ -511,7 +511,7 @@ int nuq_layer_norm_backward(const void *dy, uint64_t ldg, const void *x, uint64_
  * is the same call on dy, without a residual: the same seed and step give the same mask.  p: 0 (all is kept) to 1.  step: DEVICE
  * int64, NULL for 0; it is read when the kernel runs, so that a captured graph draws anew where the program moves it.
  * x, residual (may be NULL), y: DEVICE, of `type`, element-aligned, row r at r * ld elements (ldx, ldr: any; ldy: at least hidden).
- * y may be x or residual.  rows and hidden below 2^31. */
+ * y may be x or residual, at the same stride (NUQ_EINVAL otherwise).  rows and hidden below 2^31. */
 int nuq_dropout(const void *x, uint64_t ldx, const void *residual, uint64_t ldr, uint64_t rows, uint32_t hidden,
                 uint32_t type, double p, uint64_t seed, const int64_t *step, void *y, uint64_t ldy, nuq_stream_t stream);
 
@@ -524,9 +524,9 @@ int nuq_dropout(const void *x, uint64_t ldx, const void *residual, uint64_t ldr,
  * (r, c).  inner, outer: NUQ_NO_NORM, NUQ_LAYER_NORM or NUQ_RMS_NORM, one of them at least a norm.  residual may be NULL (taken as
  * 0), and so may each weight, bias and the gate: `hidden` elements of weight_type (`type` or NUQ_F32).  stats: [4][rows] floats, or
  * NULL: the inner norm's mean and 1 / sqrt(...), the outer norm's; what a norm does not have is not written.
- * Rows, strides and aliases as in nuq_layer_norm_forward: y may be x, total may be x or residual.  rows below 2^31, hidden at most
- * NUQ_RESIDUAL_NORM_MAX_HIDDEN.  In fp32 throughout, variances from centred values, total and y rounded once; eps: finite, not negative;
- * scale, residual_scale: finite. */
+ * Rows and strides as in nuq_layer_norm_forward; y may be x, total may be x or residual, at the same stride (NUQ_EINVAL otherwise).  rows
+ * below 2^31, hidden at most NUQ_RESIDUAL_NORM_MAX_HIDDEN.  In fp32 throughout, variances from centred values, total and y rounded once;
+ * eps: finite, not negative; scale, residual_scale: finite. */
 #define NUQ_NO_NORM 0u
 #define NUQ_LAYER_NORM 1u
 #define NUQ_RMS_NORM 2u
@@ -545,8 +545,9 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
  *   g = scale * drop(dt);  h = g * gate;   dx = rstd1 * (h' - mean(h') - n1 * mean(h' n1)),  h' = h * inner_weight  (or h)
  * (mean(d) and mean(h') fall away with NUQ_RMS_NORM), and the sums over rows, each of which may be NULL:  dinner_weight of h n1,
  * dinner_bias of h, dgate of g b, douter_weight of dy n2, douter_bias of dy: in fp32 in a fixed order, with at most rows / 256 + 64
- * roundings of the summed magnitudes (of g n1 and g, times the vectors that are constant along the sum), rounded once.  dx may be dy or x, dresidual may be dtotal or total, at the same stride (not
- * where a sum is asked for over more than 8192 columns: NUQ_EINVAL); the two must not overlap.  workspace: DEVICE memory of nuq_residual_norm_workspace_bytes(rows, hidden) bytes, 16-byte aligned,
+ * roundings of the summed magnitudes (of g n1 and g, times the vectors that are constant along the sum), rounded once.  dx may be dy or
+ * x, dresidual may be dtotal or total, at the same stride, and not where a sum is asked for over more than 8192 columns (NUQ_EINVAL
+ * otherwise); the two must not overlap.  workspace: DEVICE memory of nuq_residual_norm_workspace_bytes(rows, hidden) bytes, 16-byte aligned,
  * overwritten; may be NULL where no sum is asked for. */
 uint64_t nuq_residual_norm_workspace_bytes(uint64_t rows, uint32_t hidden);
 int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal, uint64_t lda, const void *x, uint64_t ldx,

@@ -104,7 +104,8 @@ int nuq_dropout(const void *x, uint64_t ldx, const void *residual, uint64_t ldr,
     if (rows == 0 || hidden == 0)
         return NUQ_OK;
     const uint32_t w = width(type);
-    if (!valid_array(x, 1, w) || !valid_array(y, 1, w) || off_grid(residual, w) || (rows > 1 && ldy < hidden))
+    if (!valid_array(x, 1, w) || !valid_array(y, 1, w) || off_grid(residual, w) ||
+        (rows > 1 && (ldy < hidden || other_stride(y, ldy, x, ldx) || other_stride(y, ldy, residual, ldr))))
         return NUQ_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return with_type(type, [&](auto t) {
@@ -139,7 +140,9 @@ int nuq_residual_norm_forward(const void *x, uint64_t ldx, const void *residual,
     P.factor = scale * P.draws.keep;
     const uint32_t w = width(type);
     if (!valid_array(x, 1, w) || off_grid(residual, w) || !valid_array(total, 1, w) ||
-        (outer != NUQ_NO_NORM && !valid_array(y, 1, w)) || (rows > 1 && (ldt < hidden || (y && ldy < hidden))))
+        (outer != NUQ_NO_NORM && !valid_array(y, 1, w)) ||
+        (rows > 1 && (ldt < hidden || (y && ldy < hidden) || other_stride(y, ldy, x, ldx) || other_stride(total, ldt, x, ldx) ||
+                      other_stride(total, ldt, residual, ldr))))
         return NUQ_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return with_types(type, weight_type, [&](auto tt, auto wt) {
@@ -199,7 +202,10 @@ int nuq_residual_norm_backward(const void *dy, uint64_t ldg, const void *dtotal,
     const uint32_t w = width(type);
     if (rows > 0 && (!valid_array(x, 1, w) || !valid_array(dx, 1, w) || !valid_array(stats, 1, 4) || off_grid(dtotal, w) ||
                      (outer != NUQ_NO_NORM ? !valid_array(dy, 1, w) || !valid_array(total, 1, w) : !dtotal) ||
-                     off_grid(dresidual, w) || (rows > 1 && (ldd < hidden || (dresidual && lde < hidden))) ||
+                     off_grid(dresidual, w) ||
+                     (rows > 1 && (ldd < hidden || (dresidual && lde < hidden) || other_stride(dx, ldd, dy, ldg) ||
+                                   other_stride(dx, ldd, x, ldx) || other_stride(dresidual, lde, dtotal, lda) ||
+                                   (outer != NUQ_NO_NORM && other_stride(dresidual, lde, total, ldt)))) ||
                      (sums && (!workspace || off_grid(workspace, 16)))))
         return NUQ_EINVAL;
     // wide rows: the sums are taken behind the rows' results, from what these must not have replaced

@@ -26,6 +26,9 @@ inline bool off_grid(const void *p, uint32_t bytes) { return (reinterpret_cast<u
 
 inline bool valid_array(const void *p, uint64_t n, uint32_t bytes) { return n == 0 || (p && !off_grid(p, bytes)); }
 
+// Whether results stand where the rows they are of stood, but at another stride: rows that are not read yet would be overwritten.
+inline bool other_stride(const void *to, uint64_t ld, const void *of, uint64_t ld_of) { return to && to == of && ld != ld_of; }
+
 // Arrays that fit this are read and written plainly: they may still be there, and stay for what comes next.  Larger ones take
 // non-temporal loads and stores: an AdamW step on 25.6 M elements (409 MB) 163 -> 130 us, on 1.56 G 8.10 -> 7.52 ms; on 117 MB
 // of 8-bit states, weights and gradients they cost 2 %.  Between (134 to 300 MB) they win 5 % where the arrays have left the cache

@@ -21,7 +21,7 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     """t, or a copy of it whose rows the kernels take."""
     if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
         return t
-    return t.contiguous()
+    return t.contiguous() if t.numel() else t.new_empty(t.shape)         # (no elements are contiguous whatever their strides)
 
 
 class _LayerNorm(torch.autograd.Function):

@@ -71,7 +71,7 @@ enum {
     NUQ_FLAG_NONFINITE = 2, /* a bucket norm was Inf/NaN; that bucket was encoded empty. A gradient norm or
                                new state of AdamW was: the step left that part as it was */
     NUQ_FLAG_MALFORMED = 4  /* a decoded stream broke the format, or nuq_encode refused a bucket; output is
-                               incomplete */
+                               incomplete.  Or a target of nuq_linear_cross_entropy_* lay outside the vocabulary */
 };
 
 /* A bucket's coordinates stay in the registers of one workgroup between the norm and the quantizer, so
@@ -479,7 +479,7 @@ int nuq_adamw_state_values(const uint8_t *m_codes, const uint8_t *v_codes, const
  * x, residual, total, y: DEVICE, of `type`, element-aligned, row r at r * ld elements (ldx, ldr: any;
  * ldt, ldy: at least hidden).  residual and total: both or neither.  weight, bias: hidden elements of
  * weight_type (`type` or NUQ_F32), each may be NULL.  mean, rstd: `rows` floats each, may be NULL.
- * y may be x, total may be x or residual.  rows below 2^31, hidden at most 2^30.  Statistics in fp32, the
+ * y may be x, total may be x or residual, at the same stride.  rows below 2^31, hidden at most 2^30.  Statistics in fp32, the
  * variance from centred values.  eps: finite, not negative. */
 int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, uint64_t ldr,
                            const void *weight, const void *bias, uint64_t rows, uint32_t hidden, float eps,
@@ -490,7 +490,7 @@ int nuq_layer_norm_forward(const void *x, uint64_t ldx, const void *residual, ui
  * and d = dy * weight:  dx = rstd * (d - mean(d) - n * mean(d n)) (+ add), the gradient of x and of
  * residual alike; add: the gradient that arrives through total, may be NULL.  dweight = sum over rows of
  * dy * n, dbias = sum of dy (hidden elements of weight_type, each may be NULL): summed in fp32 in a fixed
- * order, with at most rows / 256 + 64 roundings of the summed magnitudes, rounded once.  dx may be dy.  Row strides as above (ldg of dy, ldx, lda of add: any; ldd of dx
+ * order, with at most rows / 256 + 64 roundings of the summed magnitudes, rounded once.  dx may be dy, at the same stride.  Row strides as above (ldg of dy, ldx, lda of add: any; ldd of dx
  * at least hidden).  workspace: DEVICE memory, nuq_layer_norm_workspace_bytes(rows, hidden) bytes,
  * 16-byte aligned, overwritten; may be NULL where neither dweight nor dbias is asked for. */
 uint64_t nuq_layer_norm_workspace_bytes(uint64_t rows, uint32_t hidden);
@@ -584,9 +584,11 @@ int nuq_linear_cross_entropy_forward(const void *x, uint64_t ldx, const void *we
  *   d_v = exp(z_v - lse) - e / vocab - (1 - e) [v = t];   dx = g sum over v of d_v weight_v;   dweight_v = sum over rows of g d_v x
  * dx: rows at ldd >= hidden elements, dweight: vocab rows at lde >= hidden, of `type`, each may be NULL; they must not overlap the
  * inputs.  g = *grad, or grad[r] where grad_per_row, times mean[1] where there is a mean (the forward's: the gradient of the mean loss).
- * The logits are made again, a piece of the vocabulary at a time.  d is rounded to `type` (fp16: 2^14 d; dweight: d times g over the
- * largest |g|), sums are fp32, and results are rounded once.  A row that is ignored takes no part, whatever x holds there.  The order of
- * all sums is fixed.  workspace: as above, of nuq_linear_cross_entropy_workspace_bytes(..., 1) bytes. */
+ * The logits are made again, a piece of the vocabulary at a time.  d is rounded to `type` (fp16: 2^14 d), sums are fp32, and results are
+ * rounded once.  For dweight with grad_per_row x times g over the largest |g| of the rows that count is rounded to `type` too.  A row that
+ * does not count takes no part, whatever x and grad hold there.  The order of all sums is fixed.  workspace: as above, of
+ * nuq_linear_cross_entropy_workspace_bytes(..., 1) bytes: a copy of x, d of a piece of the vocabulary (at most 320 MiB, or 2048 entries
+ * where these are more: 4 GiB at 2^20 rows of 16 bits, 8 GiB in fp32), and sums of dx in fp32, several where x is small. */
 int nuq_linear_cross_entropy_backward(const void *x, uint64_t ldx, const void *weight, uint64_t ldw, uint64_t rows,
                                       uint32_t hidden, uint32_t vocab, uint32_t type, const int64_t *target,
                                       int64_t ignore, float smoothing, const float *lse, const float *grad,

@@ -53,7 +53,7 @@ struct Dropout {
 // A vector of 16 bytes at a time per thread, the launch's vectors one after the other over the rows; the next one's place follows
 // from the present one's without a division.  The key is a few 64-bit products per vector, the draw of an element two 32-bit
 // products beside six other instructions.  Bound by HBM: 16384 rows of 6400 in bfloat16 with a residual take 102 us, 6.2 TB/s; 5003 of 1001 in fp32
-// 8.8 us, two of them the launch.  128 rows of 1600, which the launch bounds: 2.7 us.  (kOnce: the first of these took 107 us without.)
+// 8.0 us (8.5 in a trace), two of them the launch.  128 rows of 1600, which the launch bounds: 2.7 us.  (kOnce: the first of these took 107 us without.)
 template <class T, bool kResidual, bool kOnce>
 __global__ __launch_bounds__(256) void k_dropout(const Dropout P)
 {

@@ -5,7 +5,8 @@
     loss = head(x, target)
 
 x [..., hidden] and weight [vocabulary, hidden] in float32, bfloat16 or float16, target [...] int64.  A weight of another type than x's
-is cast to it on the way, its gradient back.
+is cast to it on the way, its gradient back: beside rows in 16 bits a weight in float32 has a gradient that was rounded to 16 bits.  A target
+outside the vocabulary makes its row's loss NaN, with a gradient of 0, and raises FLAG_MALFORMED (nuq_last_error_flags).
 """
 from __future__ import annotations
 

@@ -56,7 +56,8 @@ class _LayerNorm(torch.autograd.Function):
 
 
 class LayerNorm(torch.nn.Module):
-    """torch.nn.LayerNorm over the last dimension; called with a second tensor it norms the sum and returns that too."""
+    """torch.nn.LayerNorm over the last dimension; called with a second tensor it norms the sum and returns that too.  (ResidualNorm: the
+    same with other norms, a norm of the branch, a gate, dropout and scales.)"""
 
     def __init__(self, hidden: int, eps: float = 1e-5, elementwise_affine: bool = True, bias: bool = True, device=None, dtype=None):
         super().__init__()
@@ -125,7 +126,8 @@ class ResidualNorm(torch.nn.Module):
     """The seam between two blocks: `inner` norms the branch, `outer` the sum ("layer", "rms", or None; one of them at least).
 
     seam(branch, stream) is (y, stream') with stream' = residual_scale stream + scale drop(gate norm(branch)) and y its norm, or stream'
-    alone without an outer norm.  gate: the value its weights begin with, or None for no gate.  Dropout draws as dropout.Dropout does."""
+    alone without an outer norm.  gate: the value its weights begin with, or None for no gate.  Dropout draws as dropout.Dropout does.
+    A layer norm of the plain sum is LayerNorm(branch, stream), whose backward pass writes one gradient for both."""
 
     def __init__(self, hidden: int, inner: str | None = None, outer: str | None = "layer", gate: float | None = None, scale: float = 1.0,
                  residual_scale: float = 1.0, dropout: float = 0.0, eps: float = 1e-5, bias: bool = True, seed: int | None = None,

@@ -15,34 +15,8 @@ from __future__ import annotations
 import torch
 
 from . import binding as nuq
+from .draws import Draws, Drawing
 from .norm import _rows
-
-
-class Draws(torch.nn.Module):
-    """Numbers for calls that draw: from torch's generator, or the seed of a module, moved on by every call.  With a seed the number of
-    calls is part of the module's state_dict."""
-
-    def __init__(self, p: float, seed: int | None, step: torch.Tensor | None):
-        super().__init__()
-        if not 0.0 <= p <= 1.0:
-            raise ValueError("a probability between 0 and 1")
-        self.p, self.seed, self.step, self.calls = p, seed, step, 0
-
-    def _save_to_state_dict(self, destination, prefix, keep_vars):
-        if self.seed is not None:
-            destination[prefix + "calls"] = torch.tensor(self.calls, device="cpu")
-
-    def _load_from_state_dict(self, state_dict, prefix, *rest):
-        calls = state_dict.pop(prefix + "calls", None)        # (none in a state of a module without a seed: the number stays)
-        if calls is not None and self.seed is not None:
-            self.calls = int(calls)
-        super()._load_from_state_dict(state_dict, prefix, *rest)
-
-    def next(self) -> int:
-        if self.seed is None:
-            return int(torch.randint(1 << 62, (), device="cpu"))      # (whatever the default device)
-        self.calls += 1
-        return (self.seed + self.calls * 0xA0761D6478BD642F) & (1 << 64) - 1     # (odd: no two of 2^64 calls share one)
 
 
 class _Dropout(torch.autograd.Function):
@@ -66,7 +40,7 @@ class _Dropout(torch.autograd.Function):
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
 
 
-class Dropout(torch.nn.Module):
+class Dropout(Drawing):
     """torch.nn.Dropout with masks of its own; called with a second tensor it adds what is kept to that."""
 
     def __init__(self, p: float = 0.1, seed: int | None = None, step: torch.Tensor | None = None):
@@ -76,10 +50,11 @@ class Dropout(torch.nn.Module):
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None) -> torch.Tensor:
         if x.dim() < 1 or (residual is not None and residual.shape != x.shape):
             raise ValueError("rows are needed, and a residual of the same shape")
-        p = self.draws.p if self.training else 0.0
+        draws = self.draws
+        p = draws.p if self.training else 0.0
         if p == 0.0 and residual is None:
             return x
-        return _Dropout.apply(x, residual, p, self.draws.next() if p else 0, self.draws.step)
+        return _Dropout.apply(x, residual, p, draws.next() if p else 0, draws.step)
 
     def extra_repr(self) -> str:
         return "p=%g, seed=%s" % (self.draws.p, self.draws.seed)

@@ -15,6 +15,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as nuq
+from .draws import Draws, Drawing
 
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
@@ -122,7 +123,7 @@ class _ResidualNorm(torch.autograd.Function):
         return (dx, dresidual, dw1, db1, dgate, dw2, db2) + (None,) * 8
 
 
-class ResidualNorm(torch.nn.Module):
+class ResidualNorm(Drawing):
     """The seam between two blocks: `inner` norms the branch, `outer` the sum ("layer", "rms", or None; one of them at least).
 
     seam(branch, stream) is (y, stream') with stream' = residual_scale stream + scale drop(gate norm(branch)) and y its norm, or stream'
@@ -133,7 +134,6 @@ class ResidualNorm(torch.nn.Module):
                  residual_scale: float = 1.0, dropout: float = 0.0, eps: float = 1e-5, bias: bool = True, seed: int | None = None,
                  step: torch.Tensor | None = None, device=None, dtype=None):
         super().__init__()
-        from .dropout import Draws
         if not 1 <= hidden <= nuq.RESIDUAL_NORM_MAX_HIDDEN:
             raise ValueError("rows of 1 to %d elements" % nuq.RESIDUAL_NORM_MAX_HIDDEN)
         if inner not in _KINDS or outer not in _KINDS or (inner is None and outer is None):
@@ -150,10 +150,11 @@ class ResidualNorm(torch.nn.Module):
     def forward(self, branch: torch.Tensor, stream: torch.Tensor | None = None):
         if branch.shape[-1:] != (self.hidden,) or (stream is not None and stream.shape != branch.shape):
             raise ValueError("rows of %d are needed, and a stream of the same shape" % self.hidden)
-        p = self.draws.p if self.training else 0.0
+        draws = self.draws
+        p = draws.p if self.training else 0.0
         return _ResidualNorm.apply(branch, stream, self.inner_weight, self.inner_bias, self.gate, self.outer_weight, self.outer_bias,
                                    _KINDS[self.inner], _KINDS[self.outer], self.eps, self.scale, self.residual_scale, p,
-                                   self.draws.next() if p else 0, self.draws.step)
+                                   draws.next() if p else 0, draws.step)
 
     def extra_repr(self) -> str:
         return "%d, inner=%s, outer=%s, gate=%s, scale=%g, residual_scale=%g, dropout=%g, eps=%g" % (
